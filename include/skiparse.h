@@ -215,6 +215,78 @@ int skiparse_attn_fwd_fp8_ex(const void* q8, const void* k8, const void* v8, con
                              void* out_bf16, int B, int heads, int T, int H, int W, int head_dim, int s, int pattern,
                              float scale, unsigned flags, void* stream);
 
+/*
+ * What stands round the attention in a transformer block: positions on q and k, the products, and what a training step keeps of them.
+ * `order` says which way rows (tokens) go, on the grid, pattern and ratio of Algorithm 1:
+ *   SKIPARSE_ORDER_SAME         rows stay where they are, in the original order (s and pattern are not looked at);
+ *   SKIPARSE_ORDER_TO_SPARSE    from the original order to the sparse layout, as skiparse_permute moves them;
+ *   SKIPARSE_ORDER_TO_ORIGINAL  from the sparse layout to the original order, as skiparse_unpermute does;
+ *   SKIPARSE_ORDER_STAY_SPARSE  rows are and stay in the sparse layout (skiparse_rope only, which has to know each row's token).
+ */
+enum { SKIPARSE_ORDER_SAME = 0, SKIPARSE_ORDER_TO_SPARSE = 1, SKIPARSE_ORDER_TO_ORIGINAL = 2, SKIPARSE_ORDER_STAY_SPARSE = 3 };
+
+/*
+ * Rotary positions on the token grid.  A head has R = rt + rh + rw turned channels (each even, R <= head_dim; the rest is copied), R/2 pairs: rt/2 that turn with
+ * the token's t, then rh/2 with h, rw/2 with w.  Pair i is channels (2i, 2i+1) (SKIPARSE_ROPE_INTERLEAVED) or (i, i + R/2) (SKIPARSE_ROPE_HALF):
+ *   y0 = x0 cos - x1 sin,  y1 = x0 sin + x1 cos.       A sequence of tokens is a grid 1 x 1 x n with rt = rh = 0.
+ * skiparse_rope_table: the table of one grid, or of a longer one: for every axis [places][pairs] (cos, sin) float32, t, h, w one after the other,
+ *   skiparse_rope_table_bytes() bytes (0 on bad arguments).  Pair j of an axis of r channels turns by place * theta^(-2j/r), changed for contexts longer than the
+ *   trained ones by `scaling` and the axis' factor:
+ *     SKIPARSE_ROPE_LINEAR  frequency / factor (position interpolation)
+ *     SKIPARSE_ROPE_NTK     theta * factor^(r/(r-2)) in the place of theta
+ *     SKIPARSE_ROPE_YARN    frequency * (g + (1-g)/factor), g = clamp((n - slow)/(fast - slow), 0, 1), n = trained * frequency / (2 pi) turns within the
+ *                           axis' trained places (YaRN's "NTK-by-parts")
+ *   cos and sin are multiplied by `attention` (1, or YaRN's correction of the logits).  Angles are formed in 64 bits.  factor >= 1, fast > slow, trained >= 1 for
+ *   YaRN; theta > 0; at most 512 channels an axis.
+ * skiparse_rope: q and, if k is not NULL, k (same shape) -> q_out, k_out.  len_t, len_h, len_w: the table's places; t0, h0, w0: where the grid begins in them
+ *   (t0 + T <= len_t for an axis with channels, as when frames follow others).  inverse = 1 turns back and is the gradient: (dq, dk) -> gradients in front of the rotation,
+ *   with `order` the other way round.  Where rows keep their places q_out may be q, and k_out k; nothing else may overlap.  dtype bf16 or float32; head_dim a multiple of 8 up to 512.
+ *   Sums in float32, one rounding.
+ */
+enum { SKIPARSE_ROPE_INTERLEAVED = 0, SKIPARSE_ROPE_HALF = 1 };                                        /* layout */
+enum { SKIPARSE_ROPE_PLAIN = 0, SKIPARSE_ROPE_LINEAR = 1, SKIPARSE_ROPE_NTK = 2, SKIPARSE_ROPE_YARN = 3 }; /* scaling */
+size_t skiparse_rope_table_bytes(int T, int H, int W, int rt, int rh, int rw);
+int skiparse_rope_table(float* table, int T, int H, int W, int rt, int rh, int rw, float theta, int scaling, float factor_t, float factor_h, float factor_w,
+                        int trained_t, int trained_h, int trained_w, float fast, float slow, float attention, void* stream);
+int skiparse_rope(const void* q, const void* k, void* q_out, void* k_out, const float* table, int B, int heads, int T, int H, int W, int head_dim, int rt, int rh,
+                  int rw, int len_t, int len_h, int len_w, int t0, int h0, int w0, int s, int pattern, int order, int layout, int inverse, int dtype, void* stream);
+
+/*
+ * 8-bit activation checkpoints: what a training step keeps of a tensor [rows][cols] (bf16 or float32) until its backward pass.  Blocks of 32 consecutive channels of
+ * a row (the last one may be shorter): codes[rows][cols] E4M3 and scales[rows][ceil(cols/32)], one byte e + 127 a block, for the smallest 2^e with
+ * |x| <= 448 * 2^e; code = rne(x * 2^-e), value = code * 2^e.  A block of zeros has byte 127.  A value that is not finite becomes NaN and does not enter the
+ * scale.  cols a multiple of 8; codes 16-byte aligned, scales at any address.  _load gives the values back in bf16 or float32 (exact in both, down to the type's
+ * smallest numbers); byte 255 stands for NaN.
+ */
+int skiparse_checkpoint_save(const void* x, void* codes, void* scales, int rows, int cols, int dtype, void* stream);
+int skiparse_checkpoint_load(const void* codes, const void* scales, void* out, int rows, int cols, int dtype, void* stream);
+
+/*
+ * Linear layer with its epilogue, bf16: z = x w^T + bias,  out = act(z) + residual.   x: [rows][in_features], w: [out_features][in_features], bias: [out_features]
+ * or NULL, residual and out: [rows][out_features] or NULL (residual only); rows = B*T*H*W (plain rows: a grid 1 x 1 x rows).  x has its rows on the one side of
+ * `order`, out, residual and pre on the other: a projection in front of a chain of sparse blocks writes the sparse layout, the one behind it reads it.
+ *   act: SKIPARSE_ACT_NONE, SKIPARSE_ACT_GELU_TANH (z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2), SKIPARSE_ACT_SILU (z / (1 + exp(-z)))
+ *   pre: NULL, or where z is kept for the backward pass: bf16 [rows][out_features] with pre_scales NULL, or the codes and scales of a checkpoint.
+ * Sums in float32; out is rounded once.  out may be residual; nothing else may overlap.  in_features and out_features multiples of 8 below 2^23; with rows that move
+ * x is less than 4 GiB.  workspace: skiparse_linear_workspace_bytes() bytes, NULL where that is 0.
+ *
+ * skiparse_linear_bwd: gradients for a loss with dL/dout = dy (rows as out's).  dz = dy act'(z),
+ *   dx = dz w + dx_add,  dw = dz^T x,  db = sum of dz over the rows;   (the residual's gradient is dy itself)
+ *   dx, dx_add, x: rows as x's; dw, db: shaped as w, bias.  Each of dx, dw, db may be NULL (not wanted), w is read for dx, x for dw; dx_add may be NULL or dx.
+ *   x: bf16 with x_scales NULL, or a checkpoint.  pre, pre_scales: what the forward call kept, not read for SKIPARSE_ACT_NONE.
+ *   dz is rounded to bf16 for the products (db is not), sums in float32, the results rounded once.  workspace: skiparse_linear_bwd_workspace_bytes() bytes
+ *   (x_checkpoint: whether x is one), NULL where that is 0.
+ */
+enum { SKIPARSE_ACT_NONE = 0, SKIPARSE_ACT_GELU_TANH = 1, SKIPARSE_ACT_SILU = 2 };
+size_t skiparse_linear_workspace_bytes(int rows, int in_features, int out_features);
+int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, void* out, void* pre, void* pre_scales, int B, int T, int H, int W,
+                        int in_features, int out_features, int s, int pattern, int order, int act, int dtype, void* workspace, size_t workspace_bytes,
+                        void* stream);
+size_t skiparse_linear_bwd_workspace_bytes(int rows, int in_features, int out_features, int order, int act, int x_checkpoint);
+int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, const void* w, const void* pre, const void* pre_scales, const void* dx_add, void* dx,
+                        void* dw, void* db, int B, int T, int H, int W, int in_features, int out_features, int s, int pattern, int order, int act, int dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text for an error code; never NULL. */
 const char* skiparse_strerror(int code);
 

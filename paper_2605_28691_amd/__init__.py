@@ -10,6 +10,7 @@ import ctypes
 import functools
 import importlib
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -22,6 +23,10 @@ FUSED = 1
 PAD = 2
 PATTERNS = {"token": TOKEN, "group": GROUP}
 OUT_LAYOUTS = {"same": 0, "other": 1, "original": 2}
+ORDERS = {"same": 0, "to_sparse": 1, "to_original": 2, "stay_sparse": 3}
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+ACTS = {"none": 0, "gelu_tanh": 1, "silu": 2}
 _DTYPES = {torch.bfloat16: BF16, torch.float32: FP32, torch.uint8: FP8_E4M3, torch.float8_e4m3fn: FP8_E4M3}
 
 _lib = None
@@ -89,6 +94,24 @@ def lib() -> ctypes.CDLL:
         L.skiparse_strerror.argtypes = [i]
         L.skiparse_last_hip_error.restype = i
         L.skiparse_last_hip_error.argtypes = []
+        L.skiparse_rope_table_bytes.restype = sz
+        L.skiparse_rope_table_bytes.argtypes = [i] * 6
+        L.skiparse_rope_table.restype = i
+        L.skiparse_rope_table.argtypes = [vp] + [i] * 6 + [f, i] + [f] * 3 + [i] * 3 + [f] * 3 + [vp]
+        L.skiparse_rope.restype = i
+        L.skiparse_rope.argtypes = [vp] * 5 + [i] * 21 + [vp]
+        L.skiparse_checkpoint_save.restype = i
+        L.skiparse_checkpoint_save.argtypes = [vp] * 3 + [i] * 3 + [vp]
+        L.skiparse_checkpoint_load.restype = i
+        L.skiparse_checkpoint_load.argtypes = [vp] * 3 + [i] * 3 + [vp]
+        L.skiparse_linear_workspace_bytes.restype = sz
+        L.skiparse_linear_workspace_bytes.argtypes = [i] * 3
+        L.skiparse_linear_fwd.restype = i
+        L.skiparse_linear_fwd.argtypes = [vp] * 7 + [i] * 11 + [vp, sz, vp]
+        L.skiparse_linear_bwd_workspace_bytes.restype = sz
+        L.skiparse_linear_bwd_workspace_bytes.argtypes = [i] * 6
+        L.skiparse_linear_bwd.restype = i
+        L.skiparse_linear_bwd.argtypes = [vp] * 10 + [i] * 11 + [vp, sz, vp]
         _bind(L)
         _lib = L
     return _lib
@@ -144,6 +167,20 @@ _TENSORS = {
     "skiparse_attn_bwd_static": (*_QKVO, (4, "dout"), (5, "lse"), (6, "dq"), (7, "dk"), (8, "dv")),
     "skiparse_quantize_fp8_ex": ((0, "x"), (1, "x8"), (2, "scales")),
     "skiparse_attn_fwd_fp8_ex": ((0, "q8"), (1, "k8"), (2, "v8"), (3, "sq"), (4, "sk"), (5, "sv"), (6, "out")),
+    "skiparse_rope_table": ((0, "table"),),
+    "skiparse_rope": ((0, "q"), (1, "k"), (2, "q_out"), (3, "k_out"), (4, "table")),
+    "skiparse_checkpoint_save": ((0, "x"), (1, "codes"), (2, "scales")),
+    "skiparse_checkpoint_load": ((0, "codes"), (1, "scales"), (2, "out")),
+    "skiparse_linear_fwd": ((0, "x"), (1, "w"), (2, "bias"), (3, "residual"), (4, "out"), (5, "pre"), (6, "pre_scales"), (18, "workspace")),
+    "skiparse_linear_bwd": ((0, "dy"), (1, "x"), (2, "x_scales"), (3, "w"), (4, "pre"), (5, "pre_scales"), (6, "dx_add"), (7, "dx"), (8, "dw"), (9, "db"),
+                            (21, "workspace")),
+}
+# Those that a call can do without.
+_OPTIONAL = {
+    "skiparse_attn_fwd": {15},  # the fused form needs no workspace
+    "skiparse_rope": {1, 3},
+    "skiparse_linear_fwd": {2, 3, 5, 6, 18},
+    "skiparse_linear_bwd": {1, 2, 3, 4, 5, 6, 7, 8, 9, 21},
 }
 
 
@@ -155,7 +192,7 @@ def _general(name: str, *args) -> None:
     """The call by way of ctypes, which takes every integer-like argument and names what it refuses."""
     args = list(args)
     for i, what in _TENSORS[name]:
-        if not (args[i] is None and (name, what) == ("skiparse_attn_fwd", "workspace")):  # the fused form needs none
+        if not (args[i] is None and i in _OPTIONAL.get(name, ())):
             args[i] = _dev(args[i], what)
     _failed(getattr(lib(), name)(*args), name)
 
@@ -423,3 +460,229 @@ def skiparse_attn_fwd_fp8(q8, k8, v8, sq, sk, sv, T: int, H: int, W: int, s: int
     _skiparse_attn_fwd_fp8_ex(q8, k8, v8, sq, sk, sv, out, B, heads, T, H, W, D, s, PATTERNS[pattern], float(scale), PAD if pad else 0,
                               _stream())
     return out
+
+
+def _here(*tensors) -> None:
+    """Calls go to the current device's stream: a tensor of another device is refused."""
+    device = torch.cuda.current_device() if _get_device is None else _get_device()
+    for t in tensors:
+        if t is not None and t.device.index not in (None, device):
+            raise ValueError(f"tensor on {t.device}, but the current device is {device}")
+
+
+def _triple(x):
+    return tuple(x) if isinstance(x, (tuple, list)) else (x, x, x)
+
+
+class RopeTable(NamedTuple):
+    """Cosines and sines of the places along the axes of a grid: `data` float32, for every axis [places][pairs][2], one after the other."""
+
+    data: torch.Tensor
+    lengths: tuple  # places of t, h, w
+    axes: tuple     # turned channels of a head that belong to t, h, w
+
+
+def skiparse_rope_table(lengths, axes, theta: float = 10000.0, scaling: str = "none", factor=1.0, trained=0, fast: float = 32.0, slow: float = 1.0,
+                        attention: float = 1.0, device="cuda", out: torch.Tensor | None = None) -> RopeTable:
+    """Table for skiparse_rope: `lengths` places along t, h, w, `axes` channels of a head that turn with each.  scaling "linear", "ntk" or "yarn" by `factor`
+    (one number, or one an axis) for contexts longer than the `trained` places (yarn); `attention` multiplies cosines and sines."""
+    (T, H, W), (rt, rh, rw) = lengths, axes
+    if out is None:
+        n = _table_bytes(T, H, W, rt, rh, rw) // 4
+        out = torch.empty(n, dtype=torch.float32, device=device)
+    elif out.dtype != torch.float32 or out.numel() * 4 != _table_bytes(T, H, W, rt, rh, rw):
+        raise ValueError("out must be float32 and of the table's size")
+    _here(out)
+    ft, fh, fw = _triple(factor)
+    nt, nh, nw = _triple(trained)
+    _skiparse_rope_table(out, T, H, W, rt, rh, rw, float(theta), ROPE_SCALINGS[scaling], float(ft), float(fh), float(fw), nt, nh, nw, float(fast), float(slow),
+                         float(attention), _stream())
+    return RopeTable(out, (T, H, W), (rt, rh, rw))
+
+
+def _table_bytes(T, H, W, rt, rh, rw) -> int:
+    n = int(lib().skiparse_rope_table_bytes(T, H, W, rt, rh, rw))
+    if n == 0:
+        raise ValueError("lengths are positive, channels even, and a table has less than 2^31 pairs")
+    return n
+
+
+def skiparse_rope(q: torch.Tensor, k: torch.Tensor | None, table: RopeTable, T: int, H: int, W: int, s: int = 1, pattern: str = "token", order: str = "same",
+                  layout: str = "interleaved", inverse: bool = False, at=(0, 0, 0), q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+    """Turns the first channels of every head of q and k by their tokens' places: (q', k'), k' None without a k.  q, k: [B][T*H*W][heads][D], or
+    [s*s*B][T*H*W/(s*s)][heads][D] for order "to_original" and "stay_sparse"; `at`: the table's place of the grid's first token along t, h, w.  inverse=True is the
+    gradient.  Where rows keep their places, q_out=q and k_out=k turn in place."""
+    n = T * H * W
+    if q.dim() != 4:
+        raise ValueError("q has four dimensions")
+    rows = q.shape[0] * q.shape[1]
+    heads, D = q.shape[2], q.shape[3]
+    s2 = s * s
+    sparse_in = order in ("to_original", "stay_sparse")
+    if n < 1 or s < 1 or rows % n or (q.shape[1] * s2 if sparse_in else q.shape[1]) != n:
+        raise ValueError("token axis does not match the grid")
+    B = rows // n
+    if k is not None and (k.shape != q.shape or k.dtype != q.dtype):
+        raise ValueError("q and k differ in shape or type")
+    if table.data.dtype != torch.float32 or table.data.numel() != 2 * sum(n_ * (r // 2) for n_, r in zip(table.lengths, table.axes)):
+        raise ValueError("the table is float32 and as long as its lengths and axes say")
+    shape = q.shape if order in ("same", "stay_sparse") else (s2 * B, n // s2, heads, D) if order == "to_sparse" else (B, n, heads, D)
+    q_out = _into(q_out, shape, q)
+    k_out = None if k is None else _into(k_out, shape, q)
+    _here(q, k, q_out, k_out, table.data)
+    _skiparse_rope(q, k, q_out, k_out, table.data, B, heads, T, H, W, D, *table.axes, *table.lengths, *at, s, PATTERNS[pattern], ORDERS[order],
+                   ROPE_LAYOUTS[layout], 1 if inverse else 0, _DTYPES[q.dtype], _stream())
+    return q_out, k_out
+
+
+def _into(out, shape, like, dtype=None):
+    """`out`, or a new tensor of that shape; one that is passed has to have it."""
+    dtype = dtype or like.dtype
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
+        raise ValueError(f"an output of shape {tuple(shape)} and type {dtype} is needed")
+    return out
+
+
+class Checkpoint(NamedTuple):
+    """An activation in 8 bits: E4M3 codes (uint8) of its shape, and one exponent byte for 32 channels of a row."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _checkpoint_of(shape, like) -> Checkpoint:
+    cols = shape[-1]
+    return Checkpoint(torch.empty(shape, dtype=torch.uint8, device=like.device), torch.empty((*shape[:-1], (cols + 31) // 32), dtype=torch.uint8, device=like.device))
+
+
+def _checked(c: Checkpoint, shape, what: str) -> Checkpoint:
+    if c.codes.dtype != torch.uint8 or c.scales.dtype != torch.uint8 or tuple(c.codes.shape) != tuple(shape) or tuple(c.scales.shape) != (*shape[:-1], (shape[-1] + 31) // 32):
+        raise ValueError(f"{what}: not a checkpoint of shape {tuple(shape)}")
+    return c
+
+
+def skiparse_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None) -> Checkpoint:
+    """[..., channels] in bf16 or float32 -> its 8-bit checkpoint, in a little over half the bytes of bf16."""
+    out = _checkpoint_of(x.shape, x) if out is None else _checked(out, x.shape, "out")
+    _here(x, *out)
+    cols = x.shape[-1]
+    _skiparse_checkpoint_save(x, out.codes, out.scales, x.numel() // max(cols, 1), cols, _DTYPES[x.dtype], _stream())
+    return out
+
+
+def skiparse_checkpoint_load(c: Checkpoint, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values that a checkpoint stands for."""
+    _checked(c, c.codes.shape, "checkpoint")
+    out = _into(out, c.codes.shape, c.codes, dtype)
+    _here(out, *c)
+    cols = out.shape[-1]
+    _skiparse_checkpoint_load(c.codes, c.scales, out, out.numel() // max(cols, 1), cols, _DTYPES[out.dtype], _stream())
+    return out
+
+
+def _linear_rows(lead, order: str, T: int, H: int, W: int, s: int):
+    """(B, T, H, W) of the rows, and the leading dimensions of the other side of `order`; `lead`: the leading dimensions of the side that rows come from."""
+    rows = 1
+    for d in lead:
+        rows *= d
+    if order == "same":
+        return (1, 1, 1, rows), lead
+    n, s2 = T * H * W, s * s
+    if n < 1 or s < 1 or rows % n or n % s2 or len(lead) != 2 or lead[1] != (n if order == "to_sparse" else n // s2):
+        raise ValueError("token axis does not match the grid")
+    B = rows // n
+    return (B, T, H, W), (s2 * B, n // s2) if order == "to_sparse" else (B, n)
+
+
+def _typed(dtype, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}")
+
+
+def skiparse_linear_fwd(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None, act: str = "none",
+                        order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", keep: str | None = None,
+                        out: torch.Tensor | None = None, pre=None, workspace: torch.Tensor | None = None):
+    """act(x w^T + bias) + residual, bf16: x [..., in], w [out, in], bias [out], residual and result [..., out].  order "to_sparse" or "to_original" moves the rows
+    of the grid T x H x W on the way: x then is [B][T*H*W][in] or [s*s*B][T*H*W/(s*s)][in], result and residual the other.  keep="bf16" or "checkpoint"
+    returns (result, values in front of the activation) for the backward pass; `out`, `pre` (what keep returns) and `workspace` are buffers to use."""
+    K, (N, Kw) = x.shape[-1], w.shape
+    if K != Kw or (bias is not None and tuple(bias.shape) != (N,)):
+        raise ValueError("x, w and bias do not fit each other")
+    _typed(torch.bfloat16, x=x, w=w, bias=bias, residual=residual)
+    grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
+    shape = (*lead, N)
+    out = _into(out, shape, x)
+    if residual is not None and tuple(residual.shape) != shape:
+        raise ValueError(f"residual must have the result's shape {shape}")
+    if keep not in (None, "bf16", "checkpoint") or (keep is None and pre is not None):
+        raise ValueError('keep is None, "bf16" or "checkpoint"')
+    codes = scales = None
+    if keep == "bf16":
+        codes = pre = _into(pre, shape, x)
+    elif keep == "checkpoint":
+        codes, scales = pre = _checkpoint_of(shape, x) if pre is None else _checked(pre, shape, "pre")
+    _here(x, w, bias, residual, out, codes, scales, workspace)
+    M = grid[0] * grid[1] * grid[2] * grid[3]
+    workspace, size = _space(workspace, x, "skiparse_linear_workspace_bytes", M, K, N)
+    _skiparse_linear_fwd(x, w, bias, residual, out, codes, scales, *grid, K, N, s, PATTERNS[pattern], ORDERS[order], ACTS[act], BF16, workspace, size, _stream())
+    return out if keep is None else (out, pre)
+
+
+@functools.lru_cache(maxsize=256)
+def _space_bytes(name: str, *sizes: int) -> int:
+    return int(getattr(lib(), name)(*sizes))
+
+
+def _space(workspace, like, name: str, *sizes):
+    """The workspace of a call and its size: the one that is passed, a new one, or none where none is needed."""
+    if workspace is not None:
+        return workspace, workspace.numel() * workspace.element_size()
+    n = _space_bytes(name, *sizes)
+    return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n else (None, 0)
+
+
+def skiparse_linear_workspace_bytes(rows: int, in_features: int, out_features: int) -> int:
+    return int(lib().skiparse_linear_workspace_bytes(rows, in_features, out_features))
+
+
+def skiparse_linear_bwd_workspace_bytes(rows: int, in_features: int, out_features: int, order: str = "same", act: str = "none", x_checkpoint: bool = False) -> int:
+    return int(lib().skiparse_linear_bwd_workspace_bytes(rows, in_features, out_features, ORDERS[order], ACTS[act], 1 if x_checkpoint else 0))
+
+
+def skiparse_linear_bwd(dy: torch.Tensor, x, w: torch.Tensor, pre=None, act: str = "none", order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1,
+                        pattern: str = "token", need_dx: bool = True, need_dw: bool = True, need_db: bool = True, dx_add: torch.Tensor | None = None,
+                        dx: torch.Tensor | None = None, dw: torch.Tensor | None = None, db: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Gradients (dx, dw, db) of skiparse_linear_fwd for dL/dresult = dy; None for one that is not needed.  x: what the forward call had, or its Checkpoint; pre: what
+    keep returned, bf16 or a Checkpoint (act "none" needs none).  dx = dz w + dx_add; dx_add may be dx.  The residual's gradient is dy."""
+    N, K = w.shape
+    xc = x.codes if isinstance(x, Checkpoint) else x
+    if xc.shape[-1] != K or dy.shape[-1] != N:
+        raise ValueError("dy, x and w do not fit each other")
+    if isinstance(x, Checkpoint):
+        _checked(x, xc.shape, "x")
+    else:
+        _typed(torch.bfloat16, x=x)
+    _typed(torch.bfloat16, dy=dy, w=w, dx_add=dx_add)
+    grid, lead = _linear_rows(xc.shape[:-1], order, T, H, W, s)
+    if tuple(dy.shape) != (*lead, N) or (dx_add is not None and dx_add.shape != xc.shape):
+        raise ValueError("dy or dx_add does not have its rows")
+    codes = scales = None
+    if act != "none":
+        if pre is None:
+            raise ValueError("an activation's gradient needs the values in front of it")
+        if isinstance(pre, Checkpoint):
+            codes, scales = _checked(pre, dy.shape, "pre")
+        else:
+            codes = _into(pre, dy.shape, dy)
+    dx = _into(dx, xc.shape, dy) if need_dx else None
+    dw = _into(dw, (N, K), dy) if need_dw else None
+    db = _into(db, (N,), dy) if need_db else None
+    xs = x.scales if isinstance(x, Checkpoint) else None
+    _here(dy, xc, xs, w, codes, scales, dx_add, dx, dw, db, workspace)
+    M = grid[0] * grid[1] * grid[2] * grid[3]
+    workspace, size = _space(workspace, dy, "skiparse_linear_bwd_workspace_bytes", M, K, N, ORDERS[order], ACTS[act], 0 if xs is None else 1)
+    _skiparse_linear_bwd(dy, xc, xs, w, codes, scales, dx_add, dx, dw, db, *grid, K, N, s, PATTERNS[pattern], ORDERS[order], ACTS[act], BF16, workspace, size, _stream())
+    return dx, dw, db

@@ -4,6 +4,7 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
 #include <mutex>
 
 #include "kernels.h"
@@ -72,6 +73,21 @@ int check_shape(int B, int heads, int T, int H, int W, int head_dim, int s, int 
     if (row_elems >= (1ull << 31) || rows * row_elems >= (1ull << 40)) return SKIPARSE_ESHAPE;
     sh->n_tok = (size_t)n_tok;
     sh->n_sub = (size_t)n_sub;
+    sh->row_elems = (size_t)row_elems;
+    sh->elems = (size_t)(rows * row_elems);
+    return SKIPARSE_OK;
+}
+
+// The same where rows keep their places, and no index map bounds the grid.
+int check_rows(int B, int heads, int T, int H, int W, int head_dim, Shape* sh) {
+    if (B < 1 || heads < 1 || T < 1 || H < 1 || W < 1 || head_dim < 1) return SKIPARSE_EINVAL;
+    const uint64_t frame = (uint64_t)H * (uint64_t)W;
+    if (frame >= (1ull << 31)) return SKIPARSE_ESHAPE;
+    const uint64_t n_tok = frame * (uint64_t)T;
+    if (n_tok >= (1ull << 31)) return SKIPARSE_ESHAPE;
+    const uint64_t rows = n_tok * (uint64_t)B, row_elems = (uint64_t)heads * (uint64_t)head_dim;
+    if (rows >= (1ull << 31) || row_elems >= (1ull << 31) || rows * row_elems >= (1ull << 40)) return SKIPARSE_ESHAPE;
+    sh->n_tok = sh->n_sub = (size_t)n_tok;
     sh->row_elems = (size_t)row_elems;
     sh->elems = (size_t)(rows * row_elems);
     return SKIPARSE_OK;
@@ -522,6 +538,263 @@ int skiparse_attn_fwd_fp8(const void* q8, const void* k8, const void* v8, const 
                           void* out_bf16, int B, int heads, int T, int H, int W, int head_dim, int s, int pattern,
                           float scale, void* stream) {
     return skiparse_attn_fwd_fp8_ex(q8, k8, v8, sq, sk, sv, out_bf16, B, heads, T, H, W, head_dim, s, pattern, scale, 0u, stream);
+}
+
+// ---- rotary positions
+
+static bool valid_order(int order, bool stay) { return order >= SKIPARSE_ORDER_SAME && order <= (stay ? SKIPARSE_ORDER_STAY_SPARSE : SKIPARSE_ORDER_TO_ORIGINAL); }
+
+// Pairs of the table, 0 on bad arguments.  Places times pairs of an axis, and all pairs, stay below 2^31.
+static uint64_t rope_pairs(int T, int H, int W, int rt, int rh, int rw) {
+    if (T < 1 || H < 1 || W < 1) return 0;
+    uint64_t n = 0;
+    const int r[3] = {rt, rh, rw}, len[3] = {T, H, W};
+    for (int i = 0; i < 3; i++) {
+        if (r[i] < 0 || r[i] % 2 != 0 || (uint32_t)r[i] / 2u > ROPE_MAX_PAIRS) return 0;
+        n += (uint64_t)len[i] * (uint32_t)(r[i] / 2);
+    }
+    return n < (1ull << 31) ? n : 0;
+}
+
+size_t skiparse_rope_table_bytes(int T, int H, int W, int rt, int rh, int rw) { return (size_t)rope_pairs(T, H, W, rt, rh, rw) * 2 * sizeof(float); }
+
+int skiparse_rope_table(float* table, int T, int H, int W, int rt, int rh, int rw, float theta, int scaling, float factor_t, float factor_h, float factor_w,
+                        int trained_t, int trained_h, int trained_w, float fast, float slow, float attention, void* stream) {
+    if (!table || misaligned(table)) return SKIPARSE_EINVAL;
+    if (T < 1 || H < 1 || W < 1 || rt < 0 || rh < 0 || rw < 0 || (rt | rh | rw) % 2 != 0 || rt + rh + rw == 0) return SKIPARSE_EINVAL;
+    if (rt > 2 * (int)ROPE_MAX_PAIRS || rh > 2 * (int)ROPE_MAX_PAIRS || rw > 2 * (int)ROPE_MAX_PAIRS) return SKIPARSE_EUNSUPPORTED;
+    if (rope_pairs(T, H, W, rt, rh, rw) == 0) return SKIPARSE_ESHAPE;
+    if (scaling < SKIPARSE_ROPE_PLAIN || scaling > SKIPARSE_ROPE_YARN) return SKIPARSE_EINVAL;
+    const float limit = 3.0e38f;  // not finite, or not a number: refused
+    if (!(theta > 0.f && theta < limit) || !(attention > -limit && attention < limit)) return SKIPARSE_EINVAL;
+    const float factor[3] = {factor_t, factor_h, factor_w};
+    const int trained[3] = {trained_t, trained_h, trained_w}, r[3] = {rt, rh, rw}, len[3] = {T, H, W};
+    RopeAxis axis[3] = {};
+    for (int i = 0; i < 3; i++) {
+        axis[i].len = (uint32_t)len[i];
+        axis[i].r = (uint32_t)r[i];
+        axis[i].factor = factor[i];
+        axis[i].trained = (uint32_t)trained[i];
+        if (scaling == SKIPARSE_ROPE_PLAIN || r[i] == 0) continue;
+        if (!(factor[i] >= 1.f && factor[i] < limit)) return SKIPARSE_EINVAL;
+        if (scaling == SKIPARSE_ROPE_YARN && trained[i] < 1) return SKIPARSE_EINVAL;
+    }
+    if (scaling == SKIPARSE_ROPE_YARN && !(fast > slow && fast < limit && slow > -limit)) return SKIPARSE_EINVAL;
+    const RopeScaling sc = {scaling, theta, fast, slow, attention};
+    return finish(launch_rope_table(table, axis[0], axis[1], axis[2], sc, (hipStream_t)stream));
+}
+
+int skiparse_rope(const void* q, const void* k, void* q_out, void* k_out, const float* table, int B, int heads, int T, int H, int W, int head_dim, int rt, int rh,
+                  int rw, int len_t, int len_h, int len_w, int t0, int h0, int w0, int s, int pattern, int order, int layout, int inverse, int dtype, void* stream) {
+    if (!q || !q_out || !table || !k != !k_out) return SKIPARSE_EINVAL;
+    if (!valid_order(order, true)) return SKIPARSE_EINVAL;
+    if ((layout != SKIPARSE_ROPE_INTERLEAVED && layout != SKIPARSE_ROPE_HALF) || (inverse != 0 && inverse != 1)) return SKIPARSE_EINVAL;
+    const int esz = elem_size(dtype);
+    if (esz == 0) return SKIPARSE_EINVAL;
+    Shape sh;
+    const bool moved = order != SKIPARSE_ORDER_SAME && s != 1;
+    const int rc = moved ? check_shape(B, heads, T, H, W, head_dim, s, pattern, &sh) : check_rows(B, heads, T, H, W, head_dim, &sh);
+    if (rc != SKIPARSE_OK) return rc;
+    if (misaligned(q) || misaligned(q_out) || misaligned(table) || (k && (misaligned(k) || misaligned(k_out)))) return SKIPARSE_EINVAL;
+    if (dtype == SKIPARSE_FP8_E4M3 || head_dim % 8 != 0 || head_dim > 512) return SKIPARSE_EUNSUPPORTED;
+    if (rt < 0 || rh < 0 || rw < 0 || (rt | rh | rw) % 2 != 0 || rt > head_dim || rh > head_dim || rw > head_dim) return SKIPARSE_EINVAL;
+    if (rt + rh + rw == 0 || rt + rh + rw > head_dim) return SKIPARSE_EINVAL;
+    const uint64_t pairs = rope_pairs(len_t, len_h, len_w, rt, rh, rw);
+    if (pairs == 0) return SKIPARSE_EINVAL;
+    if (t0 < 0 || h0 < 0 || w0 < 0) return SKIPARSE_EINVAL;
+    if ((rt && (int64_t)t0 + T > len_t) || (rh && (int64_t)h0 + H > len_h) || (rw && (int64_t)w0 + W > len_w)) return SKIPARSE_ESHAPE;
+    const size_t bytes = sh.elems * (size_t)esz, table_bytes = (size_t)pairs * 8;
+    const bool in_place = !moved || order == SKIPARSE_ORDER_STAY_SPARSE;  // a row's place is read and written by one wavefront
+    if (overlap(q_out, q, bytes) && !(in_place && q_out == q)) return SKIPARSE_EINVAL;
+    if (overlap2(q_out, bytes, table, table_bytes)) return SKIPARSE_EINVAL;
+    if (k) {
+        if (overlap(k_out, k, bytes) && !(in_place && k_out == k)) return SKIPARSE_EINVAL;
+        if (overlap(q_out, k, bytes) || overlap(k_out, q, bytes) || overlap(q_out, k_out, bytes) || overlap2(k_out, bytes, table, table_bytes)) return SKIPARSE_EINVAL;
+    }
+    RopeArgs a;
+    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.table = table;
+    a.B = B; a.heads = heads; a.T = T; a.H = H; a.W = W; a.head_dim = head_dim;
+    a.rt = rt; a.rh = rh; a.rw = rw;
+    a.len_t = len_t; a.len_h = len_h;
+    a.t0 = t0; a.h0 = h0; a.w0 = w0;
+    a.order = moved ? order : SKIPARSE_ORDER_SAME;  // with s = 1 every layout is the original one
+    a.half = layout == SKIPARSE_ROPE_HALF;
+    a.inverse = inverse != 0;
+    a.f32 = dtype == SKIPARSE_FP32;
+    a.g = moved ? make_gridmap(T, H, W, s, pattern) : make_dense_gridmap(sh.n_tok);
+    return finish(launch_rope(a, (hipStream_t)stream));
+}
+
+// ---- 8-bit activation checkpoints
+
+static size_t checkpoint_scales(size_t rows, size_t cols) { return rows * ((cols + 31) / 32); }
+
+static int checkpoint_common(const void* x, const void* codes, const void* scales, int rows, int cols, int dtype) {
+    if (!x || !codes || !scales || rows < 1 || cols < 1) return SKIPARSE_EINVAL;
+    const int esz = elem_size(dtype);
+    if (esz == 0 || misaligned(x) || misaligned(codes)) return SKIPARSE_EINVAL;
+    if (dtype == SKIPARSE_FP8_E4M3 || cols % 8 != 0) return SKIPARSE_EUNSUPPORTED;
+    const size_t n = (size_t)rows * (size_t)cols, m = checkpoint_scales((size_t)rows, (size_t)cols);
+    if (n >= (1ull << 36)) return SKIPARSE_ESHAPE;
+    if (overlap2(x, n * esz, codes, n) || overlap2(x, n * esz, scales, m) || overlap2(codes, n, scales, m)) return SKIPARSE_EINVAL;
+    return SKIPARSE_OK;
+}
+
+int skiparse_checkpoint_save(const void* x, void* codes, void* scales, int rows, int cols, int dtype, void* stream) {
+    const int rc = checkpoint_common(x, codes, scales, rows, cols, dtype);
+    if (rc != SKIPARSE_OK) return rc;
+    return finish(launch_checkpoint_save(x, codes, scales, (uint32_t)rows, (uint32_t)cols, dtype == SKIPARSE_FP32, (hipStream_t)stream));
+}
+
+int skiparse_checkpoint_load(const void* codes, const void* scales, void* out, int rows, int cols, int dtype, void* stream) {
+    const int rc = checkpoint_common(out, codes, scales, rows, cols, dtype);
+    if (rc != SKIPARSE_OK) return rc;
+    return finish(launch_checkpoint_load(codes, scales, out, (uint32_t)rows, (uint32_t)cols, dtype == SKIPARSE_FP32, (hipStream_t)stream));
+}
+
+// ---- linear layer
+
+// Sizes, enums and the row map that both directions share; `moved`: rows change places.
+static int linear_common(int B, int T, int H, int W, int in_features, int out_features, int s, int pattern, int order, int act, int dtype, bool* moved, size_t* rows) {
+    if (!valid_order(order, false) || act < SKIPARSE_ACT_NONE || act > SKIPARSE_ACT_SILU || elem_size(dtype) == 0) return SKIPARSE_EINVAL;
+    *moved = order != SKIPARSE_ORDER_SAME && s != 1;
+    Shape sh;
+    for (int features : {in_features, out_features}) {
+        const int rc = *moved ? check_shape(B, 1, T, H, W, features, s, pattern, &sh) : check_rows(B, 1, T, H, W, features, &sh);
+        if (rc != SKIPARSE_OK) return rc;
+        if (features >= (1 << 23)) return SKIPARSE_ESHAPE;
+    }
+    if (dtype != SKIPARSE_BF16 || in_features % 8 != 0 || out_features % 8 != 0) return SKIPARSE_EUNSUPPORTED;
+    *rows = (size_t)B * sh.n_tok;
+    return SKIPARSE_OK;
+}
+
+struct Span {
+    const void* at;
+    size_t bytes;
+};
+// Whether the buffer `x`, which is written, shares a byte with one of the others; null spans are not there.
+static bool touches(Span x, std::initializer_list<Span> others) {
+    for (const Span& o : others)
+        if (x.at && o.at && overlap2(x.at, x.bytes, o.at, o.bytes)) return true;
+    return false;
+}
+
+size_t skiparse_linear_workspace_bytes(int rows, int in_features, int out_features) {
+    (void)rows; (void)in_features; (void)out_features;
+    return 0;
+}
+
+int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, void* out, void* pre, void* pre_scales, int B, int T, int H, int W,
+                        int in_features, int out_features, int s, int pattern, int order, int act, int dtype, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+    (void)workspace; (void)workspace_bytes;
+    if (!x || !w || !out || (pre_scales && !pre)) return SKIPARSE_EINVAL;
+    bool moved;
+    size_t rows;
+    const int rc = linear_common(B, T, H, W, in_features, out_features, s, pattern, order, act, dtype, &moved, &rows);
+    if (rc != SKIPARSE_OK) return rc;
+    for (const void* p : {x, w, bias, residual, (const void*)out, (const void*)pre})
+        if (p && misaligned(p)) return SKIPARSE_EINVAL;
+    const size_t K = (size_t)in_features, N = (size_t)out_features;
+    if (moved && rows * K * 2 >= (1ull << 32) - 64) return SKIPARSE_ESHAPE;  // rows that move are addressed with 32-bit byte offsets
+    const Span sx = {x, rows * K * 2}, sw = {w, N * K * 2}, sb = {bias, N * 2}, so = {out, rows * N * 2};
+    const Span sp = {pre, rows * N * (pre_scales ? 1 : 2)}, ss = {pre_scales, checkpoint_scales(rows, N)}, sr = {residual, rows * N * 2};
+    if (touches(so, {sx, sw, sb, sp, ss}) || (residual && residual != out && overlap2(out, so.bytes, residual, sr.bytes))) return SKIPARSE_EINVAL;
+    if (touches(sp, {sx, sw, sb, ss, sr}) || touches(ss, {sx, sw, sb, sr})) return SKIPARSE_EINVAL;
+    LinearArgs a = {};
+    a.p = x; a.q = w;
+    a.M = (uint32_t)rows; a.N = (uint32_t)N; a.K = (uint32_t)K;
+    a.e = {bias, residual, out, pre, pre_scales, act};
+    a.order = moved ? order : SKIPARSE_ORDER_SAME;
+    if (moved) {
+        const GridMap g = make_gridmap(T, H, W, s, pattern);
+        a.rows = order == SKIPARSE_ORDER_TO_SPARSE ? make_row_args<TO_SPARSE>(g, (uint32_t)B) : make_row_args<TO_ORIGINAL>(g, (uint32_t)B);
+    }
+    return finish(launch_linear(LINEAR_FWD, a, (hipStream_t)stream));
+}
+
+// What a backward call keeps in its workspace, one after the other.
+struct LinearBwdSpace {
+    size_t dz, x, db, total;
+};
+static LinearBwdSpace linear_bwd_space(size_t rows, size_t K, size_t N, bool dz, bool x, bool db) {
+    LinearBwdSpace l;
+    l.dz = dz ? align256(rows * N * 2) : 0;
+    l.x = x ? align256(rows * K * 2) : 0;
+    l.db = db ? align256((size_t)linear_rows_parts((uint32_t)rows) * N * sizeof(float)) : 0;
+    l.total = l.dz + l.x + l.db;
+    return l;
+}
+
+size_t skiparse_linear_bwd_workspace_bytes(int rows, int in_features, int out_features, int order, int act, int x_checkpoint) {
+    if (rows < 1 || in_features < 1 || out_features < 1 || !valid_order(order, false) || act < SKIPARSE_ACT_NONE || act > SKIPARSE_ACT_SILU) return 0;
+    return linear_bwd_space((size_t)rows, (size_t)in_features, (size_t)out_features, order != SKIPARSE_ORDER_SAME || act != SKIPARSE_ACT_NONE, x_checkpoint != 0, true).total;
+}
+
+int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, const void* w, const void* pre, const void* pre_scales, const void* dx_add, void* dx,
+                        void* dw, void* db, int B, int T, int H, int W, int in_features, int out_features, int s, int pattern, int order, int act, int dtype,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    if (!dy || (!dx && !dw && !db) || (dx && !w) || (dw && !x) || (x_scales && !x) || (pre_scales && !pre) || (dx_add && !dx)) return SKIPARSE_EINVAL;
+    bool moved;
+    size_t rows;
+    const int rc = linear_common(B, T, H, W, in_features, out_features, s, pattern, order, act, dtype, &moved, &rows);
+    if (rc != SKIPARSE_OK) return rc;
+    if (act != SKIPARSE_ACT_NONE && !pre) return SKIPARSE_EINVAL;
+    for (const void* p : {dy, x, w, pre, dx_add, (const void*)dx, (const void*)dw, (const void*)db})
+        if (p && misaligned(p)) return SKIPARSE_EINVAL;
+    if (act == SKIPARSE_ACT_NONE) pre = pre_scales = nullptr;
+    if (!dw) x = x_scales = nullptr;
+    if (!dx) w = nullptr;
+    const size_t K = (size_t)in_features, N = (size_t)out_features;
+    const LinearBwdSpace l = linear_bwd_space(rows, K, N, (dx || dw) && (moved || act != SKIPARSE_ACT_NONE), x_scales != nullptr, db != nullptr);
+    if (l.total && (!workspace || workspace_bytes < l.total || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
+    const Span sy = {dy, rows * N * 2}, sx = {x, rows * K * (x_scales ? 1 : 2)}, sxs = {x_scales, checkpoint_scales(rows, K)}, sw = {w, N * K * 2};
+    const Span sp = {pre, rows * N * (pre_scales ? 1 : 2)}, sps = {pre_scales, checkpoint_scales(rows, N)}, sa = {dx_add, rows * K * 2};
+    const Span gx = {dx, rows * K * 2}, gw = {dw, N * K * 2}, gb = {db, N * 2}, ws = {l.total ? workspace : nullptr, l.total};
+    if (touches(gx, {sy, sx, sxs, sw, sp, sps, gw, gb, ws}) || (dx_add && dx_add != dx && overlap(dx, dx_add, gx.bytes))) return SKIPARSE_EINVAL;
+    if (touches(gw, {sy, sx, sxs, sw, sp, sps, sa, gb, ws}) || touches(gb, {sy, sx, sxs, sw, sp, sps, sa, ws})) return SKIPARSE_EINVAL;
+    if (touches(ws, {sy, sx, sxs, sw, sp, sps, sa})) return SKIPARSE_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    char* const at = (char*)workspace;
+    hipError_t e;
+    const void* dz = dy;
+    if (l.dz || db) {
+        LinearRowsArgs r = {};
+        r.dy = dy; r.pre = pre; r.pre_scales = pre_scales;
+        r.dz = l.dz ? at : nullptr;
+        r.db_part = db ? (float*)(at + l.dz + l.x) : nullptr;
+        r.db = db;
+        r.M = (uint32_t)rows; r.N = (uint32_t)N;
+        r.act = act;
+        if (moved) {  // row of the input -> row of the output that was made of it
+            const GridMap g = make_gridmap(T, H, W, s, pattern);
+            const bool back = order == SKIPARSE_ORDER_TO_SPARSE;
+            r.order = back ? SKIPARSE_ORDER_TO_ORIGINAL : SKIPARSE_ORDER_TO_SPARSE;
+            r.rows = back ? make_row_args<TO_ORIGINAL>(g, (uint32_t)B) : make_row_args<TO_SPARSE>(g, (uint32_t)B);
+        }
+        if ((e = launch_linear_rows(r, st)) != hipSuccess) return finish(e);
+        if (l.dz) dz = at;
+    }
+    if (x_scales) {
+        if ((e = launch_checkpoint_load(x, x_scales, at + l.dz, (uint32_t)rows, (uint32_t)K, false, st)) != hipSuccess) return finish(e);
+        x = at + l.dz;
+    }
+    if (dx) {
+        LinearArgs a = {};
+        a.p = dz; a.q = w;
+        a.M = (uint32_t)rows; a.N = (uint32_t)K; a.K = (uint32_t)N;
+        a.e = {nullptr, dx_add, dx, nullptr, nullptr, ACT_NONE};
+        if ((e = launch_linear(LINEAR_DX, a, st)) != hipSuccess) return finish(e);
+    }
+    if (dw) {
+        LinearArgs a = {};
+        a.p = dz; a.q = x;
+        a.M = (uint32_t)N; a.N = (uint32_t)K; a.K = (uint32_t)rows;
+        a.e = {nullptr, nullptr, dw, nullptr, nullptr, ACT_NONE};
+        if ((e = launch_linear(LINEAR_DW, a, st)) != hipSuccess) return finish(e);
+    }
+    return SKIPARSE_OK;
 }
 
 const char* skiparse_strerror(int code) {

@@ -1,0 +1,167 @@
+// 8-bit activation checkpoints (format: checkpoint.h): what a training step keeps of a bf16 or float32 tensor until its backward pass, in 33 / 64 of the
+// bytes of bf16.  Bound by HBM bandwidth.  A lane has 8 channels, four lanes a block, whose maximum takes two exchanges between neighbours.
+#include "checkpoint.h"
+#include "kernels.h"
+
+namespace skiparse {
+
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+
+constexpr int CKPT_THREADS = 256;
+constexpr int CKPT_UNROLL = 4;  // 8-channel pieces a lane
+
+struct CkptArgs {
+    uint64_t pieces;   // 8-channel places of all rows, those behind the end of a short last block included
+    Div32 per_row;     // of a row: 4 * blocks
+    uint32_t cols;
+};
+
+// Where piece i lies: element offset and block; false: behind the row's end.  !RAGGED: rows are whole blocks, so that the tensor is one run of them.
+template <bool RAGGED>
+__device__ inline bool piece_at(const CkptArgs& a, uint64_t i, uint64_t& elem, uint64_t& block) {
+    block = i >> 2;
+    elem = i * 8u;
+    if (!RAGGED) return true;
+    const uint64_t row = i / a.per_row.d;
+    const uint32_t c = (uint32_t)(i - row * a.per_row.d) * 8u;
+    elem = row * a.cols + c;
+    return c < a.cols;
+}
+
+template <typename T>
+__device__ inline void load8(const T* p, float (&v)[8]);
+template <>
+__device__ inline void load8<__bf16>(const __bf16* p, float (&v)[8]) {
+    const u32x4 x = *(const u32x4*)p;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        v[2 * e] = __uint_as_float(x[e] << 16);
+        v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+    }
+}
+template <>
+__device__ inline void load8<float>(const float* p, float (&v)[8]) {
+    const u32x4 x = *(const u32x4*)p, y = *(const u32x4*)(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        v[e] = __uint_as_float(x[e]);
+        v[4 + e] = __uint_as_float(y[e]);
+    }
+}
+__device__ inline void store8(__bf16* p, const float (&v)[8]) {
+    typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+    bf16x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; e++) y[e] = (__bf16)v[e];
+    *(bf16x8*)p = y;
+}
+__device__ inline void store8(float* p, const float (&v)[8]) {
+    typedef __attribute__((ext_vector_type(4))) float f32x4;
+    *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+
+template <typename T, bool RAGGED>
+__global__ __launch_bounds__(CKPT_THREADS) void checkpoint_save_kernel(const T* __restrict__ x, unsigned char* __restrict__ codes, unsigned char* __restrict__ scales, CkptArgs a) {
+    const uint64_t first = (uint64_t)blockIdx.x * (CKPT_THREADS * CKPT_UNROLL) + threadIdx.x;
+    float v[CKPT_UNROLL][8];
+    uint64_t elem[CKPT_UNROLL], block[CKPT_UNROLL];
+    bool real[CKPT_UNROLL];
+#pragma unroll
+    for (int u = 0; u < CKPT_UNROLL; u++) {
+        const uint64_t i = first + u * CKPT_THREADS;
+        real[u] = i < a.pieces && piece_at<RAGGED>(a, i, elem[u], block[u]);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[u][e] = 0.f;
+        if (real[u]) load8(x + elem[u], v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < CKPT_UNROLL; u++) {
+        uint32_t m = 0u;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const uint32_t s = ckpt_size(v[u][e]);
+            m = s > m ? s : m;
+        }
+#pragma unroll
+        for (int off = 1; off <= 2; off <<= 1) {  // a block's four lanes are neighbours: pieces of a row come in fours
+            const uint32_t o = (uint32_t)__shfl_xor((int)m, off);
+            m = o > m ? o : m;
+        }
+        const uint32_t byte = ckpt_byte(m);
+        const float down = ckpt_down(byte);
+        if (real[u]) {
+            *(u32x2*)(codes + elem[u]) = u32x2{ckpt_codes(v[u][0], v[u][1], v[u][2], v[u][3], down), ckpt_codes(v[u][4], v[u][5], v[u][6], v[u][7], down)};
+            if ((threadIdx.x & 3u) == 0u) scales[block[u]] = (unsigned char)byte;
+        }
+    }
+}
+
+template <typename T, bool RAGGED>
+__global__ __launch_bounds__(CKPT_THREADS) void checkpoint_load_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales, T* __restrict__ out, CkptArgs a) {
+    const uint64_t first = (uint64_t)blockIdx.x * (CKPT_THREADS * CKPT_UNROLL) + threadIdx.x;
+    u32x2 c[CKPT_UNROLL];
+    uint32_t byte[CKPT_UNROLL];
+    uint64_t elem[CKPT_UNROLL], block;
+    bool real[CKPT_UNROLL];
+#pragma unroll
+    for (int u = 0; u < CKPT_UNROLL; u++) {
+        const uint64_t i = first + u * CKPT_THREADS;
+        real[u] = i < a.pieces && piece_at<RAGGED>(a, i, elem[u], block);
+        if (real[u]) {
+            c[u] = *(const u32x2*)(codes + elem[u]);
+            byte[u] = scales[block];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < CKPT_UNROLL; u++) {
+        if (!real[u]) continue;
+        const float up = ckpt_up(byte[u]);
+        float lo[4], hi[4];
+        ckpt_values(c[u][0], up, lo);
+        ckpt_values(c[u][1], up, hi);
+        const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        store8(out + elem[u], v);
+    }
+}
+
+static CkptArgs make_args(uint32_t rows, uint32_t cols) {
+    const uint32_t blocks = (cols + CKPT_BLOCK - 1u) / CKPT_BLOCK;
+    return {(uint64_t)rows * blocks * 4u, make_div32(blocks * 4u), cols};
+}
+
+template <typename T>
+static hipError_t save_t(const void* x, void* codes, void* scales, const CkptArgs& a, uint32_t blocks, hipStream_t stream) {
+    if (a.cols % CKPT_BLOCK) checkpoint_save_kernel<T, true><<<blocks, CKPT_THREADS, 0, stream>>>((const T*)x, (unsigned char*)codes, (unsigned char*)scales, a);
+    else checkpoint_save_kernel<T, false><<<blocks, CKPT_THREADS, 0, stream>>>((const T*)x, (unsigned char*)codes, (unsigned char*)scales, a);
+    return hipGetLastError();
+}
+template <typename T>
+static hipError_t load_t(const void* codes, const void* scales, void* out, const CkptArgs& a, uint32_t blocks, hipStream_t stream) {
+    if (a.cols % CKPT_BLOCK) checkpoint_load_kernel<T, true><<<blocks, CKPT_THREADS, 0, stream>>>((const unsigned char*)codes, (const unsigned char*)scales, (T*)out, a);
+    else checkpoint_load_kernel<T, false><<<blocks, CKPT_THREADS, 0, stream>>>((const unsigned char*)codes, (const unsigned char*)scales, (T*)out, a);
+    return hipGetLastError();
+}
+
+static bool ckpt_grid(const CkptArgs& a, uint32_t* blocks) {
+    const uint64_t n = (a.pieces + CKPT_THREADS * CKPT_UNROLL - 1) / (CKPT_THREADS * CKPT_UNROLL);
+    *blocks = (uint32_t)n;
+    return fits_grid(n, CKPT_THREADS);
+}
+
+hipError_t launch_checkpoint_save(const void* x, void* codes, void* scales, uint32_t rows, uint32_t cols, bool f32, hipStream_t stream) {
+    const CkptArgs a = make_args(rows, cols);
+    uint32_t blocks;
+    if (!ckpt_grid(a, &blocks)) return hipErrorInvalidConfiguration;
+    return f32 ? save_t<float>(x, codes, scales, a, blocks, stream) : save_t<__bf16>(x, codes, scales, a, blocks, stream);
+}
+
+hipError_t launch_checkpoint_load(const void* codes, const void* scales, void* out, uint32_t rows, uint32_t cols, bool f32, hipStream_t stream) {
+    const CkptArgs a = make_args(rows, cols);
+    uint32_t blocks;
+    if (!ckpt_grid(a, &blocks)) return hipErrorInvalidConfiguration;
+    return f32 ? load_t<float>(codes, scales, out, a, blocks, stream) : load_t<__bf16>(codes, scales, out, a, blocks, stream);
+}
+
+}  // namespace skiparse

@@ -154,4 +154,78 @@ struct Fp8AttnArgs {
 };
 hipError_t launch_attn_fp8(const Fp8AttnArgs& a, hipStream_t stream);
 
+// 8-bit activation checkpoints of [rows][cols] (format: checkpoint.h).  f32: the tensor is float32, else bf16.
+hipError_t launch_checkpoint_save(const void* x, void* codes, void* scales, uint32_t rows, uint32_t cols, bool f32, hipStream_t stream);
+hipError_t launch_checkpoint_load(const void* codes, const void* scales, void* out, uint32_t rows, uint32_t cols, bool f32, hipStream_t stream);
+
+// Rotary positions on the token grid.
+struct RopeArgs {
+    const void* q;
+    const void* k;        // or null
+    void* q_out;
+    void* k_out;
+    const float* table;   // [len_t][rt / 2], [len_h][rh / 2], [len_w][rw / 2] pairs (cos, sin)
+    int B, heads, T, H, W, head_dim;
+    int rt, rh, rw;       // channels of a head that turn with t, h, w
+    int len_t, len_h;     // places of the table's axes
+    int t0, h0, w0;       // the grid's first place on each
+    int order;            // SKIPARSE_ORDER_*
+    bool half, inverse, f32;
+    GridMap g;
+};
+hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
+
+constexpr uint32_t ROPE_MAX_PAIRS = 256;
+enum RopeScale : int { ROPE_PLAIN = 0, ROPE_LINEAR = 1, ROPE_NTK = 2, ROPE_YARN = 3 };
+struct RopeAxis {
+    uint32_t len, r;      // places, channels
+    float factor;
+    uint32_t trained;     // places that the model was trained on
+    uint32_t first, blocks;  // set by the launcher: first entry, workgroups
+    Div32 pairs;
+};
+struct RopeScaling {
+    int kind;
+    float theta, fast, slow, attention;
+};
+hipError_t launch_rope_table(float* table, RopeAxis t, RopeAxis h, RopeAxis w, const RopeScaling& s, hipStream_t stream);
+
+// Products of the linear layer.  C[m][n] = sum_k P(m, k) Q(n, k), P given as [m][k] or, transposed, as [k][m], Q likewise.
+enum LinearForm : int { LINEAR_FWD = 0, LINEAR_DX = 1, LINEAR_DW = 2 };  // neither, Q, both transposed
+enum LinearAct : int { ACT_NONE = 0, ACT_GELU_TANH = 1, ACT_SILU = 2 };
+// What happens to C on the way out: z = C + bias, kept in pre; out = act(z) + residual.
+struct LinearEpilogue {
+    const void* bias;      // bf16 [n] or null
+    const void* residual;  // bf16 [m][n] or null; may be out
+    void* out;             // bf16 [m][n]
+    void* pre;             // null; bf16 [m][n]; or, with pre_scales, the codes of a checkpoint
+    void* pre_scales;
+    int act;
+};
+struct LinearArgs {
+    const void* p;
+    const void* q;
+    uint32_t M, N, K;
+    LinearEpilogue e;
+    int order;     // ORDER_SAME, or the row map from which row m of C takes its row of P (LINEAR_FWD only)
+    RowArgs rows;
+};
+hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream);
+
+// The passes over rows in front of a backward's products.
+struct LinearRowsArgs {
+    const void* dy;          // bf16 [rows][N], rows in the output's order
+    const void* pre;         // null: no activation; bf16, or codes with pre_scales
+    const void* pre_scales;
+    void* dz;                // bf16 [rows][N] in the input's order, or null
+    float* db_part;          // [linear_rows_parts()][N], or null
+    void* db;                // bf16 [N]
+    uint32_t M, N;
+    int act;
+    int order;               // from the output's order back to the input's
+    RowArgs rows;
+};
+uint32_t linear_rows_parts(uint32_t M);
+hipError_t launch_linear_rows(const LinearRowsArgs& a, hipStream_t stream);
+
 }  // namespace skiparse

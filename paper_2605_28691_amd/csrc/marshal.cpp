@@ -74,15 +74,15 @@ struct Arg<P*> {
     }
 };
 
-// Argument I of N: the last one is the stream's handle; argument NONE may be None.
-template <size_t I, size_t N, size_t NONE, typename T>
+// Argument I of N: the last one is the stream's handle; the arguments in the set NONE, a bit each, may be None.
+template <size_t I, size_t N, unsigned NONE, typename T>
 bool get_arg(PyObject* o, T& v) {
     if constexpr (I + 1 == N) {
         if (!PyLong_CheckExact(o)) return false;
         v = (T)(uintptr_t)PyLong_AsUnsignedLongLongMask(o);
         return true;
     } else {
-        if constexpr (I == NONE) {
+        if constexpr (NONE >> I & 1u) {
             if (o == Py_None) {
                 v = nullptr;
                 return true;
@@ -119,7 +119,7 @@ PyObject* general(const char* name, PyObject* const* args, Py_ssize_t n) {
     return r;
 }
 
-template <size_t NONE, typename... A, size_t... I>
+template <unsigned NONE, typename... A, size_t... I>
 PyObject* call_with(int (*fn)(A...), const char* name, PyObject* const* args, Py_ssize_t n, std::index_sequence<I...>) {
     std::tuple<A...> v;
     bool plain = n == (Py_ssize_t)sizeof...(A) && g_general != nullptr && g_failed != nullptr;
@@ -137,15 +137,18 @@ PyObject* call_with(int (*fn)(A...), const char* name, PyObject* const* args, Py
     return PyObject_CallFunction(g_failed, "is", code, name);
 }
 
-template <size_t NONE, typename... A>
+template <unsigned NONE, typename... A>
 PyObject* call(int (*fn)(A...), const char* name, PyObject* const* args, Py_ssize_t n) {
     return call_with<NONE>(fn, name, args, n, std::index_sequence_for<A...>{});
 }
 
-constexpr size_t NEVER = ~(size_t)0;
+constexpr unsigned NEVER = 0u;
+constexpr unsigned at() { return 0u; }
+template <typename... I>
+constexpr unsigned at(int i, I... more) { return 1u << i | at(more...); }
 // address of the C function: none until the binding has opened the library, and the general way is taken (which opens it)
 #define SLOT(name, none) decltype(&::name) g_##name = nullptr;
-// argument that may be None: the workspace of the forward layer, which the fused form does not need
+// `none`: arguments that may be None, as the workspace of the forward layer, which the fused form does not need
 #define ENTRY(name, none)                                                 \
     PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) { \
         return g_##name ? call<none>(g_##name, #name, args, n) : general(#name, args, n); \
@@ -154,7 +157,7 @@ constexpr size_t NEVER = ~(size_t)0;
     if (strcmp(what, #name) == 0) g_##name = (decltype(g_##name))address;
 #define LISTED(name, none) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr},
 #define ENTRIES(X) \
-    X(skiparse_attn_fwd, 15) \
+    X(skiparse_attn_fwd, at(15)) \
     X(skiparse_permute, NEVER) \
     X(skiparse_unpermute, NEVER) \
     X(skiparse_switch_pattern, NEVER) \
@@ -166,7 +169,13 @@ constexpr size_t NEVER = ~(size_t)0;
     X(skiparse_attn_bwd, NEVER) \
     X(skiparse_attn_bwd_static, NEVER) \
     X(skiparse_quantize_fp8_ex, NEVER) \
-    X(skiparse_attn_fwd_fp8_ex, NEVER)
+    X(skiparse_attn_fwd_fp8_ex, NEVER) \
+    X(skiparse_rope_table, NEVER) \
+    X(skiparse_rope, at(1, 3)) \
+    X(skiparse_checkpoint_save, NEVER) \
+    X(skiparse_checkpoint_load, NEVER) \
+    X(skiparse_linear_fwd, at(2, 3, 5, 6, 18)) \
+    X(skiparse_linear_bwd, at(1, 2, 3, 4, 5, 6, 7, 8, 9, 21))
 ENTRIES(SLOT)
 ENTRIES(ENTRY)
 
