@@ -8,6 +8,8 @@
 //     128 bytes and read 16 bytes at a time; transposed ones in rows of 256 and read with ds_read_b64_tr_b16; swizzles as in lds_layout.h.
 //   * Ends: a 16-byte piece behind the end of k is given an offset outside the buffer and reads as zero; transposed operands end with the buffer; rows
 //     past the last read the last one, columns past the last whatever lies there, and neither is stored.
+#include <type_traits>
+
 #include "checkpoint.h"
 #include "kernels.h"
 #include "lds_layout.h"
@@ -50,12 +52,10 @@ struct Side {
             }
         }
     }
-    __device__ __attribute__((always_inline)) inline void issue(const char* base, uint32_t records, uint32_t k_left, char* buf, uint32_t wave) const {
+    __device__ __attribute__((always_inline)) inline void issue(int i, const char* base, uint32_t records, uint32_t k_left, char* buf, uint32_t wave) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass does not know the buffer's type, and would drop the kernel without a word
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, records, 0x27000);
-#pragma unroll
-        for (int i = 0; i < INSTR; i++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LDS_PTR(void))(buf + (wave * INSTR + i) * 1024u), 16, T || kofs[i] < k_left ? off[i] : LIN_OUTSIDE, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LDS_PTR(void))(buf + (wave * INSTR + i) * 1024u), 16, T || kofs[i] < k_left ? off[i] : LIN_OUTSIDE, 0, 0, 0);
 #endif
     }
 };
@@ -81,27 +81,138 @@ __device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char
     return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Row m of C, channels n .. n + 3 of a block of 32: z = acc + bias; the result's value, without the residual.
-__device__ __attribute__((always_inline)) inline f32x4 with_bias(const LinearEpilogue& e, f32x4 z, uint32_t n) {
-    if (e.bias != nullptr) {
-        const bf16x4 b = *(const bf16x4*)((const __bf16*)e.bias + n);
-#pragma unroll
-        for (int i = 0; i < 4; i++) z[i] += (float)b[i];
+// Workgroup -> tile.  Workgroup id % 8 is the XCD; each XCD has a contiguous range of an order in which TILE_GROUP tiles of m are walked together along n, so that the 32
+// tiles that it works on at once share operands in its L2.
+constexpr uint32_t TILE_GROUP = 8;
+struct TileMap {
+    Div32 group;   // tiles of a group: TILE_GROUP * tiles_n
+    Div32 size, last;  // tiles of m in a group, in the last one
+    uint32_t tiles_m, total, per_xcd;
+    __device__ inline void at(uint32_t id, uint32_t& tm, uint32_t& tn) const {
+        const uint32_t xcd = id & 7u, rest = total & 7u;  // the first `rest` XCDs have one tile more
+        const uint32_t lin = xcd * per_xcd + (xcd < rest ? xcd : rest) + (id >> 3);
+        const uint32_t g = group.div(lin), in = lin - g * group.d, first = g * TILE_GROUP;
+        const bool full = first + TILE_GROUP <= tiles_m;
+        const uint32_t n = full ? size.div(in) : last.div(in);
+        tn = n;
+        tm = first + in - n * (full ? size.d : last.d);
     }
-    return z;
+};
+static TileMap make_tile_map(uint32_t tiles_m, uint32_t tiles_n) {
+    const uint32_t rest = tiles_m % TILE_GROUP;
+    return {make_div32(TILE_GROUP * tiles_n), make_div32(TILE_GROUP), make_div32(rest ? rest : 1u), tiles_m, tiles_m * tiles_n, tiles_m * tiles_n / 8u};
 }
 
+// The way out: 32 rows by 32 FN channels of C at a time, a wavefront's own.  The sums are laid down in LDS as they are (float32: a residual is added before the one
+// rounding) and picked up 8 channels of a row a lane, so that everything in memory is moved in 16-byte pieces of whole rows, and a checkpoint's blocks are four
+// neighbouring lanes.
+template <int FN>
+struct Out {
+    static constexpr uint32_t LPR = FN * 4, RPI = 64 / LPR;  // lanes a row, rows at once
+    uint32_t n;      // the lane's channels n .. n + 7
+    bool in;
+    float bias[8];
+    __device__ __attribute__((always_inline)) inline Out(const LinearArgs& a, uint32_t n0, uint32_t lane) {
+        n = n0 + lane % LPR * 8u;
+        in = n < a.N;
+#pragma unroll
+        for (int e = 0; e < 8; e++) bias[e] = 0.f;
+        if (a.e.bias != nullptr && in) {
+            const bf16x8 b = *(const bf16x8*)((const __bf16*)a.e.bias + n);
+#pragma unroll
+            for (int e = 0; e < 8; e++) bias[e] = (float)b[e];
+        }
+    }
+    // 16-byte piece c of row r lies at c ^ (r % 16): 8 lanes that write (8 rows) or read (a row) touch different banks
+    __device__ __attribute__((always_inline)) inline static uint32_t place(uint32_t r, uint32_t c) { return r * (FN * 128u) + ((c ^ (r & (FN == 4 ? 15u : 7u))) * 16u); }
+    __device__ __attribute__((always_inline)) inline void lay_down(char* stage, const f32x16 (&acc)[FN], uint32_t lane) const {
+        const uint32_t r = lane & 31u, h = lane >> 5;
+        // the wavefront's LDS accesses take effect in order; the fences keep the compiler from exchanging them
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < FN; j++)
+#pragma unroll
+            for (int g = 0; g < 4; g++)
+                *(f32x4*)(stage + place(r, j * 8u + g * 2u + h)) = f32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    __device__ __attribute__((always_inline)) inline void rows(const char* stage, const LinearArgs& a, uint32_t m0, uint32_t lane) const {
+#pragma unroll
+        for (uint32_t it = 0; it < 32u / RPI; it++) {
+            const uint32_t r = it * RPI + lane / LPR, c = lane % LPR * 2u;
+            const f32x4 x = *(const f32x4*)(stage + place(r, c)), y = *(const f32x4*)(stage + place(r, c + 1u));
+            const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            finish(a, m0 + r, z);
+        }
+    }
+    // row m, the lane's channels: act(z + bias) + residual; z + bias kept
+    __device__ __attribute__((always_inline)) inline void finish(const LinearArgs& a, uint32_t m, const float (&sum)[8]) const {
+        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+        const LinearEpilogue& e = a.e;
+        const bool here = in && m < a.M;
+        const size_t at = (size_t)m * a.N + n;
+        float z[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) z[i] = sum[i] + bias[i];
+        if (e.pre_scales != nullptr) {
+            uint32_t top = 0u;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t s = in ? ckpt_size(z[i]) : 0u;
+                top = s > top ? s : top;
+            }
+#pragma unroll
+            for (int off = 1; off <= 2; off <<= 1) {
+                const uint32_t o = (uint32_t)__shfl_xor((int)top, off);
+                top = o > top ? o : top;
+            }
+            const uint32_t byte = ckpt_byte(top);
+            const float down = ckpt_down(byte);
+            if (here) {
+                *(u32x2*)((char*)e.pre + at) = u32x2{ckpt_codes(z[0], z[1], z[2], z[3], down), ckpt_codes(z[4], z[5], z[6], z[7], down)};
+                if (n % CKPT_BLOCK == 0u) ((unsigned char*)e.pre_scales)[(size_t)m * ((a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK) + n / CKPT_BLOCK] = (unsigned char)byte;
+            }
+        }
+        if (!here) return;
+        if (e.pre != nullptr && e.pre_scales == nullptr) {
+            bf16x8 o;
+#pragma unroll
+            for (int i = 0; i < 8; i++) o[i] = (__bf16)z[i];
+            *(bf16x8*)((__bf16*)e.pre + at) = o;
+        }
+        if (e.act != ACT_NONE) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) z[i] = act_value(e.act, z[i]);
+        }
+        if (e.residual != nullptr) {
+            const bf16x8 r = *(const bf16x8*)((const __bf16*)e.residual + at);
+#pragma unroll
+            for (int i = 0; i < 8; i++) z[i] += (float)r[i];
+        }
+        bf16x8 o;
+#pragma unroll
+        for (int i = 0; i < 8; i++) o[i] = (__bf16)z[i];
+        *(bf16x8*)((__bf16*)e.out + at) = o;
+    }
+};
+
 template <int BM, int BN, int FORM>
-__global__ __launch_bounds__(256) void linear_kernel(LinearArgs a, uint32_t tiles_n) {
+__global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kernel(LinearArgs a, TileMap tiles) {
     constexpr bool PT = FORM == LINEAR_DW, QT = FORM != LINEAR_FWD;
     constexpr int NW = 4, FM = BM / 64, FN = BN / 64;  // wavefronts 2 x 2; blocks of 32 that each has
     using SP = Side<BM, PT, NW>;
     using SQ = Side<BN, QT, NW>;
-    __shared__ __attribute__((aligned(1024))) char pbuf[2][SP::BYTES];
-    __shared__ __attribute__((aligned(1024))) char qbuf[2][SQ::BYTES];
+    // separate arrays: the compiler must be able to tell that the tile being filled is not the tile being read
+    __shared__ __attribute__((aligned(1024))) char pbuf0[SP::BYTES];
+    __shared__ __attribute__((aligned(1024))) char pbuf1[SP::BYTES];
+    __shared__ __attribute__((aligned(1024))) char qbuf0[SQ::BYTES];
+    __shared__ __attribute__((aligned(1024))) char qbuf1[SQ::BYTES];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave & 1u, wn = wave >> 1;
-    const uint32_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
+    uint32_t tm, tn;
+    tiles.at(blockIdx.x, tm, tn);
     const uint32_t m0 = tm * BM, n0 = tn * BN;
     const uint32_t ldp = (PT ? a.M : a.K) * 2u, ldq = (QT ? a.N : a.K) * 2u;  // bytes
     const bool mapped = FORM == LINEAR_FWD && a.order != 0;
@@ -119,14 +230,24 @@ __global__ __launch_bounds__(256) void linear_kernel(LinearArgs a, uint32_t tile
     });
     const char* const p0 = (const char*)a.p + (PT ? (size_t)m0 * 2u : mapped ? 0 : (size_t)m0 * ldp);
     const char* const q0 = (const char*)a.q + (QT ? (size_t)n0 * 2u : (size_t)n0 * ldq);
+    // bytes of a buffer that begins with row k: what a transposed operand still has; 0 behind the end
     auto records = [&](bool t, uint32_t k, uint32_t ld, uint32_t col0) __attribute__((always_inline)) -> uint32_t {
+        if (k >= a.K) return 0u;
         if (!t) return LIN_RECORDS;
         const uint64_t left = (uint64_t)(a.K - k) * ld - col0 * 2u;
         return left < LIN_RECORDS ? (uint32_t)left : LIN_RECORDS;
     };
-    auto issue = [&](uint32_t k, int b) __attribute__((always_inline)) {
-        sp.issue(p0 + (PT ? (size_t)k * ldp : (size_t)k * 2u), records(PT, k, ldp, m0), a.K - k, pbuf[b], wave);
-        sq.issue(q0 + (QT ? (size_t)k * ldq : (size_t)k * 2u), records(QT, k, ldq, n0), a.K - k, qbuf[b], wave);
+    constexpr int LOADS = SP::INSTR + SQ::INSTR;
+    struct Step {
+        const char *p, *q;
+        uint32_t rp, rq, left;
+    };
+    auto step_at = [&](uint32_t k) __attribute__((always_inline)) -> Step {
+        return {p0 + (PT ? (size_t)k * ldp : (size_t)k * 2u), q0 + (QT ? (size_t)k * ldq : (size_t)k * 2u), records(PT, k, ldp, m0), records(QT, k, ldq, n0), k < a.K ? a.K - k : 0u};
+    };
+    auto load = [&](const Step& s, char* pb, char* qb, int i) __attribute__((always_inline)) {
+        if (i < SP::INSTR) sp.issue(i, s.p, s.rp, s.left, pb, wave);
+        else sq.issue(i - SP::INSTR, s.q, s.rq, s.left, qb, wave);
     };
     f32x16 acc[FM][FN];
 #pragma unroll
@@ -135,94 +256,81 @@ __global__ __launch_bounds__(256) void linear_kernel(LinearArgs a, uint32_t tile
         for (int j = 0; j < FN; j++)
 #pragma unroll
             for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
-    issue(0, 0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    int b = 0;
-    for (uint32_t k = 0; k < a.K; k += LIN_KT) {
-        if (k + LIN_KT < a.K) issue(k + LIN_KT, b ^ 1);
+    struct Frags {
+        bf16x8 p[FM], q[FN];
+    };
+    // fragment n in the order of use: the first of P, all of Q, the others of P
+    auto fragment = [&](Frags& f, const char* pb, const char* qb, uint32_t ks, int n) __attribute__((always_inline)) {
+        if (n == 0) f.p[0] = read_fragment<PT>(pb, (wm * FM) * 32u, ks, lane);
+        else if (n <= FN) f.q[n - 1] = read_fragment<QT>(qb, (wn * FN + n - 1) * 32u, ks, lane);
+        else f.p[n - FN] = read_fragment<PT>(pb, (wm * FM + n - FN) * 32u, ks, lane);
+    };
+    // 16 of k: the products of `f`, and between them the reads of what comes next and, with LOAD, a whole step's loads
+    constexpr int MF = FM * FN, RD = FM + FN;
+    auto sixteen = [&](auto LOADC, const Frags& f, Frags& next, const char* pb, const char* qb, uint32_t ks, const Step& s, char* pl, char* ql) __attribute__((always_inline)) {
+        constexpr bool LOAD = decltype(LOADC)::value;
 #pragma unroll
-        for (uint32_t ks = 0; ks < 4; ks++) {
-            bf16x8 pf[FM], qf[FN];
+        for (int g = 0; g < MF; g++) {
+            acc[g / FN][g % FN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.q[g % FN], f.p[g / FN], acc[g / FN][g % FN], 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < FM; i++) pf[i] = read_fragment<PT>(pbuf[b], (wm * FM + i) * 32u, ks, lane);
+            for (int n = 0; n < RD; n++)
+                if (n * MF / RD == g) fragment(next, pb, qb, ks, n);
+            if (LOAD) {
 #pragma unroll
-            for (int j = 0; j < FN; j++) qf[j] = read_fragment<QT>(qbuf[b], (wn * FN + j) * 32u, ks, lane);
-#pragma unroll
-            for (int i = 0; i < FM; i++)
-#pragma unroll
-                for (int j = 0; j < FN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j], pf[i], acc[i][j], 0, 0, 0);
+                for (int i = 0; i < LOADS; i++)
+                    if (i * MF / LOADS == g) load(s, pl, ql, i);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        b ^= 1;
+    };
+    using No = std::integral_constant<bool, false>;
+    using Yes = std::integral_constant<bool, true>;
+    Frags f0, f1;
+    // A step of 64 on the tile in (pc, qc), whose first fragments are in f0.  Its last 16 of k are worked on behind the barrier, from registers: (pc, qc) is free then for the
+    // tile after the next, and the next one, in (pn, qn), has landed.
+    auto step = [&](uint32_t k, char* pc, char* qc, char* pn, char* qn) __attribute__((always_inline)) {
+        const Step s = step_at(k + 2u * LIN_KT);
+        sixteen(No{}, f0, f1, pc, qc, 1, s, pc, qc);
+        sixteen(No{}, f1, f0, pc, qc, 2, s, pc, qc);
+        sixteen(No{}, f0, f1, pc, qc, 3, s, pc, qc);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        sixteen(Yes{}, f1, f0, pn, qn, 0, s, pc, qc);
+    };
+    const Step first = step_at(0), second = step_at(LIN_KT);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) load(first, pbuf0, qbuf0, i);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) load(second, pbuf1, qbuf1, i);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int n = 0; n < RD; n++) fragment(f0, pbuf0, qbuf0, 0, n);
+    for (uint32_t k = 0; k < a.K; k += 2u * LIN_KT) {  // a second step behind the end adds zeros
+        step(k, pbuf0, qbuf0, pbuf1, qbuf1);
+        step(k + LIN_KT, pbuf1, qbuf1, pbuf0, qbuf0);
     }
-    // the epilogue: a lane has row m and, of every block of 32 channels, 8 g + 4 h .. + 3
-    const LinearEpilogue& e = a.e;
-    const uint32_t h = lane >> 5;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads behind the end still write (zeros) to LDS
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    // the epilogue, 32 rows of the wavefront at a time, through LDS
+    char* const stage = wave == 0u ? pbuf0 : wave == 1u ? pbuf1 : wave == 2u ? qbuf0 : qbuf1;
+    Out<FN> out(a, n0 + wn * (FN * 32u), lane);
 #pragma unroll
     for (int i = 0; i < FM; i++) {
-        const uint32_t m = m0 + (wm * FM + i) * 32u + (lane & 31u);
-        const bool row_in = m < a.M;
-        const size_t row = (size_t)(row_in ? m : 0u) * a.N;
-#pragma unroll
-        for (int j = 0; j < FN; j++) {
-            const uint32_t nb = n0 + (wn * FN + j) * 32u;
-            f32x4 z[4];
-            uint32_t top = 0u;
-#pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const uint32_t n = nb + 8u * g + 4u * h;
-                z[g] = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                if (n < a.N) {
-                    z[g] = with_bias(e, z[g], n);
-#pragma unroll
-                    for (int x = 0; x < 4; x++) {
-                        const uint32_t s = ckpt_size(z[g][x]);
-                        top = s > top ? s : top;
-                    }
-                }
-            }
-            uint32_t byte = 0u;
-            if (e.pre_scales != nullptr) {
-                const uint32_t o = (uint32_t)__shfl_xor((int)top, 32);
-                byte = ckpt_byte(o > top ? o : top);
-                if (row_in && nb < a.N && h == 0u) ((unsigned char*)e.pre_scales)[(size_t)m * ((a.N + 31u) / 32u) + nb / 32u] = (unsigned char)byte;
-            }
-#pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const uint32_t n = nb + 8u * g + 4u * h;
-                if (!row_in || n >= a.N) continue;
-                if (e.pre_scales != nullptr) *(uint32_t*)((char*)e.pre + row + n) = ckpt_codes(z[g][0], z[g][1], z[g][2], z[g][3], ckpt_down(byte));
-                else if (e.pre != nullptr) {
-                    bf16x4 o;
-#pragma unroll
-                    for (int x = 0; x < 4; x++) o[x] = (__bf16)z[g][x];
-                    *(bf16x4*)((__bf16*)e.pre + row + n) = o;
-                }
-                f32x4 y;
-#pragma unroll
-                for (int x = 0; x < 4; x++) y[x] = act_value(e.act, z[g][x]);
-                if (e.residual != nullptr) {
-                    const bf16x4 r = *(const bf16x4*)((const __bf16*)e.residual + row + n);
-#pragma unroll
-                    for (int x = 0; x < 4; x++) y[x] += (float)r[x];
-                }
-                bf16x4 o;
-#pragma unroll
-                for (int x = 0; x < 4; x++) o[x] = (__bf16)y[x];
-                *(bf16x4*)((__bf16*)e.out + row + n) = o;
-            }
-        }
+        out.lay_down(stage, acc[i], lane);
+        out.rows(stage, a, m0 + (wm * FM + i) * 32u, lane);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
 template <int FORM>
 static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
-    constexpr int BM = 128, BN = 128;
+    constexpr int BM = 256, BN = 256;
     const uint32_t tiles_m = (a.M + BM - 1u) / BM, tiles_n = (a.N + BN - 1u) / BN;
     if (!fits_grid((uint64_t)tiles_m * tiles_n, 256u)) return hipErrorInvalidConfiguration;
-    linear_kernel<BM, BN, FORM><<<tiles_m * tiles_n, 256, 0, stream>>>(a, tiles_n);
+    linear_kernel<BM, BN, FORM><<<tiles_m * tiles_n, 256, 0, stream>>>(a, make_tile_map(tiles_m, tiles_n));
     return hipGetLastError();
 }
 
