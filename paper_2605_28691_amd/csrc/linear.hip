@@ -2,13 +2,16 @@
 //     z = C + bias (kept, if asked for, in bf16 or as an 8-bit checkpoint),  out = act(z) + residual
 // Three forms:  out = x w^T (neither operand transposed),  dx = dz w (Q = w given as [k][n]),  dw = dz^T x (both given as [k][..]).
 //
-//   * The MFMA takes Q's rows as its A operand and P's as B, so that a lane's accumulators are 16 channels of ONE row of C: bias, residual and the blocks of a
-//     checkpoint are its own.
+//   * v_mfma_f32_16x16x32_bf16: the board's power sets the clock on real data, and this form takes less of it than 32x32x16, which reads and writes twice the accumulators
+//     a product (products alone, operands N(0,1): 2041 and 1820 TFLOP/s; on zeros 2419 and 2453).  Q's rows are its A operand, P's its B.
+//   * A workgroup is 4 wavefronts, 2 x 2, one a SIMD; at 256 x 256 each has 128 x 128 of C in 256 accumulation registers, so that a fragment read from LDS feeds 8
+//     products.
 //   * Tiles go from memory straight into LDS (buffer_load_dwordx4 ... lds), 64 of k a step, double buffered.  Operands with k along the row are laid out in rows of
 //     128 bytes and read 16 bytes at a time; transposed ones in rows of 256 and read with ds_read_b64_tr_b16; swizzles as in lds_layout.h.
 //   * Ends: a 16-byte piece behind the end of k is given an offset outside the buffer and reads as zero; transposed operands end with the buffer; rows
 //     past the last read the last one, columns past the last whatever lies there, and neither is stored.
 #include <type_traits>
+#include <utility>
 
 #include "checkpoint.h"
 #include "kernels.h"
@@ -20,7 +23,6 @@ namespace skiparse {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 #define LDS_PTR(T) __attribute__((address_space(3))) T*
 
@@ -28,13 +30,15 @@ constexpr uint32_t LIN_KT = 64;           // of k a step
 constexpr uint32_t LIN_OUTSIDE = ~0u;     // an offset outside every buffer
 constexpr uint32_t LIN_RECORDS = 0xfffffff0u;
 
-// One operand's side of a workgroup's tile: ROWS of m (or n) by 64 of k.
+// One operand's side of a workgroup's tile: ROWS of m (or n).
+//   !T: a step, 64 of k, in one piece: rows of 128 bytes, whole lines of the caches (64 bytes of a line at a time, 8192^3 took 900 us instead of 846)
+//    T: halves of 32 rows of k, 128 columns (256 bytes) each, which are free and filled again one after the other
 template <int ROWS, bool T, int NW>
 struct Side {
-    static constexpr int INSTR = ROWS * 128 / 1024 / NW;  // direct loads of a wavefront and step, 1 KiB each
-    static constexpr int BYTES = ROWS * 128;
-    uint32_t off[INSTR];  // of the lane's piece from the step's base
-    uint32_t kofs[INSTR]; // !T: where in the step's k it lies
+    static constexpr int INSTR = ROWS * (T ? 64 : 128) / 1024 / NW;  // direct loads of a wavefront and piece, 1 KiB each
+    static constexpr int BYTES = ROWS * (T ? 64 : 128);
+    uint32_t off[INSTR];   // of the lane's chunk from the piece's base
+    uint32_t kofs[INSTR];  // !T: where in the step's k it lies
     // row_off: byte offset of row r of the tile from the base (!T), row_bytes: of a row of k (T)
     template <typename F>
     __device__ __attribute__((always_inline)) inline void init(uint32_t wave, uint32_t lane, uint32_t row_bytes, F row_off) {
@@ -46,7 +50,7 @@ struct Side {
                 kofs[i] = ((lane % 8u) ^ lds_swizzle<64>(r)) * 8u;
                 off[i] = row_off(r) + kofs[i] * 2u;
             } else {
-                const uint32_t part = n / 16u, r = n % 16u * 4u + lane / 16u;  // 128 columns a part
+                const uint32_t part = n / 8u, r = n % 8u * 4u + lane / 16u;  // 128 columns a part
                 kofs[i] = 0u;
                 off[i] = r * row_bytes + part * 256u + ((lane % 16u) ^ lds_swizzle<128>(r)) * 16u;
             }
@@ -60,21 +64,17 @@ struct Side {
     }
 };
 
-// Fragment of 32 rows from `row0` (a multiple of 32) and 16 of k: lane l has row l % 32, k = 16 ks + 8 (l / 32) ...
+// Fragment of 16 rows from `row0` (a multiple of 16) and 32 of k, the step's half `half`: lane l has row l % 16, k = 8 (l / 16) ...  T: `buf` is the half.
 template <bool T>
-__device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char* buf, uint32_t row0, uint32_t ks, uint32_t lane) {
-    const uint32_t h = lane >> 5;
-    if (!T) {
-        const uint32_t r = lane & 31u;
-        return *(const bf16x8*)(buf + (row0 + r) * 128u + ((2u * ks + h) ^ lds_swizzle<64>(r)) * 16u);
-    }
-    const uint32_t li = lane & 15u, group = lane >> 4 & 1u;
-    const char* const part = buf + row0 / 128u * 16384u;
+__device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char* buf, uint32_t row0, uint32_t half, uint32_t lane) {
+    const uint32_t li = lane & 15u, g = lane >> 4;
+    if (!T) return *(const bf16x8*)(buf + (row0 + li) * 128u + ((4u * half + g) ^ lds_swizzle<64>(li)) * 16u);
+    const char* const part = buf + row0 / 128u * 8192u;
     bf16x4 v[2];
 #pragma unroll
     for (uint32_t sec = 0; sec < 2; sec++) {
-        const uint32_t r = 16u * ks + 8u * h + 4u * sec + (li >> 2);
-        const uint32_t c = row0 % 128u / 8u + group * 2u + ((li & 3u) >> 1);
+        const uint32_t r = 8u * g + 4u * sec + (li >> 2);
+        const uint32_t c = row0 % 128u / 8u + ((li & 3u) >> 1);
         const char* const at = part + r * 256u + ((c ^ lds_swizzle<128>(r)) * 16u) + 8u * (li & 1u);
         v[sec] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(LDS_PTR(char))at);
     }
@@ -83,7 +83,7 @@ __device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char
 
 // Workgroup -> tile.  Workgroup id % 8 is the XCD; each XCD has a contiguous range of an order in which TILE_GROUP tiles of m are walked together along n, so that the 32
 // tiles that it works on at once share operands in its L2.
-constexpr uint32_t TILE_GROUP = 8;
+constexpr uint32_t TILE_GROUP = 4;
 struct TileMap {
     Div32 group;   // tiles of a group: TILE_GROUP * tiles_n
     Div32 size, last;  // tiles of m in a group, in the last one
@@ -103,12 +103,12 @@ static TileMap make_tile_map(uint32_t tiles_m, uint32_t tiles_n) {
     return {make_div32(TILE_GROUP * tiles_n), make_div32(TILE_GROUP), make_div32(rest ? rest : 1u), tiles_m, tiles_m * tiles_n, tiles_m * tiles_n / 8u};
 }
 
-// The way out: 32 rows by 32 FN channels of C at a time, a wavefront's own.  The sums are laid down in LDS as they are (float32: a residual is added before the one
+// The way out: 32 rows by 16 FN channels of C at a time, a wavefront's own.  The sums are laid down in LDS as they are (float32: a residual is added before the one
 // rounding) and picked up 8 channels of a row a lane, so that everything in memory is moved in 16-byte pieces of whole rows, and a checkpoint's blocks are four
 // neighbouring lanes.
 template <int FN>
 struct Out {
-    static constexpr uint32_t LPR = FN * 4, RPI = 64 / LPR;  // lanes a row, rows at once
+    static constexpr uint32_t LPR = FN * 2, RPI = 64 / LPR;  // lanes a row, rows at once
     uint32_t n;      // the lane's channels n .. n + 7
     bool in;
     float bias[8];
@@ -124,22 +124,22 @@ struct Out {
         }
     }
     // 16-byte piece c of row r lies at c ^ (r % 16): 8 lanes that write (8 rows) or read (a row) touch different banks
-    __device__ __attribute__((always_inline)) inline static uint32_t place(uint32_t r, uint32_t c) { return r * (FN * 128u) + ((c ^ (r & (FN == 4 ? 15u : 7u))) * 16u); }
-    __device__ __attribute__((always_inline)) inline void lay_down(char* stage, const f32x16 (&acc)[FN], uint32_t lane) const {
-        const uint32_t r = lane & 31u, h = lane >> 5;
+    __device__ __attribute__((always_inline)) inline static uint32_t place(uint32_t r, uint32_t c) { return r * (FN * 64u) + ((c ^ (r & 15u)) * 16u); }
+    __device__ __attribute__((always_inline)) inline void lay_down(char* stage, const f32x4 (&first)[FN], const f32x4 (&second)[FN], uint32_t lane) const {
+        const uint32_t r = lane & 15u, g = lane >> 4;
         // the wavefront's LDS accesses take effect in order; the fences keep the compiler from exchanging them
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int j = 0; j < FN; j++)
-#pragma unroll
-            for (int g = 0; g < 4; g++)
-                *(f32x4*)(stage + place(r, j * 8u + g * 2u + h)) = f32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+        for (int j = 0; j < FN; j++) {
+            *(f32x4*)(stage + place(r, j * 4u + g)) = first[j];
+            *(f32x4*)(stage + place(r + 16u, j * 4u + g)) = second[j];
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
     __device__ __attribute__((always_inline)) inline void rows(const char* stage, const LinearArgs& a, uint32_t m0, uint32_t lane) const {
-#pragma unroll
+#pragma unroll 2
         for (uint32_t it = 0; it < 32u / RPI; it++) {
             const uint32_t r = it * RPI + lane / LPR, c = lane % LPR * 2u;
             const f32x4 x = *(const f32x4*)(stage + place(r, c)), y = *(const f32x4*)(stage + place(r, c + 1u));
@@ -182,9 +182,12 @@ struct Out {
             for (int i = 0; i < 8; i++) o[i] = (__bf16)z[i];
             *(bf16x8*)((__bf16*)e.pre + at) = o;
         }
-        if (e.act != ACT_NONE) {
+        if (e.act == ACT_GELU_TANH) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) z[i] = act_value(e.act, z[i]);
+            for (int i = 0; i < 8; i++) z[i] = act_value(ACT_GELU_TANH, z[i]);
+        } else if (e.act == ACT_SILU) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) z[i] = act_value(ACT_SILU, z[i]);
         }
         if (e.residual != nullptr) {
             const bf16x8 r = *(const bf16x8*)((const __bf16*)e.residual + at);
@@ -198,17 +201,27 @@ struct Out {
     }
 };
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+// f(Int<0>) ... f(Int<N - 1>), written out (the loop of 64 products with what stands between them is too much for the unroller)
+template <int... I, typename F>
+__device__ __attribute__((always_inline)) inline void each(std::integer_sequence<int, I...>, F f) {
+    (f(Int<I>{}), ...);
+}
+template <int N, typename F>
+__device__ __attribute__((always_inline)) inline void each(F f) {
+    each(std::make_integer_sequence<int, N>{}, f);
+}
+
 template <int BM, int BN, int FORM>
 __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kernel(LinearArgs a, TileMap tiles) {
     constexpr bool PT = FORM == LINEAR_DW, QT = FORM != LINEAR_FWD;
-    constexpr int NW = 4, FM = BM / 64, FN = BN / 64;  // wavefronts 2 x 2; blocks of 32 that each has
+    constexpr int NW = 4, FM = BM / 32, FN = BN / 32;  // wavefronts 2 x 2; blocks of 16 that each has
     using SP = Side<BM, PT, NW>;
     using SQ = Side<BN, QT, NW>;
-    // separate arrays: the compiler must be able to tell that the tile being filled is not the tile being read
-    __shared__ __attribute__((aligned(1024))) char pbuf0[SP::BYTES];
-    __shared__ __attribute__((aligned(1024))) char pbuf1[SP::BYTES];
-    __shared__ __attribute__((aligned(1024))) char qbuf0[SQ::BYTES];
-    __shared__ __attribute__((aligned(1024))) char qbuf1[SQ::BYTES];
+    // separate arrays: the compiler must be able to tell that what is being filled is not what is being read.  [buffer][half]; what is in one piece has the first only
+    __shared__ __attribute__((aligned(1024))) char p00[SP::BYTES], p01[PT ? SP::BYTES : 16], p10[SP::BYTES], p11[PT ? SP::BYTES : 16];
+    __shared__ __attribute__((aligned(1024))) char q00[SQ::BYTES], q01[QT ? SQ::BYTES : 16], q10[SQ::BYTES], q11[QT ? SQ::BYTES : 16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave & 1u, wn = wave >> 1;
     uint32_t tm, tn;
@@ -237,7 +250,6 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
         const uint64_t left = (uint64_t)(a.K - k) * ld - col0 * 2u;
         return left < LIN_RECORDS ? (uint32_t)left : LIN_RECORDS;
     };
-    constexpr int LOADS = SP::INSTR + SQ::INSTR;
     struct Step {
         const char *p, *q;
         uint32_t rp, rq, left;
@@ -245,82 +257,98 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
     auto step_at = [&](uint32_t k) __attribute__((always_inline)) -> Step {
         return {p0 + (PT ? (size_t)k * ldp : (size_t)k * 2u), q0 + (QT ? (size_t)k * ldq : (size_t)k * 2u), records(PT, k, ldp, m0), records(QT, k, ldq, n0), k < a.K ? a.K - k : 0u};
     };
-    auto load = [&](const Step& s, char* pb, char* qb, int i) __attribute__((always_inline)) {
-        if (i < SP::INSTR) sp.issue(i, s.p, s.rp, s.left, pb, wave);
-        else sq.issue(i - SP::INSTR, s.q, s.rq, s.left, qb, wave);
-    };
-    f32x16 acc[FM][FN];
+    f32x4 acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; i++)
 #pragma unroll
-        for (int j = 0; j < FN; j++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
+        for (int j = 0; j < FN; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     struct Frags {
         bf16x8 p[FM], q[FN];
     };
-    // fragment n in the order of use: the first of P, all of Q, the others of P
-    auto fragment = [&](Frags& f, const char* pb, const char* qb, uint32_t ks, int n) __attribute__((always_inline)) {
-        if (n == 0) f.p[0] = read_fragment<PT>(pb, (wm * FM) * 32u, ks, lane);
-        else if (n <= FN) f.q[n - 1] = read_fragment<QT>(qb, (wn * FN + n - 1) * 32u, ks, lane);
-        else f.p[n - FN] = read_fragment<PT>(pb, (wm * FM + n - FN) * 32u, ks, lane);
+    struct Half {
+        char *p, *q;
+        uint32_t n;
     };
-    // 16 of k: the products of `f`, and between them the reads of what comes next and, with LOAD, a whole step's loads
+    // fragment i in the order of use: the first of P, all of Q, the others of P
+    auto fragment = [&](Frags& f, const Half& from, int i) __attribute__((always_inline)) {
+        if (i == 0) f.p[0] = read_fragment<PT>(from.p, (wm * FM) * 16u, from.n, lane);
+        else if (i <= FN) f.q[i - 1] = read_fragment<QT>(from.q, (wn * FN + i - 1) * 16u, from.n, lane);
+        else f.p[i - FN] = read_fragment<PT>(from.p, (wm * FM + i - FN) * 16u, from.n, lane);
+    };
+    // Loads of a step's first part (the first halves of transposed operands) and of its second (operands in one piece, the second halves).
+    constexpr int LOADS_A = (PT ? SP::INSTR : 0) + (QT ? SQ::INSTR : 0), WHOLE = (PT ? 0 : SP::INSTR) + (QT ? 0 : SQ::INSTR), LOADS_B = WHOLE + LOADS_A;
+    auto load_a = [&](const Step& s, const Half& to, int i) __attribute__((always_inline)) {
+        if (PT && i < SP::INSTR) sp.issue(i, s.p, s.rp, s.left, to.p, wave);
+        else if (QT) sq.issue(i - (PT ? SP::INSTR : 0), s.q, s.rq, s.left, to.q, wave);
+    };
+    auto load_b = [&](const Step& whole, const Half& first, const Step& s, const Half& second, int i) __attribute__((always_inline)) {
+        if (i >= WHOLE) load_a(s, second, i - WHOLE);
+        else if (!PT && i < SP::INSTR) sp.issue(i, whole.p, whole.rp, whole.left, first.p, wave);
+        else if (!QT) sq.issue(i - (PT ? 0 : SP::INSTR), whole.q, whole.rq, whole.left, first.q, wave);
+    };
+    // 32 of k: the products of `f`; between them the fragments of what comes next are read, and `load`s are sent off
     constexpr int MF = FM * FN, RD = FM + FN;
-    auto sixteen = [&](auto LOADC, const Frags& f, Frags& next, const char* pb, const char* qb, uint32_t ks, const Step& s, char* pl, char* ql) __attribute__((always_inline)) {
-        constexpr bool LOAD = decltype(LOADC)::value;
-#pragma unroll
-        for (int g = 0; g < MF; g++) {
-            acc[g / FN][g % FN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.q[g % FN], f.p[g / FN], acc[g / FN][g % FN], 0, 0, 0);
-#pragma unroll
-            for (int n = 0; n < RD; n++)
-                if (n * MF / RD == g) fragment(next, pb, qb, ks, n);
-            if (LOAD) {
-#pragma unroll
-                for (int i = 0; i < LOADS; i++)
-                    if (i * MF / LOADS == g) load(s, pl, ql, i);
-            }
+    auto part = [&](auto LOADC, const Frags& f, Frags& next, const Half& from, auto load) __attribute__((always_inline)) {
+        constexpr int LOADS = decltype(LOADC)::value;
+        each<MF>([&](auto G) __attribute__((always_inline)) {
+            constexpr int g = decltype(G)::value;
+            asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[g / FN][g % FN]) : "v"(f.q[g % FN]), "v"(f.p[g / FN]));
+            // number i of n stands behind product i * MF / n
+            constexpr int first = (g * RD + MF - 1) / MF, last = ((g + 1) * RD + MF - 1) / MF;
+            each<last - first>([&](auto I) __attribute__((always_inline)) { fragment(next, from, first + decltype(I)::value); });
+            constexpr int lf = (g * LOADS + MF - 1) / MF, ll = ((g + 1) * LOADS + MF - 1) / MF;
+            each<ll - lf>([&](auto I) __attribute__((always_inline)) { load(lf + decltype(I)::value); });
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
     };
-    using No = std::integral_constant<bool, false>;
-    using Yes = std::integral_constant<bool, true>;
-    Frags f0, f1;
-    // A step of 64 on the tile in (pc, qc), whose first fragments are in f0.  Its last 16 of k are worked on behind the barrier, from registers: (pc, qc) is free then for the
-    // tile after the next, and the next one, in (pn, qn), has landed.
-    auto step = [&](uint32_t k, char* pc, char* qc, char* pn, char* qn) __attribute__((always_inline)) {
-        const Step s = step_at(k + 2u * LIN_KT);
-        sixteen(No{}, f0, f1, pc, qc, 1, s, pc, qc);
-        sixteen(No{}, f1, f0, pc, qc, 2, s, pc, qc);
-        sixteen(No{}, f0, f1, pc, qc, 3, s, pc, qc);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // What this wavefront has read is in registers, and all but its last N loads have landed: behind the barrier that holds for the workgroup.
+    auto meet = [&](auto NC) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(NC)::value) : "memory");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        sixteen(Yes{}, f1, f0, pn, qn, 0, s, pc, qc);
     };
-    const Step first = step_at(0), second = step_at(LIN_KT);
+    Frags f0, f1;
+    // A step of 64, tile t at k: halves c0 and c1, of which c0 is in f0; the next tile's first half is n0.  A half is free once it is in registers, and is filled with its part
+    // of tile t + 2 at once: what comes in halves 3/2 steps before it is read, what comes in one piece a step before.
+    auto step = [&](uint32_t k, const Half& c0, const Half& c1, const Half& n0) __attribute__((always_inline)) {
+        const Step s0 = step_at(k + 2u * LIN_KT), s1 = step_at(k + 2u * LIN_KT + LIN_KT / 2u);
+        part(Int<LOADS_A>{}, f0, f1, c1, [&](int i) __attribute__((always_inline)) { load_a(s0, c0, i); });
+        meet(Int<2 * LOADS_A>{});
+        part(Int<LOADS_B>{}, f1, f0, n0, [&](int i) __attribute__((always_inline)) { load_b(s0, c0, s1, c1, i); });
+        if (LOADS_A) meet(Int<LOADS_A + LOADS_B>{});
+    };
+    const Half h00 = {p00, q00, 0}, h01 = {PT ? p01 : p00, QT ? q01 : q00, 1}, h10 = {p10, q10, 0}, h11 = {PT ? p11 : p10, QT ? q11 : q10, 1};
+    auto fill = [&](uint32_t k, const Half& first, const Half& second) __attribute__((always_inline)) {
+        const Step s0 = step_at(k), s1 = step_at(k + LIN_KT / 2u);
 #pragma unroll
-    for (int i = 0; i < LOADS; i++) load(first, pbuf0, qbuf0, i);
+        for (int i = 0; i < LOADS_A; i++) load_a(s0, first, i);
 #pragma unroll
-    for (int i = 0; i < LOADS; i++) load(second, pbuf1, qbuf1, i);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+        for (int i = 0; i < LOADS_B; i++) load_b(s0, first, s1, second, i);
+    };
+    fill(0, h00, h01);
+    fill(LIN_KT, h10, h11);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS_A + LOADS_B) : "memory");
     __builtin_amdgcn_s_barrier();
 #pragma unroll
-    for (int n = 0; n < RD; n++) fragment(f0, pbuf0, qbuf0, 0, n);
+    for (int i = 0; i < RD; i++) fragment(f0, h00, i);
+    if (LOADS_A) meet(Int<LOADS_A + LOADS_B>{});
     for (uint32_t k = 0; k < a.K; k += 2u * LIN_KT) {  // a second step behind the end adds zeros
-        step(k, pbuf0, qbuf0, pbuf1, qbuf1);
-        step(k + LIN_KT, pbuf1, qbuf1, pbuf0, qbuf0);
+        step(k, h00, h01, h10);
+        step(k + LIN_KT, h10, h11, h00);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads behind the end still write (zeros) to LDS
+    // The products are written as asm, with their accumulators pinned to accumulation registers: left to choose, the compiler moved 200 of them in and out a step.  It does not
+    // see their latency then: the last ones are waited for here.
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_waitcnt vmcnt(0)" ::: "memory");  // loads behind the end still write (zeros) to LDS
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     // the epilogue, 32 rows of the wavefront at a time, through LDS
-    char* const stage = wave == 0u ? pbuf0 : wave == 1u ? pbuf1 : wave == 2u ? qbuf0 : qbuf1;
-    Out<FN> out(a, n0 + wn * (FN * 32u), lane);
+    char* const stage = wave == 0u ? p00 : wave == 1u ? p10 : wave == 2u ? q00 : q10;
+    Out<FN> out(a, n0 + wn * (FN * 16u), lane);
 #pragma unroll
-    for (int i = 0; i < FM; i++) {
-        out.lay_down(stage, acc[i], lane);
-        out.rows(stage, a, m0 + (wm * FM + i) * 32u, lane);
+    for (int i = 0; i < FM; i += 2) {
+        out.lay_down(stage, acc[i], acc[i + 1], lane);
+        out.rows(stage, a, m0 + (wm * FM + i) * 16u, lane);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
