@@ -681,14 +681,13 @@ static bool touches(Span x, std::initializer_list<Span> others) {
 }
 
 size_t skiparse_linear_workspace_bytes(int rows, int in_features, int out_features) {
-    (void)rows; (void)in_features; (void)out_features;
-    return 0;
+    if (rows < 1 || in_features < 1 || out_features < 1) return 0;
+    return linear_workspace((uint32_t)rows, (uint32_t)out_features, (uint32_t)in_features);
 }
 
 int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, void* out, void* pre, void* pre_scales, int B, int T, int H, int W,
                         int in_features, int out_features, int s, int pattern, int order, int act, int dtype, void* workspace, size_t workspace_bytes,
                         void* stream) {
-    (void)workspace; (void)workspace_bytes;
     if (!x || !w || !out || (pre_scales && !pre)) return SKIPARSE_EINVAL;
     bool moved;
     size_t rows;
@@ -702,10 +701,14 @@ int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const vo
     const Span sp = {pre, rows * N * (pre_scales ? 1 : 2)}, ss = {pre_scales, checkpoint_scales(rows, N)}, sr = {residual, rows * N * 2};
     if (touches(so, {sx, sw, sb, sp, ss}) || (residual && residual != out && overlap2(out, so.bytes, residual, sr.bytes))) return SKIPARSE_EINVAL;
     if (touches(sp, {sx, sw, sb, ss, sr}) || touches(ss, {sx, sw, sb, sr})) return SKIPARSE_EINVAL;
+    const size_t need = linear_workspace((uint32_t)rows, (uint32_t)N, (uint32_t)K);
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
+    if (touches({need ? workspace : nullptr, need}, {sx, sw, sb, sr, so, sp, ss})) return SKIPARSE_EINVAL;
     LinearArgs a = {};
     a.p = x; a.q = w;
     a.M = (uint32_t)rows; a.N = (uint32_t)N; a.K = (uint32_t)K;
     a.e = {bias, residual, out, pre, pre_scales, act};
+    a.partial = (float*)workspace;
     a.order = moved ? order : SKIPARSE_ORDER_SAME;
     if (moved) {
         const GridMap g = make_gridmap(T, H, W, s, pattern);
@@ -716,20 +719,22 @@ int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const vo
 
 // What a backward call keeps in its workspace, one after the other.
 struct LinearBwdSpace {
-    size_t dz, x, db, total;
+    size_t dz, x, db, parts, total;
 };
-static LinearBwdSpace linear_bwd_space(size_t rows, size_t K, size_t N, bool dz, bool x, bool db) {
+static LinearBwdSpace linear_bwd_space(size_t rows, size_t K, size_t N, bool dz, bool x, bool db, bool dx, bool dw) {
     LinearBwdSpace l;
     l.dz = dz ? align256(rows * N * 2) : 0;
     l.x = x ? align256(rows * K * 2) : 0;
     l.db = db ? align256((size_t)linear_rows_parts((uint32_t)rows) * N * sizeof(float)) : 0;
-    l.total = l.dz + l.x + l.db;
+    const size_t px = dx ? linear_workspace((uint32_t)rows, (uint32_t)K, (uint32_t)N) : 0, pw = dw ? linear_workspace((uint32_t)N, (uint32_t)K, (uint32_t)rows) : 0;
+    l.parts = px > pw ? px : pw;  // one product after the other
+    l.total = l.dz + l.x + l.db + l.parts;
     return l;
 }
 
 size_t skiparse_linear_bwd_workspace_bytes(int rows, int in_features, int out_features, int order, int act, int x_checkpoint) {
     if (rows < 1 || in_features < 1 || out_features < 1 || !valid_order(order, false) || act < SKIPARSE_ACT_NONE || act > SKIPARSE_ACT_SILU) return 0;
-    return linear_bwd_space((size_t)rows, (size_t)in_features, (size_t)out_features, order != SKIPARSE_ORDER_SAME || act != SKIPARSE_ACT_NONE, x_checkpoint != 0, true).total;
+    return linear_bwd_space((size_t)rows, (size_t)in_features, (size_t)out_features, order != SKIPARSE_ORDER_SAME || act != SKIPARSE_ACT_NONE, x_checkpoint != 0, true, true, true).total;
 }
 
 int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, const void* w, const void* pre, const void* pre_scales, const void* dx_add, void* dx,
@@ -747,7 +752,7 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
     if (!dw) x = x_scales = nullptr;
     if (!dx) w = nullptr;
     const size_t K = (size_t)in_features, N = (size_t)out_features;
-    const LinearBwdSpace l = linear_bwd_space(rows, K, N, (dx || dw) && (moved || act != SKIPARSE_ACT_NONE), x_scales != nullptr, db != nullptr);
+    const LinearBwdSpace l = linear_bwd_space(rows, K, N, (dx || dw) && (moved || act != SKIPARSE_ACT_NONE), x_scales != nullptr, db != nullptr, dx != nullptr, dw != nullptr);
     if (l.total && (!workspace || workspace_bytes < l.total || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
     const Span sy = {dy, rows * N * 2}, sx = {x, rows * K * (x_scales ? 1 : 2)}, sxs = {x_scales, checkpoint_scales(rows, K)}, sw = {w, N * K * 2};
     const Span sp = {pre, rows * N * (pre_scales ? 1 : 2)}, sps = {pre_scales, checkpoint_scales(rows, N)}, sa = {dx_add, rows * K * 2};
@@ -759,6 +764,7 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
     char* const at = (char*)workspace;
     hipError_t e;
     const void* dz = dy;
+    float* const partial = (float*)(at + l.dz + l.x + l.db);
     if (l.dz || db) {
         LinearRowsArgs r = {};
         r.dy = dy; r.pre = pre; r.pre_scales = pre_scales;
@@ -785,6 +791,7 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
         a.p = dz; a.q = w;
         a.M = (uint32_t)rows; a.N = (uint32_t)K; a.K = (uint32_t)N;
         a.e = {nullptr, dx_add, dx, nullptr, nullptr, ACT_NONE};
+        a.partial = partial;
         if ((e = launch_linear(LINEAR_DX, a, st)) != hipSuccess) return finish(e);
     }
     if (dw) {
@@ -792,6 +799,7 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
         a.p = dz; a.q = x;
         a.M = (uint32_t)N; a.N = (uint32_t)K; a.K = (uint32_t)rows;
         a.e = {nullptr, nullptr, dw, nullptr, nullptr, ACT_NONE};
+        a.partial = partial;
         if ((e = launch_linear(LINEAR_DW, a, st)) != hipSuccess) return finish(e);
     }
     return SKIPARSE_OK;

@@ -209,7 +209,9 @@ struct LinearArgs {
     LinearEpilogue e;
     int order;     // ORDER_SAME, or the row map from which row m of C takes its row of P (LINEAR_FWD only)
     RowArgs rows;
+    float* partial;  // linear_workspace() bytes
 };
+size_t linear_workspace(uint32_t M, uint32_t N, uint32_t K);
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream);
 
 // The passes over rows in front of a backward's products.

@@ -17,6 +17,7 @@
 #include "kernels.h"
 #include "lds_layout.h"
 #include "linear_act.h"
+#include "linear_plan.h"
 
 namespace skiparse {
 
@@ -85,22 +86,41 @@ __device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char
 // tiles that it works on at once share operands in its L2.
 constexpr uint32_t TILE_GROUP = 4;
 struct TileMap {
-    Div32 group;   // tiles of a group: TILE_GROUP * tiles_n
+    Div32 group;       // tiles of a group: TILE_GROUP * tiles_n
     Div32 size, last;  // tiles of m in a group, in the last one
-    uint32_t tiles_m, total, per_xcd;
-    __device__ inline void at(uint32_t id, uint32_t& tm, uint32_t& tn) const {
-        const uint32_t xcd = id & 7u, rest = total & 7u;  // the first `rest` XCDs have one tile more
-        const uint32_t lin = xcd * per_xcd + (xcd < rest ? xcd : rest) + (id >> 3);
+    Div32 rest;        // tiles that are cut along k
+    uint32_t tiles_m, whole, parts, per;
+    static __device__ inline uint32_t of_xcd(uint32_t id, uint32_t total) {
+        const uint32_t xcd = id & 7u, over = total & 7u;  // the first `over` XCDs have one more
+        return xcd * (total >> 3) + (xcd < over ? xcd : over) + (id >> 3);
+    }
+    // tile number `lin`
+    __device__ inline void tile(uint32_t lin, uint32_t& tm, uint32_t& tn) const {
         const uint32_t g = group.div(lin), in = lin - g * group.d, first = g * TILE_GROUP;
         const bool full = first + TILE_GROUP <= tiles_m;
-        const uint32_t n = full ? size.div(in) : last.div(in);
-        tn = n;
-        tm = first + in - n * (full ? size.d : last.d);
+        tn = full ? size.div(in) : last.div(in);
+        tm = first + in - tn * (full ? size.d : last.d);
+    }
+    // workgroup `id`: its tile, its range of k, and for a part its number among the parts, else ~0
+    __device__ inline void at(uint32_t id, uint32_t K, uint32_t& tm, uint32_t& tn, uint32_t& k0, uint32_t& k1, uint32_t& slot) const {
+        k0 = 0u;
+        k1 = K;
+        slot = ~0u;
+        if (id < whole) {
+            tile(of_xcd(id, whole), tm, tn);
+            return;
+        }
+        const uint32_t lin = of_xcd(id - whole, rest.d * parts);  // neighbours: tiles that walk the same k
+        const uint32_t part = rest.div(lin), r = lin - part * rest.d;
+        tile(whole + r, tm, tn);
+        k0 = part * per;
+        k1 = K - k0 < per ? K : k0 + per;
+        slot = r * parts + part;
     }
 };
-static TileMap make_tile_map(uint32_t tiles_m, uint32_t tiles_n) {
-    const uint32_t rest = tiles_m % TILE_GROUP;
-    return {make_div32(TILE_GROUP * tiles_n), make_div32(TILE_GROUP), make_div32(rest ? rest : 1u), tiles_m, tiles_m * tiles_n, tiles_m * tiles_n / 8u};
+static TileMap make_tile_map(const LinearPlan& p) {
+    const uint32_t over = p.tiles_m % TILE_GROUP;
+    return {make_div32(TILE_GROUP * p.tiles_n), make_div32(TILE_GROUP), make_div32(over ? over : 1u), make_div32(p.rest ? p.rest : 1u), p.tiles_m, p.whole, p.parts, p.per};
 }
 
 // The way out: 32 rows by 16 FN channels of C at a time, a wavefront's own.  The sums are laid down in LDS as they are (float32: a residual is added before the one
@@ -224,8 +244,8 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
     __shared__ __attribute__((aligned(1024))) char q00[SQ::BYTES], q01[QT ? SQ::BYTES : 16], q10[SQ::BYTES], q11[QT ? SQ::BYTES : 16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave & 1u, wn = wave >> 1;
-    uint32_t tm, tn;
-    tiles.at(blockIdx.x, tm, tn);
+    uint32_t tm, tn, k0, k1, slot;
+    tiles.at(blockIdx.x, a.K, tm, tn, k0, k1, slot);
     const uint32_t m0 = tm * BM, n0 = tn * BN;
     const uint32_t ldp = (PT ? a.M : a.K) * 2u, ldq = (QT ? a.N : a.K) * 2u;  // bytes
     const bool mapped = FORM == LINEAR_FWD && a.order != 0;
@@ -245,9 +265,9 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
     const char* const q0 = (const char*)a.q + (QT ? (size_t)n0 * 2u : (size_t)n0 * ldq);
     // bytes of a buffer that begins with row k: what a transposed operand still has; 0 behind the end
     auto records = [&](bool t, uint32_t k, uint32_t ld, uint32_t col0) __attribute__((always_inline)) -> uint32_t {
-        if (k >= a.K) return 0u;
+        if (k >= k1) return 0u;
         if (!t) return LIN_RECORDS;
-        const uint64_t left = (uint64_t)(a.K - k) * ld - col0 * 2u;
+        const uint64_t left = (uint64_t)(k1 - k) * ld - col0 * 2u;
         return left < LIN_RECORDS ? (uint32_t)left : LIN_RECORDS;
     };
     struct Step {
@@ -255,7 +275,7 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
         uint32_t rp, rq, left;
     };
     auto step_at = [&](uint32_t k) __attribute__((always_inline)) -> Step {
-        return {p0 + (PT ? (size_t)k * ldp : (size_t)k * 2u), q0 + (QT ? (size_t)k * ldq : (size_t)k * 2u), records(PT, k, ldp, m0), records(QT, k, ldq, n0), k < a.K ? a.K - k : 0u};
+        return {p0 + (PT ? (size_t)k * ldp : (size_t)k * 2u), q0 + (QT ? (size_t)k * ldq : (size_t)k * 2u), records(PT, k, ldp, m0), records(QT, k, ldq, n0), k < k1 ? k1 - k : 0u};
     };
     f32x4 acc[FM][FN];
 #pragma unroll
@@ -325,14 +345,14 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
 #pragma unroll
         for (int i = 0; i < LOADS_B; i++) load_b(s0, first, s1, second, i);
     };
-    fill(0, h00, h01);
-    fill(LIN_KT, h10, h11);
+    fill(k0, h00, h01);
+    fill(k0 + LIN_KT, h10, h11);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS_A + LOADS_B) : "memory");
     __builtin_amdgcn_s_barrier();
 #pragma unroll
     for (int i = 0; i < RD; i++) fragment(f0, h00, i);
     if (LOADS_A) meet(Int<LOADS_A + LOADS_B>{});
-    for (uint32_t k = 0; k < a.K; k += 2u * LIN_KT) {  // a second step behind the end adds zeros
+    for (uint32_t k = k0; k < k1; k += 2u * LIN_KT) {  // a second step behind the end adds zeros
         step(k, h00, h01, h10);
         step(k + LIN_KT, h10, h11, h00);
     }
@@ -340,6 +360,14 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
     // see their latency then: the last ones are waited for here.
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_waitcnt vmcnt(0)" ::: "memory");  // loads behind the end still write (zeros) to LDS
     __builtin_amdgcn_sched_barrier(0);
+    if (slot != ~0u) {  // a part: sums as they lie in the registers, for linear_join_kernel
+        f32x4* const to = (f32x4*)a.partial + ((size_t)slot * 4u + wave) * (FM * FN * 64u) + lane;
+#pragma unroll
+        for (int i = 0; i < FM; i++)
+#pragma unroll
+            for (int j = 0; j < FN; j++) to[(i * FN + j) * 64] = acc[i][j];
+        return;
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     // the epilogue, 32 rows of the wavefront at a time, through LDS
@@ -353,14 +381,49 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
     }
 }
 
-template <int FORM>
-static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
-    constexpr int BM = 256, BN = 256;
-    const uint32_t tiles_m = (a.M + BM - 1u) / BM, tiles_n = (a.N + BN - 1u) / BN;
-    if (!fits_grid((uint64_t)tiles_m * tiles_n, 256u)) return hipErrorInvalidConfiguration;
-    linear_kernel<BM, BN, FORM><<<tiles_m * tiles_n, 256, 0, stream>>>(a, make_tile_map(tiles_m, tiles_n));
+// Adds up the parts of a tile, in order, and finishes 32 rows of a wavefront's share.
+template <int BM, int BN>
+__global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a, TileMap tiles) {
+    constexpr int FM = BM / 32, FN = BN / 32;
+    constexpr uint32_t UNITS = 4 * FM / 2;  // of a tile
+    __shared__ __attribute__((aligned(16))) char stage[32 * FN * 64];
+    const uint32_t lane = threadIdx.x, r = blockIdx.x / UNITS, unit = blockIdx.x % UNITS, wave = unit / (FM / 2), i = unit % (FM / 2) * 2u;
+    uint32_t tm, tn;
+    tiles.tile(tiles.whole + r, tm, tn);
+    const f32x4* from = (const f32x4*)a.partial + ((size_t)r * tiles.parts * 4u + wave) * (FM * FN * 64u) + i * (FN * 64u) + lane;
+    f32x4 acc[2][FN];
+#pragma unroll
+    for (int j = 0; j < 2 * FN; j++) acc[j / FN][j % FN] = from[j * 64];
+    for (uint32_t p = 1; p < tiles.parts; p++) {
+        from += 4 * FM * FN * 64;
+#pragma unroll
+        for (int j = 0; j < 2 * FN; j++) acc[j / FN][j % FN] += from[j * 64];
+    }
+    const Out<FN> out(a, tn * BN + (wave >> 1) * (FN * 16u), lane);
+    out.lay_down(stage, acc[0], acc[1], lane);
+    out.rows(stage, a, tm * BM + ((wave & 1u) * FM + i) * 16u, lane);
+}
+
+template <int SHAPE, int FORM>
+static hipError_t launch_tiles(const LinearArgs& a, const LinearPlan& p, hipStream_t stream) {
+    constexpr int BM = LINEAR_TILE[SHAPE].m, BN = LINEAR_TILE[SHAPE].n;
+    const uint64_t blocks = (uint64_t)p.whole + (uint64_t)p.rest * p.parts;
+    if (!fits_grid(blocks, 256u)) return hipErrorInvalidConfiguration;
+    const TileMap tiles = make_tile_map(p);
+    linear_kernel<BM, BN, FORM><<<(uint32_t)blocks, 256, 0, stream>>>(a, tiles);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.rest == 0u) return e;
+    linear_join_kernel<BM, BN><<<p.rest * (4u * BM / 64u), 64, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
+
+template <int FORM>
+static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
+    const LinearPlan p = plan_linear(a.M, a.N, a.K);
+    return p.shape == T256 ? launch_tiles<T256, FORM>(a, p, stream) : launch_tiles<T128, FORM>(a, p, stream);
+}
+
+size_t linear_workspace(uint32_t M, uint32_t N, uint32_t K) { return plan_linear(M, N, K).workspace(); }
 
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream) {
     switch (form) {
