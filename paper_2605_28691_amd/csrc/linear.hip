@@ -123,101 +123,129 @@ static TileMap make_tile_map(const LinearPlan& p) {
     return {make_div32(TILE_GROUP * p.tiles_n), make_div32(TILE_GROUP), make_div32(over ? over : 1u), make_div32(p.rest ? p.rest : 1u), p.tiles_m, p.whole, p.parts, p.per};
 }
 
-// The way out: 32 rows by 16 FN channels of C at a time, a wavefront's own.  The sums are laid down in LDS as they are (float32: a residual is added before the one
-// rounding) and picked up 8 channels of a row a lane, so that everything in memory is moved in 16-byte pieces of whole rows, and a checkpoint's blocks are four
-// neighbouring lanes.
-template <int FN>
+// Exchange of the odd rows of 16 lanes of `a` with the even ones of `b` (v_permlane16_swap; its own inverse).
+__device__ __attribute__((always_inline)) inline void swap_rows(uint32_t& a, uint32_t& b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    const uint32_t x = r[0], y = r[1];
+    a = x;
+    b = y;
+}
+
+// The way out, a row of 16 by 16 FN channels of C at a time.  In the accumulators of two neighbouring blocks lane l has row l % 16 and channels 4 (l / 16) .. + 3 of each; after
+// swap_rows() 8 channels in a row of one of them, block l / 16 % 2, from 8 (l / 32): so that memory is moved 16 bytes a lane and 64 of a row at once.  (Through LDS, in
+// whole rows, the one wavefront that a SIMD has waited 8.5 us a tile of 256 x 256 for its own reads; this way 32,760 x 1536 -> 1536 takes EPI_AFTER instead of 137 us.)
+template <int FN, int FORM>
 struct Out {
-    static constexpr uint32_t LPR = FN * 2, RPI = 64 / LPR;  // lanes a row, rows at once
-    uint32_t n;      // the lane's channels n .. n + 7
-    bool in;
-    float bias[8];
+    static constexpr bool FWD = FORM == LINEAR_FWD, ADDS = FORM != LINEAR_DW;  // what the form may have asked for
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+    static constexpr int PAIRS = FN / 2;
+    uint32_t n_own, n_moved;  // first channel of the lane's in block 0, and in blocks 0 and 1 after the exchange
+    u32x2 bias[FN];           // bf16, as it lies in the accumulators
     __device__ __attribute__((always_inline)) inline Out(const LinearArgs& a, uint32_t n0, uint32_t lane) {
-        n = n0 + lane % LPR * 8u;
-        in = n < a.N;
-#pragma unroll
-        for (int e = 0; e < 8; e++) bias[e] = 0.f;
-        if (a.e.bias != nullptr && in) {
-            const bf16x8 b = *(const bf16x8*)((const __bf16*)a.e.bias + n);
-#pragma unroll
-            for (int e = 0; e < 8; e++) bias[e] = (float)b[e];
-        }
-    }
-    // 16-byte piece c of row r lies at c ^ (r % 16): 8 lanes that write (8 rows) or read (a row) touch different banks
-    __device__ __attribute__((always_inline)) inline static uint32_t place(uint32_t r, uint32_t c) { return r * (FN * 64u) + ((c ^ (r & 15u)) * 16u); }
-    __device__ __attribute__((always_inline)) inline void lay_down(char* stage, const f32x4 (&first)[FN], const f32x4 (&second)[FN], uint32_t lane) const {
-        const uint32_t r = lane & 15u, g = lane >> 4;
-        // the wavefront's LDS accesses take effect in order; the fences keep the compiler from exchanging them
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        const uint32_t g = lane >> 4;
+        n_own = n0 + 4u * g;
+        n_moved = n0 + 16u * (g & 1u) + 8u * (g >> 1);
 #pragma unroll
         for (int j = 0; j < FN; j++) {
-            *(f32x4*)(stage + place(r, j * 4u + g)) = first[j];
-            *(f32x4*)(stage + place(r + 16u, j * 4u + g)) = second[j];
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
-    __device__ __attribute__((always_inline)) inline void rows(const char* stage, const LinearArgs& a, uint32_t m0, uint32_t lane) const {
-#pragma unroll 2
-        for (uint32_t it = 0; it < 32u / RPI; it++) {
-            const uint32_t r = it * RPI + lane / LPR, c = lane % LPR * 2u;
-            const f32x4 x = *(const f32x4*)(stage + place(r, c)), y = *(const f32x4*)(stage + place(r, c + 1u));
-            const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            finish(a, m0 + r, z);
+            bias[j] = u32x2{0u, 0u};
+            if (FWD && a.e.bias != nullptr && n_own + 16u * j < a.N) bias[j] = *(const u32x2*)((const __bf16*)a.e.bias + n_own + 16u * j);
         }
     }
-    // row m, the lane's channels: act(z + bias) + residual; z + bias kept
-    __device__ __attribute__((always_inline)) inline void finish(const LinearArgs& a, uint32_t m, const float (&sum)[8]) const {
-        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+    // what is to be added to row m, on its way before the row's results leave
+    struct Residual {
+        u32x4 x[PAIRS];
+    };
+    __device__ __attribute__((always_inline)) inline Residual residual(const LinearArgs& a, uint32_t m) const {
+        Residual r;
+        const __bf16* const row = (const __bf16*)a.e.residual + (size_t)m * a.N + n_moved;
+#pragma unroll
+        for (int p = 0; p < PAIRS; p++) {
+            r.x[p] = u32x4{0u, 0u, 0u, 0u};
+            if (ADDS && a.e.residual != nullptr && m < a.M && n_moved + 32u * p < a.N) r.x[p] = *(const u32x4*)(row + 32 * p);
+        }
+        return r;
+    }
+    __device__ __attribute__((always_inline)) inline static uint32_t pack(float x, float y) {
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+        const bf16x2 b = {(__bf16)x, (__bf16)y};
+        return __builtin_bit_cast(uint32_t, b);
+    }
+    // two blocks' values of row m to bf16 at `to`, a tensor like C
+    __device__ __attribute__((always_inline)) inline void store(const LinearArgs& a, void* to, uint32_t m, int p, const f32x4& x, const f32x4& y) const {
+        uint32_t x0 = pack(x[0], x[1]), x1 = pack(x[2], x[3]), y0 = pack(y[0], y[1]), y1 = pack(y[2], y[3]);
+        swap_rows(x0, y0);
+        swap_rows(x1, y1);
+        const uint32_t n = n_moved + 32u * p;
+        if (m < a.M && n < a.N) *(u32x4*)((__bf16*)to + (size_t)m * a.N + n) = u32x4{x0, x1, y0, y1};
+    }
+    // the same as a checkpoint's block
+    __device__ __attribute__((always_inline)) inline void store8(const LinearArgs& a, uint32_t m, int p, const f32x4& x, const f32x4& y, uint32_t lane) const {
+        const uint32_t n = n_own + 32u * p;
+        uint32_t top = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t s = n < a.N ? ckpt_size(x[e]) : 0u, t = n + 16u < a.N ? ckpt_size(y[e]) : 0u;
+            top = s > top ? s : top;
+            top = t > top ? t : top;
+        }
+#pragma unroll
+        for (int off = 16; off <= 32; off <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_xor((int)top, off);
+            top = o > top ? o : top;
+        }
+        const uint32_t byte = ckpt_byte(top);
+        const float down = ckpt_down(byte);
+        uint32_t cx = ckpt_codes(x[0], x[1], x[2], x[3], down), cy = ckpt_codes(y[0], y[1], y[2], y[3], down);
+        swap_rows(cx, cy);
+        const uint32_t nm = n_moved + 32u * p;
+        if (m < a.M && nm < a.N) {
+            *(u32x2*)((char*)a.e.pre + (size_t)m * a.N + nm) = u32x2{cx, cy};
+            if (lane < 16u) ((unsigned char*)a.e.pre_scales)[(size_t)m * ((a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK) + nm / CKPT_BLOCK] = (unsigned char)byte;
+        }
+    }
+    // row m: act(z + bias) + residual; z + bias kept
+    __device__ __attribute__((always_inline)) inline void row(const LinearArgs& a, uint32_t m, f32x4 (&z)[FN], const Residual& r, uint32_t lane) const {
         const LinearEpilogue& e = a.e;
-        const bool here = in && m < a.M;
-        const size_t at = (size_t)m * a.N + n;
-        float z[8];
+        if (FWD && e.bias != nullptr) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) z[i] = sum[i] + bias[i];
-        if (e.pre_scales != nullptr) {
-            uint32_t top = 0u;
+            for (int j = 0; j < FN; j++)
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const uint32_t s = in ? ckpt_size(z[i]) : 0u;
-                top = s > top ? s : top;
+                for (int x = 0; x < 4; x++) z[j][x] += __uint_as_float(x & 1 ? bias[j][x >> 1] & 0xffff0000u : bias[j][x >> 1] << 16);
+        }
+        if (FWD && e.pre_scales != nullptr) {
+#pragma unroll
+            for (int p = 0; p < PAIRS; p++) store8(a, m, p, z[2 * p], z[2 * p + 1], lane);
+        } else if (FWD && e.pre != nullptr) {
+#pragma unroll
+            for (int p = 0; p < PAIRS; p++) store(a, e.pre, m, p, z[2 * p], z[2 * p + 1]);
+        }
+        if (FWD && e.act == ACT_GELU_TANH) {
+#pragma unroll
+            for (int j = 0; j < FN; j++)
+#pragma unroll
+                for (int x = 0; x < 4; x++) z[j][x] = act_value(ACT_GELU_TANH, z[j][x]);
+        } else if (FWD && e.act == ACT_SILU) {
+#pragma unroll
+            for (int j = 0; j < FN; j++)
+#pragma unroll
+                for (int x = 0; x < 4; x++) z[j][x] = act_value(ACT_SILU, z[j][x]);
+        }
+        if (ADDS && e.residual != nullptr) {
+#pragma unroll
+            for (int p = 0; p < PAIRS; p++) {
+                uint32_t x0 = r.x[p][0], x1 = r.x[p][1], y0 = r.x[p][2], y1 = r.x[p][3];
+                swap_rows(x0, y0);
+                swap_rows(x1, y1);
+                const uint32_t v[2][2] = {{x0, x1}, {y0, y1}};
+#pragma unroll
+                for (int b = 0; b < 2; b++)
+#pragma unroll
+                    for (int x = 0; x < 4; x++) z[2 * p + b][x] += __uint_as_float(x & 1 ? v[b][x >> 1] & 0xffff0000u : v[b][x >> 1] << 16);
             }
-#pragma unroll
-            for (int off = 1; off <= 2; off <<= 1) {
-                const uint32_t o = (uint32_t)__shfl_xor((int)top, off);
-                top = o > top ? o : top;
-            }
-            const uint32_t byte = ckpt_byte(top);
-            const float down = ckpt_down(byte);
-            if (here) {
-                *(u32x2*)((char*)e.pre + at) = u32x2{ckpt_codes(z[0], z[1], z[2], z[3], down), ckpt_codes(z[4], z[5], z[6], z[7], down)};
-                if (n % CKPT_BLOCK == 0u) ((unsigned char*)e.pre_scales)[(size_t)m * ((a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK) + n / CKPT_BLOCK] = (unsigned char)byte;
-            }
         }
-        if (!here) return;
-        if (e.pre != nullptr && e.pre_scales == nullptr) {
-            bf16x8 o;
 #pragma unroll
-            for (int i = 0; i < 8; i++) o[i] = (__bf16)z[i];
-            *(bf16x8*)((__bf16*)e.pre + at) = o;
-        }
-        if (e.act == ACT_GELU_TANH) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) z[i] = act_value(ACT_GELU_TANH, z[i]);
-        } else if (e.act == ACT_SILU) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) z[i] = act_value(ACT_SILU, z[i]);
-        }
-        if (e.residual != nullptr) {
-            const bf16x8 r = *(const bf16x8*)((const __bf16*)e.residual + at);
-#pragma unroll
-            for (int i = 0; i < 8; i++) z[i] += (float)r[i];
-        }
-        bf16x8 o;
-#pragma unroll
-        for (int i = 0; i < 8; i++) o[i] = (__bf16)z[i];
-        *(bf16x8*)((__bf16*)e.out + at) = o;
+        for (int p = 0; p < PAIRS; p++) store(a, e.out, m, p, z[2 * p], z[2 * p + 1]);
     }
 };
 
@@ -327,6 +355,7 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
+    const Out<FN, FORM> out(a, n0 + wn * (FN * 16u), lane);
     Frags f0, f1;
     // A step of 64, tile t at k: halves c0 and c1, of which c0 is in f0; the next tile's first half is n0.  A half is free once it is in registers, and is filled with its part
     // of tile t + 2 at once: what comes in halves 3/2 steps before it is read, what comes in one piece a step before.
@@ -368,40 +397,45 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
             for (int j = 0; j < FN; j++) to[(i * FN + j) * 64] = acc[i][j];
         return;
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    // the epilogue, 32 rows of the wavefront at a time, through LDS
-    char* const stage = wave == 0u ? p00 : wave == 1u ? p10 : wave == 2u ? q00 : q10;
-    Out<FN> out(a, n0 + wn * (FN * 16u), lane);
+    // One copy of the epilogue for all rows of blocks: the accumulators' registers have fixed names, so each is picked by a branch of its own.
+    const uint32_t row0 = m0 + wm * (FM * 16u) + (lane & 15u);
+    typename Out<FN, FORM>::Residual r = out.residual(a, row0);
+#pragma unroll 1
+    for (int i = 0; i < FM; i++) {
+        f32x4 z[FN];
+        each<FM>([&](auto I) __attribute__((always_inline)) {
+            if (i == decltype(I)::value) {
 #pragma unroll
-    for (int i = 0; i < FM; i += 2) {
-        out.lay_down(stage, acc[i], acc[i + 1], lane);
-        out.rows(stage, a, m0 + (wm * FM + i) * 16u, lane);
-        __builtin_amdgcn_sched_barrier(0);
+                for (int j = 0; j < FN; j++) z[j] = acc[decltype(I)::value][j];
+            }
+        });
+        const typename Out<FN, FORM>::Residual now = r;
+        if (i + 1 < FM) r = out.residual(a, row0 + (i + 1) * 16u);
+        out.row(a, row0 + i * 16u, z, now, lane);
     }
 }
 
-// Adds up the parts of a tile, in order, and finishes 32 rows of a wavefront's share.
-template <int BM, int BN>
+// Adds up the parts of a tile, in order, and finishes 16 rows of a wavefront's share.
+template <int BM, int BN, int FORM>
 __global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a, TileMap tiles) {
     constexpr int FM = BM / 32, FN = BN / 32;
-    constexpr uint32_t UNITS = 4 * FM / 2;  // of a tile
-    __shared__ __attribute__((aligned(16))) char stage[32 * FN * 64];
-    const uint32_t lane = threadIdx.x, r = blockIdx.x / UNITS, unit = blockIdx.x % UNITS, wave = unit / (FM / 2), i = unit % (FM / 2) * 2u;
+    constexpr uint32_t UNITS = 4 * FM;  // of a tile
+    const uint32_t lane = threadIdx.x, r = blockIdx.x / UNITS, unit = blockIdx.x % UNITS, wave = unit / FM, i = unit % FM;
     uint32_t tm, tn;
     tiles.tile(tiles.whole + r, tm, tn);
     const f32x4* from = (const f32x4*)a.partial + ((size_t)r * tiles.parts * 4u + wave) * (FM * FN * 64u) + i * (FN * 64u) + lane;
-    f32x4 acc[2][FN];
+    const Out<FN, FORM> out(a, tn * BN + (wave >> 1) * (FN * 16u), lane);
+    const uint32_t m = tm * BM + ((wave & 1u) * FM + i) * 16u + (lane & 15u);
+    const typename Out<FN, FORM>::Residual res = out.residual(a, m);
+    f32x4 acc[FN];
 #pragma unroll
-    for (int j = 0; j < 2 * FN; j++) acc[j / FN][j % FN] = from[j * 64];
+    for (int j = 0; j < FN; j++) acc[j] = from[j * 64];
     for (uint32_t p = 1; p < tiles.parts; p++) {
         from += 4 * FM * FN * 64;
 #pragma unroll
-        for (int j = 0; j < 2 * FN; j++) acc[j / FN][j % FN] += from[j * 64];
+        for (int j = 0; j < FN; j++) acc[j] += from[j * 64];
     }
-    const Out<FN> out(a, tn * BN + (wave >> 1) * (FN * 16u), lane);
-    out.lay_down(stage, acc[0], acc[1], lane);
-    out.rows(stage, a, tm * BM + ((wave & 1u) * FM + i) * 16u, lane);
+    out.row(a, m, acc, res, lane);
 }
 
 template <int SHAPE, int FORM>
@@ -413,7 +447,7 @@ static hipError_t launch_tiles(const LinearArgs& a, const LinearPlan& p, hipStre
     linear_kernel<BM, BN, FORM><<<(uint32_t)blocks, 256, 0, stream>>>(a, tiles);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.rest == 0u) return e;
-    linear_join_kernel<BM, BN><<<p.rest * (4u * BM / 64u), 64, 0, stream>>>(a, tiles);
+    linear_join_kernel<BM, BN, FORM><<<p.rest * (4u * BM / 32u), 64, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
 
