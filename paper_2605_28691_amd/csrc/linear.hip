@@ -132,38 +132,55 @@ __device__ __attribute__((always_inline)) inline void swap_rows(uint32_t& a, uin
 }
 
 // The way out, a row of 16 by 16 FN channels of C at a time.  In the accumulators of two neighbouring blocks lane l has row l % 16 and channels 4 (l / 16) .. + 3 of each; after
-// swap_rows() 8 channels in a row of one of them, block l / 16 % 2, from 8 (l / 32): so that memory is moved 16 bytes a lane and 64 of a row at once.  (Through LDS, in
-// whole rows, the one wavefront that a SIMD has waited 8.5 us a tile of 256 x 256 for its own reads; this way 32,760 x 1536 -> 1536 takes EPI_AFTER instead of 137 us.)
-template <int FN, int FORM>
+// swap_rows() 8 channels in a row of one of them, block l / 16 % 2, from 8 (l / 32): so that memory is moved 16 bytes a lane and 64 of a row at once.  The one wavefront that a
+// SIMD has issues an instruction in five clocks, so it is their number that costs: addresses are offsets in buffers, which drop what lies behind the last row, and a channel behind
+// the last one has an offset behind every buffer.  (32,760 x 1536 -> 1536: through LDS in whole rows 137 us, this way with 64-bit addresses and tests 134, without any
+// epilogue 106.)
+template <int FN, int FORM, bool EXTRAS>
 struct Out {
-    static constexpr bool FWD = FORM == LINEAR_FWD, ADDS = FORM != LINEAR_DW;  // what the form may have asked for
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
     typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
     static constexpr int PAIRS = FN / 2;
-    uint32_t n_own, n_moved;  // first channel of the lane's in block 0, and in blocks 0 and 1 after the exchange
-    u32x2 bias[FN];           // bf16, as it lies in the accumulators
-    __device__ __attribute__((always_inline)) inline Out(const LinearArgs& a, uint32_t n0, uint32_t lane) {
-        const uint32_t g = lane >> 4;
-        n_own = n0 + 4u * g;
-        n_moved = n0 + 16u * (g & 1u) + 8u * (g >> 1);
+    static constexpr bool FWD = FORM == LINEAR_FWD, KEEPS = FWD && EXTRAS, ADDS = FORM == LINEAR_DX || KEEPS;  // what may have been asked for
+    static constexpr uint32_t OUTSIDE = 0x80000000u;  // 128 rows are less: N < 2^23; no sum with a row's offset passes 2^32
+    uint32_t n0, row0, rows;   // the wavefront's first channel and row; rows from there on, at most 128
+    uint32_t at[PAIRS];        // bytes, in bf16, from the wavefront's first row to the lane's 8 channels of row l % 16
+    __device__ __attribute__((always_inline)) inline Out(const LinearArgs& a, uint32_t m, uint32_t n, uint32_t lane) {
+        n0 = n;
+        row0 = m;
+        rows = m >= a.M ? 0u : a.M - m < 128u ? a.M - m : 128u;
 #pragma unroll
-        for (int j = 0; j < FN; j++) {
-            bias[j] = u32x2{0u, 0u};
-            if (FWD && a.e.bias != nullptr && n_own + 16u * j < a.N) bias[j] = *(const u32x2*)((const __bf16*)a.e.bias + n_own + 16u * j);
+        for (int p = 0; p < PAIRS; p++) {
+            const uint32_t g = lane >> 4, c = n + 32u * p + 16u * (g & 1u) + 8u * (g >> 1);
+            at[p] = c < a.N ? ((lane & 15u) * a.N + c) * 2u : OUTSIDE;
         }
     }
-    // what is to be added to row m, on its way before the row's results leave
+    // bias of the lane's channels of block j, as they lie in the accumulators
+    __device__ __attribute__((always_inline)) inline static f32x4 bias(const LinearArgs& a, uint32_t n0, int j, uint32_t lane) {
+        f32x4 b = {0.f, 0.f, 0.f, 0.f};
+        const uint32_t n = n0 + 16u * j + 4u * (lane >> 4);
+        if (FWD && a.e.bias != nullptr && n < a.N) {
+            const bf16x4 x = *(const bf16x4*)((const __bf16*)a.e.bias + n);
+#pragma unroll
+            for (int e = 0; e < 4; e++) b[e] = (float)x[e];
+        }
+        return b;
+    }
+    // what is to be added to rows 16 i .., on its way before their results leave
     struct Residual {
         u32x4 x[PAIRS];
     };
-    __device__ __attribute__((always_inline)) inline Residual residual(const LinearArgs& a, uint32_t m) const {
+    __device__ __attribute__((always_inline)) inline Residual residual(const LinearArgs& a, uint32_t i) const {
         Residual r;
-        const __bf16* const row = (const __bf16*)a.e.residual + (size_t)m * a.N + n_moved;
 #pragma unroll
-        for (int p = 0; p < PAIRS; p++) {
-            r.x[p] = u32x4{0u, 0u, 0u, 0u};
-            if (ADDS && a.e.residual != nullptr && m < a.M && n_moved + 32u * p < a.N) r.x[p] = *(const u32x4*)(row + 32 * p);
+        for (int p = 0; p < PAIRS; p++) r.x[p] = u32x4{0u, 0u, 0u, 0u};
+#if defined(__HIP_DEVICE_COMPILE__)
+        if (ADDS && a.e.residual != nullptr) {
+            const auto from = __builtin_amdgcn_make_buffer_rsrc((char*)a.e.residual + (size_t)row0 * a.N * 2u, 0, rows * a.N * 2u, 0x27000);
+#pragma unroll
+            for (int p = 0; p < PAIRS; p++) r.x[p] = __builtin_amdgcn_raw_buffer_load_b128(from, at[p] + i * 32u * a.N, 0, 0);
         }
+#endif
         return r;
     }
     __device__ __attribute__((always_inline)) inline static uint32_t pack(float x, float y) {
@@ -171,61 +188,63 @@ struct Out {
         const bf16x2 b = {(__bf16)x, (__bf16)y};
         return __builtin_bit_cast(uint32_t, b);
     }
-    // two blocks' values of row m to bf16 at `to`, a tensor like C
-    __device__ __attribute__((always_inline)) inline void store(const LinearArgs& a, void* to, uint32_t m, int p, const f32x4& x, const f32x4& y) const {
-        uint32_t x0 = pack(x[0], x[1]), x1 = pack(x[2], x[3]), y0 = pack(y[0], y[1]), y1 = pack(y[2], y[3]);
-        swap_rows(x0, y0);
-        swap_rows(x1, y1);
-        const uint32_t n = n_moved + 32u * p;
-        if (m < a.M && n < a.N) *(u32x4*)((__bf16*)to + (size_t)m * a.N + n) = u32x4{x0, x1, y0, y1};
-    }
-    // the same as a checkpoint's block
-    __device__ __attribute__((always_inline)) inline void store8(const LinearArgs& a, uint32_t m, int p, const f32x4& x, const f32x4& y, uint32_t lane) const {
-        const uint32_t n = n_own + 32u * p;
-        uint32_t top = 0u;
+    // rows 16 i .. in bf16 to a tensor like C
+    __device__ __attribute__((always_inline)) inline void store(const LinearArgs& a, void* tensor, uint32_t i, const f32x4 (&z)[FN]) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const auto to = __builtin_amdgcn_make_buffer_rsrc((char*)tensor + (size_t)row0 * a.N * 2u, 0, rows * a.N * 2u, 0x27000);
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const uint32_t s = n < a.N ? ckpt_size(x[e]) : 0u, t = n + 16u < a.N ? ckpt_size(y[e]) : 0u;
-            top = s > top ? s : top;
-            top = t > top ? t : top;
+        for (int p = 0; p < PAIRS; p++) {
+            const f32x4 &x = z[2 * p], &y = z[2 * p + 1];
+            uint32_t x0 = pack(x[0], x[1]), x1 = pack(x[2], x[3]), y0 = pack(y[0], y[1]), y1 = pack(y[2], y[3]);
+            swap_rows(x0, y0);
+            swap_rows(x1, y1);
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{x0, x1, y0, y1}, to, at[p] + i * 32u * a.N, 0, 0);
         }
-#pragma unroll
-        for (int off = 16; off <= 32; off <<= 1) {
-            const uint32_t o = (uint32_t)__shfl_xor((int)top, off);
-            top = o > top ? o : top;
-        }
-        const uint32_t byte = ckpt_byte(top);
-        const float down = ckpt_down(byte);
-        uint32_t cx = ckpt_codes(x[0], x[1], x[2], x[3], down), cy = ckpt_codes(y[0], y[1], y[2], y[3], down);
-        swap_rows(cx, cy);
-        const uint32_t nm = n_moved + 32u * p;
-        if (m < a.M && nm < a.N) {
-            *(u32x2*)((char*)a.e.pre + (size_t)m * a.N + nm) = u32x2{cx, cy};
-            if (lane < 16u) ((unsigned char*)a.e.pre_scales)[(size_t)m * ((a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK) + nm / CKPT_BLOCK] = (unsigned char)byte;
-        }
+#endif
     }
-    // row m: act(z + bias) + residual; z + bias kept
-    __device__ __attribute__((always_inline)) inline void row(const LinearArgs& a, uint32_t m, f32x4 (&z)[FN], const Residual& r, uint32_t lane) const {
+    // the same as blocks of a checkpoint
+    __device__ __attribute__((always_inline)) inline void store8(const LinearArgs& a, uint32_t i, const f32x4 (&z)[FN], uint32_t lane) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const auto to = __builtin_amdgcn_make_buffer_rsrc((char*)a.e.pre + (size_t)row0 * a.N, 0, rows * a.N, 0x27000);
+        const uint32_t blocks = (a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK;
+        const auto scales = __builtin_amdgcn_make_buffer_rsrc((char*)a.e.pre_scales + (size_t)row0 * blocks, 0, rows * blocks, 0x27000);
+#pragma unroll
+        for (int p = 0; p < PAIRS; p++) {
+            const f32x4 &x = z[2 * p], &y = z[2 * p + 1];
+            const uint32_t n = n0 + 32u * p + 4u * (lane >> 4);
+            uint32_t top = 0u;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const uint32_t s = n < a.N ? ckpt_size(x[e]) : 0u, t = n + 16u < a.N ? ckpt_size(y[e]) : 0u;
+                top = s > top ? s : top;
+                top = t > top ? t : top;
+            }
+#pragma unroll
+            for (int off = 16; off <= 32; off <<= 1) {
+                const uint32_t o = (uint32_t)__shfl_xor((int)top, off);
+                top = o > top ? o : top;
+            }
+            const uint32_t byte = ckpt_byte(top);
+            const float down = ckpt_down(byte);
+            uint32_t cx = ckpt_codes(x[0], x[1], x[2], x[3], down), cy = ckpt_codes(y[0], y[1], y[2], y[3], down);
+            swap_rows(cx, cy);
+            __builtin_amdgcn_raw_buffer_store_b64(u32x2{cx, cy}, to, (at[p] >> 1) + i * 16u * a.N, 0, 0);
+            const uint32_t block = n0 / CKPT_BLOCK + p;
+            __builtin_amdgcn_raw_buffer_store_b8((unsigned char)byte, scales, lane < 16u && block < blocks ? (16u * i + lane) * blocks + block : OUTSIDE, 0, 0);
+        }
+#endif
+    }
+    // rows 16 i ..: act(z) + residual, z kept
+    __device__ __attribute__((always_inline)) inline void row(const LinearArgs& a, uint32_t i, f32x4 (&z)[FN], const Residual& r, uint32_t lane) const {
         const LinearEpilogue& e = a.e;
-        if (FWD && e.bias != nullptr) {
-#pragma unroll
-            for (int j = 0; j < FN; j++)
-#pragma unroll
-                for (int x = 0; x < 4; x++) z[j][x] += __uint_as_float(x & 1 ? bias[j][x >> 1] & 0xffff0000u : bias[j][x >> 1] << 16);
-        }
-        if (FWD && e.pre_scales != nullptr) {
-#pragma unroll
-            for (int p = 0; p < PAIRS; p++) store8(a, m, p, z[2 * p], z[2 * p + 1], lane);
-        } else if (FWD && e.pre != nullptr) {
-#pragma unroll
-            for (int p = 0; p < PAIRS; p++) store(a, e.pre, m, p, z[2 * p], z[2 * p + 1]);
-        }
-        if (FWD && e.act == ACT_GELU_TANH) {
+        if (KEEPS && e.pre_scales != nullptr) store8(a, i, z, lane);
+        else if (KEEPS && e.pre != nullptr) store(a, e.pre, i, z);
+        if (KEEPS && e.act == ACT_GELU_TANH) {
 #pragma unroll
             for (int j = 0; j < FN; j++)
 #pragma unroll
                 for (int x = 0; x < 4; x++) z[j][x] = act_value(ACT_GELU_TANH, z[j][x]);
-        } else if (FWD && e.act == ACT_SILU) {
+        } else if (KEEPS && e.act == ACT_SILU) {
 #pragma unroll
             for (int j = 0; j < FN; j++)
 #pragma unroll
@@ -244,10 +263,18 @@ struct Out {
                     for (int x = 0; x < 4; x++) z[2 * p + b][x] += __uint_as_float(x & 1 ? v[b][x >> 1] & 0xffff0000u : v[b][x >> 1] << 16);
             }
         }
-#pragma unroll
-        for (int p = 0; p < PAIRS; p++) store(a, e.out, m, p, z[2 * p], z[2 * p + 1]);
+        store(a, e.out, i, z);
     }
 };
+
+// Accumulators from their registers.  In asm as the products are, so that none is read before the wait behind the last of these: the compiler, which does not know of it, would
+// take all of them at once, and put some aside in memory in front of the wait.
+__device__ __attribute__((always_inline)) inline f32x4 take(const f32x4& acc) {
+    float a = acc[0], b = acc[1], c = acc[2], d = acc[3], w, x, y, z;
+    asm volatile("v_accvgpr_read_b32 %0, %4\n\tv_accvgpr_read_b32 %1, %5\n\tv_accvgpr_read_b32 %2, %6\n\tv_accvgpr_read_b32 %3, %7"
+                 : "=&v"(w), "=&v"(x), "=&v"(y), "=&v"(z) : "a"(a), "a"(b), "a"(c), "a"(d));
+    return f32x4{w, x, y, z};
+}
 
 template <int N>
 using Int = std::integral_constant<int, N>;
@@ -261,7 +288,7 @@ __device__ __attribute__((always_inline)) inline void each(F f) {
     each(std::make_integer_sequence<int, N>{}, f);
 }
 
-template <int BM, int BN, int FORM>
+template <int BM, int BN, int FORM, bool EXTRAS>
 __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kernel(LinearArgs a, TileMap tiles) {
     constexpr bool PT = FORM == LINEAR_DW, QT = FORM != LINEAR_FWD;
     constexpr int NW = 4, FM = BM / 32, FN = BN / 32;  // wavefronts 2 x 2; blocks of 16 that each has
@@ -305,11 +332,13 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
     auto step_at = [&](uint32_t k) __attribute__((always_inline)) -> Step {
         return {p0 + (PT ? (size_t)k * ldp : (size_t)k * 2u), q0 + (QT ? (size_t)k * ldq : (size_t)k * 2u), records(PT, k, ldp, m0), records(QT, k, ldq, n0), k < k1 ? k1 - k : 0u};
     };
-    f32x4 acc[FM][FN];
+    f32x4 acc[FM][FN];  // sums begin with the bias; those of a part with 0
 #pragma unroll
-    for (int i = 0; i < FM; i++)
+    for (int j = 0; j < FN; j++) {
+        const f32x4 b = slot == ~0u ? Out<FN, FORM, EXTRAS>::bias(a, n0 + wn * (FN * 16u), j, lane) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < FN; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < FM; i++) acc[i][j] = b;
+    }
     struct Frags {
         bf16x8 p[FM], q[FN];
     };
@@ -355,7 +384,6 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
-    const Out<FN, FORM> out(a, n0 + wn * (FN * 16u), lane);
     Frags f0, f1;
     // A step of 64, tile t at k: halves c0 and c1, of which c0 is in f0; the next tile's first half is n0.  A half is free once it is in registers, and is filled with its part
     // of tile t + 2 at once: what comes in halves 3/2 steps before it is read, what comes in one piece a step before.
@@ -381,42 +409,44 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
 #pragma unroll
     for (int i = 0; i < RD; i++) fragment(f0, h00, i);
     if (LOADS_A) meet(Int<LOADS_A + LOADS_B>{});
-    for (uint32_t k = k0; k < k1; k += 2u * LIN_KT) {  // a second step behind the end adds zeros
+    uint32_t k = k0;  // below k1
+    do {              // a second step behind the end adds zeros
         step(k, h00, h01, h10);
         step(k + LIN_KT, h10, h11, h00);
-    }
-    // The products are written as asm, with their accumulators pinned to accumulation registers: left to choose, the compiler moved 200 of them in and out a step.  It does not
-    // see their latency then: the last ones are waited for here.
-    asm volatile("s_nop 15\n\ts_nop 15\n\ts_waitcnt vmcnt(0)" ::: "memory");  // loads behind the end still write (zeros) to LDS
+        // The products are written as asm, with their accumulators pinned to accumulation registers: left to choose, the compiler moved 200 of them in and out a step.  It does not
+        // see their latency then (4 passes, so 7 clocks until a result may be read): the last ones are waited for here, in front of all that may follow.
+        asm volatile("s_nop 15" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        k += 2u * LIN_KT;
+    } while (k < k1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads behind the end still write (zeros) to LDS
     __builtin_amdgcn_sched_barrier(0);
     if (slot != ~0u) {  // a part: sums as they lie in the registers, for linear_join_kernel
         f32x4* const to = (f32x4*)a.partial + ((size_t)slot * 4u + wave) * (FM * FN * 64u) + lane;
 #pragma unroll
         for (int i = 0; i < FM; i++)
 #pragma unroll
-            for (int j = 0; j < FN; j++) to[(i * FN + j) * 64] = acc[i][j];
+            for (int j = 0; j < FN; j++) to[(i * FN + j) * 64] = take(acc[i][j]);
         return;
     }
-    // One copy of the epilogue for all rows of blocks: the accumulators' registers have fixed names, so each is picked by a branch of its own.
-    const uint32_t row0 = m0 + wm * (FM * 16u) + (lane & 15u);
-    typename Out<FN, FORM>::Residual r = out.residual(a, row0);
-#pragma unroll 1
-    for (int i = 0; i < FM; i++) {
+    uint32_t own = lane;
+    asm volatile("" : "+v"(own));  // formed here: else what follows from it is kept in registers through the whole walk
+    const Out<FN, FORM, EXTRAS> out(a, m0 + wm * (FM * 16u), n0 + wn * (FN * 16u), own);
+    typename Out<FN, FORM, EXTRAS>::Residual r = out.residual(a, 0);
+    each<FM>([&](auto I) __attribute__((always_inline)) {
+        constexpr int i = decltype(I)::value;
+        const typename Out<FN, FORM, EXTRAS>::Residual now = r;
+        if (i + 1 < FM) r = out.residual(a, i + 1);
         f32x4 z[FN];
-        each<FM>([&](auto I) __attribute__((always_inline)) {
-            if (i == decltype(I)::value) {
 #pragma unroll
-                for (int j = 0; j < FN; j++) z[j] = acc[decltype(I)::value][j];
-            }
-        });
-        const typename Out<FN, FORM>::Residual now = r;
-        if (i + 1 < FM) r = out.residual(a, row0 + (i + 1) * 16u);
-        out.row(a, row0 + i * 16u, z, now, lane);
-    }
+        for (int j = 0; j < FN; j++) z[j] = take(acc[i][j]);
+        out.row(a, i, z, now, own);
+        __builtin_amdgcn_sched_barrier(0);
+    });
 }
 
 // Adds up the parts of a tile, in order, and finishes 16 rows of a wavefront's share.
-template <int BM, int BN, int FORM>
+template <int BM, int BN, int FORM, bool EXTRAS>
 __global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a, TileMap tiles) {
     constexpr int FM = BM / 32, FN = BN / 32;
     constexpr uint32_t UNITS = 4 * FM;  // of a tile
@@ -424,44 +454,44 @@ __global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a, TileMap t
     uint32_t tm, tn;
     tiles.tile(tiles.whole + r, tm, tn);
     const f32x4* from = (const f32x4*)a.partial + ((size_t)r * tiles.parts * 4u + wave) * (FM * FN * 64u) + i * (FN * 64u) + lane;
-    const Out<FN, FORM> out(a, tn * BN + (wave >> 1) * (FN * 16u), lane);
-    const uint32_t m = tm * BM + ((wave & 1u) * FM + i) * 16u + (lane & 15u);
-    const typename Out<FN, FORM>::Residual res = out.residual(a, m);
+    const Out<FN, FORM, EXTRAS> out(a, tm * BM + (wave & 1u) * (FM * 16u), tn * BN + (wave >> 1) * (FN * 16u), lane);
+    const typename Out<FN, FORM, EXTRAS>::Residual res = out.residual(a, i);
     f32x4 acc[FN];
 #pragma unroll
-    for (int j = 0; j < FN; j++) acc[j] = from[j * 64];
+    for (int j = 0; j < FN; j++) acc[j] = out.bias(a, out.n0, j, lane) + from[j * 64];
     for (uint32_t p = 1; p < tiles.parts; p++) {
         from += 4 * FM * FN * 64;
 #pragma unroll
         for (int j = 0; j < FN; j++) acc[j] += from[j * 64];
     }
-    out.row(a, m, acc, res, lane);
+    out.row(a, i, acc, res, lane);
 }
 
-template <int SHAPE, int FORM>
+// EXTRAS: an activation, a residual, or values to be kept
+template <int SHAPE, int FORM, bool EXTRAS>
 static hipError_t launch_tiles(const LinearArgs& a, const LinearPlan& p, hipStream_t stream) {
     constexpr int BM = LINEAR_TILE[SHAPE].m, BN = LINEAR_TILE[SHAPE].n;
     const uint64_t blocks = (uint64_t)p.whole + (uint64_t)p.rest * p.parts;
     if (!fits_grid(blocks, 256u)) return hipErrorInvalidConfiguration;
     const TileMap tiles = make_tile_map(p);
-    linear_kernel<BM, BN, FORM><<<(uint32_t)blocks, 256, 0, stream>>>(a, tiles);
+    linear_kernel<BM, BN, FORM, EXTRAS><<<(uint32_t)blocks, 256, 0, stream>>>(a, tiles);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.rest == 0u) return e;
-    linear_join_kernel<BM, BN, FORM><<<p.rest * (4u * BM / 32u), 64, 0, stream>>>(a, tiles);
+    linear_join_kernel<BM, BN, FORM, EXTRAS><<<p.rest * (4u * BM / 32u), 64, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
 
-template <int FORM>
+template <int FORM, bool EXTRAS = false>
 static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
     const LinearPlan p = plan_linear(a.M, a.N, a.K);
-    return p.shape == T256 ? launch_tiles<T256, FORM>(a, p, stream) : launch_tiles<T128, FORM>(a, p, stream);
+    return p.shape == T256 ? launch_tiles<T256, FORM, EXTRAS>(a, p, stream) : launch_tiles<T128, FORM, EXTRAS>(a, p, stream);
 }
 
 size_t linear_workspace(uint32_t M, uint32_t N, uint32_t K) { return plan_linear(M, N, K).workspace(); }
 
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream) {
     switch (form) {
-        case LINEAR_FWD: return launch_form<LINEAR_FWD>(a, stream);
+        case LINEAR_FWD: return a.e.act != ACT_NONE || a.e.residual || a.e.pre ? launch_form<LINEAR_FWD, true>(a, stream) : launch_form<LINEAR_FWD>(a, stream);
         case LINEAR_DX: return launch_form<LINEAR_DX>(a, stream);
         default: return launch_form<LINEAR_DW>(a, stream);
     }

@@ -14,18 +14,20 @@ constexpr float GELU_C0 = 0.7978845608028654f, GELU_C1 = 0.044715f;  // sqrt(2 /
 // 1 / (1 + exp(-v)): exp overflows to infinity for v below -88, the quotient is 0 then
 __device__ inline float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.4426950408889634f)); }
 
-// z s without 0 * inf: where v is -inf the product is the limit 0
+// Far out s or s (1 - s) is 0 and so is the product with an infinite z, not 0 * inf: the other factor is kept finite.  (A z that is not a number makes s one that is none.)
+constexpr float ACT_FAR = 3.4028234663852886e38f;
+
 __device__ inline float act_value(int act, float z) {
     if (act == ACT_NONE) return z;
-    const float v = act == ACT_SILU ? z : 2.f * GELU_C0 * (z + GELU_C1 * z * z * z);
-    const float s = sigmoid(v);
-    return s == 0.f ? 0.f * s : z * s;
+    const float v = act == ACT_SILU ? z : z * fmaf(z * z, 2.f * GELU_C0 * GELU_C1, 2.f * GELU_C0);
+    return fmaxf(z, -ACT_FAR) * sigmoid(v);
 }
 __device__ inline float act_slope(int act, float z) {
-    const float v = act == ACT_SILU ? z : 2.f * GELU_C0 * (z + GELU_C1 * z * z * z);
-    const float dv = act == ACT_SILU ? 1.f : 2.f * GELU_C0 * (1.f + 3.f * GELU_C1 * z * z);
+    const float z2 = z * z;
+    const float v = act == ACT_SILU ? z : z * fmaf(z2, 2.f * GELU_C0 * GELU_C1, 2.f * GELU_C0);
+    const float dv = act == ACT_SILU ? 1.f : fmaf(z2, 6.f * GELU_C0 * GELU_C1, 2.f * GELU_C0);
     const float s = sigmoid(v), t = s * (1.f - s);
-    return t == 0.f ? s : s + z * t * dv;  // far out the second term is 0, not 0 * inf
+    return s + t * __builtin_amdgcn_fmed3f(z * dv, -ACT_FAR, ACT_FAR);
 }
 
 }  // namespace skiparse
