@@ -30,11 +30,14 @@ __device__ inline float ckpt_down(uint32_t byte) { return __uint_as_float((254u 
 __device__ inline float ckpt_up(uint32_t byte) { return __uint_as_float(byte == 0u ? 0x00400000u : byte == 255u ? 0x7fc00000u : byte << 23); }
 
 __device__ inline float ckpt_scaled(float x, float down) { return ckpt_size(x) != 0u || x == 0.f ? x * down : __uint_as_float(0x7fc00000u); }
-// four codes
-__device__ inline uint32_t ckpt_codes(float a, float b, float c, float d, float down) {
-    int u = __builtin_amdgcn_cvt_pk_fp8_f32(ckpt_scaled(a, down), ckpt_scaled(b, down), 0, false);
-    u = __builtin_amdgcn_cvt_pk_fp8_f32(ckpt_scaled(c, down), ckpt_scaled(d, down), u, true);
+// four codes of values that are scaled, and finite or NaN
+__device__ inline uint32_t ckpt_codes_of(float a, float b, float c, float d) {
+    int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    u = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, u, true);
     return (uint32_t)u;
+}
+__device__ inline uint32_t ckpt_codes(float a, float b, float c, float d, float down) {
+    return ckpt_codes_of(ckpt_scaled(a, down), ckpt_scaled(b, down), ckpt_scaled(c, down), ckpt_scaled(d, down));
 }
 __device__ inline void ckpt_values(uint32_t codes, float up, float (&v)[4]) {
     const ckpt_f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);

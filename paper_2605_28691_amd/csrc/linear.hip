@@ -33,9 +33,10 @@ constexpr uint32_t LIN_RECORDS = 0xfffffff0u;
 
 // One operand's side of a workgroup's tile: ROWS of m (or n).
 //   !T: a step, 64 of k, in one piece: rows of 128 bytes, whole lines of the caches (64 bytes of a line at a time, 8192^3 took 900 us instead of 846)
-//    T: halves of 32 rows of k, 128 columns (256 bytes) each, which are free and filled again one after the other
+//    T: halves of 32 rows of k, COLS columns each, which are free and filled again one after the other
 template <int ROWS, bool T, int NW>
 struct Side {
+    static constexpr uint32_t COLS = ROWS < 128 ? 64 : 128, LANES = COLS / 8;  // of a row of k in LDS: columns, lanes that fetch it
     static constexpr int INSTR = ROWS * (T ? 64 : 128) / 1024 / NW;  // direct loads of a wavefront and piece, 1 KiB each
     static constexpr int BYTES = ROWS * (T ? 64 : 128);
     uint32_t off[INSTR];   // of the lane's chunk from the piece's base
@@ -51,9 +52,10 @@ struct Side {
                 kofs[i] = ((lane % 8u) ^ lds_swizzle<64>(r)) * 8u;
                 off[i] = row_off(r) + kofs[i] * 2u;
             } else {
-                const uint32_t part = n / 8u, r = n % 8u * 4u + lane / 16u;  // 128 columns a part
+                constexpr uint32_t PER = 64 / LANES;  // rows at once
+                const uint32_t part = n / (32u / PER), r = n % (32u / PER) * PER + lane / LANES;
                 kofs[i] = 0u;
-                off[i] = r * row_bytes + part * 256u + ((lane % 16u) ^ lds_swizzle<128>(r)) * 16u;
+                off[i] = r * row_bytes + part * (COLS * 2u) + ((lane % LANES) ^ lds_swizzle<COLS>(r)) * 16u;
             }
         }
     }
@@ -66,17 +68,17 @@ struct Side {
 };
 
 // Fragment of 16 rows from `row0` (a multiple of 16) and 32 of k, the step's half `half`: lane l has row l % 16, k = 8 (l / 16) ...  T: `buf` is the half.
-template <bool T>
+template <bool T, uint32_t COLS>
 __device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char* buf, uint32_t row0, uint32_t half, uint32_t lane) {
     const uint32_t li = lane & 15u, g = lane >> 4;
     if (!T) return *(const bf16x8*)(buf + (row0 + li) * 128u + ((4u * half + g) ^ lds_swizzle<64>(li)) * 16u);
-    const char* const part = buf + row0 / 128u * 8192u;
+    const char* const part = buf + row0 / COLS * (COLS * 64u);
     bf16x4 v[2];
 #pragma unroll
     for (uint32_t sec = 0; sec < 2; sec++) {
         const uint32_t r = 8u * g + 4u * sec + (li >> 2);
-        const uint32_t c = row0 % 128u / 8u + ((li & 3u) >> 1);
-        const char* const at = part + r * 256u + ((c ^ lds_swizzle<128>(r)) * 16u) + 8u * (li & 1u);
+        const uint32_t c = row0 % COLS / 8u + ((li & 3u) >> 1);
+        const char* const at = part + r * (COLS * 2u) + ((c ^ lds_swizzle<COLS>(r)) * 16u) + 8u * (li & 1u);
         v[sec] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(LDS_PTR(char))at);
     }
     return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -202,31 +204,35 @@ struct Out {
         }
 #endif
     }
-    // the same as blocks of a checkpoint
-    __device__ __attribute__((always_inline)) inline void store8(const LinearArgs& a, uint32_t i, const f32x4 (&z)[FN], uint32_t lane) const {
+    // the same as blocks of a checkpoint; z is changed where it is not finite or lies behind the last channel
+    __device__ __attribute__((always_inline)) inline void store8(const LinearArgs& a, uint32_t i, f32x4 (&z)[FN], uint32_t lane) const {
 #if defined(__HIP_DEVICE_COMPILE__)
         const auto to = __builtin_amdgcn_make_buffer_rsrc((char*)a.e.pre + (size_t)row0 * a.N, 0, rows * a.N, 0x27000);
         const uint32_t blocks = (a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK;
         const auto scales = __builtin_amdgcn_make_buffer_rsrc((char*)a.e.pre_scales + (size_t)row0 * blocks, 0, rows * blocks, 0x27000);
+        if (n0 + 16u * FN > a.N) {
+#pragma unroll
+            for (int j = 0; j < FN; j++)
+                if (n0 + 16u * j + 4u * (lane >> 4) >= a.N) z[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 #pragma unroll
         for (int p = 0; p < PAIRS; p++) {
             const f32x4 &x = z[2 * p], &y = z[2 * p + 1];
-            const uint32_t n = n0 + 32u * p + 4u * (lane >> 4);
-            uint32_t top = 0u;
+            float top = ckpt_top(x, y);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(top == INFINITY) != 0, 0)) {  // rare, and the same for the wavefront
+                f32x4 u = x, v = y;
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const uint32_t s = n < a.N ? ckpt_size(x[e]) : 0u, t = n + 16u < a.N ? ckpt_size(y[e]) : 0u;
-                top = s > top ? s : top;
-                top = t > top ? t : top;
+                for (int e = 0; e < 4; e++) {
+                    u[e] = __builtin_isinf(u[e]) ? NAN : u[e];
+                    v[e] = __builtin_isinf(v[e]) ? NAN : v[e];
+                }
+                z[2 * p] = u;
+                z[2 * p + 1] = v;
+                top = ckpt_top(u, v);
             }
-#pragma unroll
-            for (int off = 16; off <= 32; off <<= 1) {
-                const uint32_t o = (uint32_t)__shfl_xor((int)top, off);
-                top = o > top ? o : top;
-            }
-            const uint32_t byte = ckpt_byte(top);
+            const uint32_t byte = ckpt_byte(__float_as_uint(top));
             const float down = ckpt_down(byte);
-            uint32_t cx = ckpt_codes(x[0], x[1], x[2], x[3], down), cy = ckpt_codes(y[0], y[1], y[2], y[3], down);
+            uint32_t cx = ckpt_codes_of(x[0] * down, x[1] * down, x[2] * down, x[3] * down), cy = ckpt_codes_of(y[0] * down, y[1] * down, y[2] * down, y[3] * down);
             swap_rows(cx, cy);
             __builtin_amdgcn_raw_buffer_store_b64(u32x2{cx, cy}, to, (at[p] >> 1) + i * 16u * a.N, 0, 0);
             const uint32_t block = n0 / CKPT_BLOCK + p;
@@ -234,11 +240,26 @@ struct Out {
         }
 #endif
     }
+    // the largest |value| of a row's block, not counting what is no number: lanes l, l + 16, l + 32, l + 48 hold it
+    __device__ __attribute__((always_inline)) inline static float ckpt_top(const f32x4& x, const f32x4& y) {
+        auto max3 = [](float u, float v, float w) __attribute__((always_inline)) { return fmaxf(fmaxf(u, v), w); };
+        const float m = max3(max3(fabsf(x[0]), fabsf(x[1]), 0.f), max3(fabsf(x[2]), fabsf(x[3]), fabsf(y[0])), max3(fabsf(y[1]), fabsf(y[2]), fabsf(y[3])));
+        uint32_t u = __float_as_uint(m), v = u;
+        swap_rows(u, v);
+        const float h = fmaxf(__uint_as_float(u), __uint_as_float(v));
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(h), __float_as_uint(h), false, false);
+        const uint32_t r0 = r[0], r1 = r[1];
+        return fmaxf(__uint_as_float(r0), __uint_as_float(r1));
+    }
     // rows 16 i ..: act(z) + residual, z kept
     __device__ __attribute__((always_inline)) inline void row(const LinearArgs& a, uint32_t i, f32x4 (&z)[FN], const Residual& r, uint32_t lane) const {
         const LinearEpilogue& e = a.e;
-        if (KEEPS && e.pre_scales != nullptr) store8(a, i, z, lane);
-        else if (KEEPS && e.pre != nullptr) store(a, e.pre, i, z);
+        if (KEEPS && e.pre_scales != nullptr) {
+            f32x4 kept[FN];
+#pragma unroll
+            for (int j = 0; j < FN; j++) kept[j] = z[j];
+            store8(a, i, kept, lane);
+        } else if (KEEPS && e.pre != nullptr) store(a, e.pre, i, z);
         if (KEEPS && e.act == ACT_GELU_TANH) {
 #pragma unroll
             for (int j = 0; j < FN; j++)
@@ -289,7 +310,7 @@ __device__ __attribute__((always_inline)) inline void each(F f) {
 }
 
 template <int BM, int BN, int FORM, bool EXTRAS>
-__global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kernel(LinearArgs a, TileMap tiles) {
+__global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) == 4 ? 2 : 4) void linear_kernel(LinearArgs a, TileMap tiles) {
     constexpr bool PT = FORM == LINEAR_DW, QT = FORM != LINEAR_FWD;
     constexpr int NW = 4, FM = BM / 32, FN = BN / 32;  // wavefronts 2 x 2; blocks of 16 that each has
     using SP = Side<BM, PT, NW>;
@@ -348,9 +369,9 @@ __global__ __launch_bounds__(256, BM * BN == 256 * 256 ? 1 : 2) void linear_kern
     };
     // fragment i in the order of use: the first of P, all of Q, the others of P
     auto fragment = [&](Frags& f, const Half& from, int i) __attribute__((always_inline)) {
-        if (i == 0) f.p[0] = read_fragment<PT>(from.p, (wm * FM) * 16u, from.n, lane);
-        else if (i <= FN) f.q[i - 1] = read_fragment<QT>(from.q, (wn * FN + i - 1) * 16u, from.n, lane);
-        else f.p[i - FN] = read_fragment<PT>(from.p, (wm * FM + i - FN) * 16u, from.n, lane);
+        if (i == 0) f.p[0] = read_fragment<PT, SP::COLS>(from.p, (wm * FM) * 16u, from.n, lane);
+        else if (i <= FN) f.q[i - 1] = read_fragment<QT, SQ::COLS>(from.q, (wn * FN + i - 1) * 16u, from.n, lane);
+        else f.p[i - FN] = read_fragment<PT, SP::COLS>(from.p, (wm * FM + i - FN) * 16u, from.n, lane);
     };
     // Loads of a step's first part (the first halves of transposed operands) and of its second (operands in one piece, the second halves).
     constexpr int LOADS_A = (PT ? SP::INSTR : 0) + (QT ? SQ::INSTR : 0), WHOLE = (PT ? 0 : SP::INSTR) + (QT ? 0 : SQ::INSTR), LOADS_B = WHOLE + LOADS_A;
@@ -484,7 +505,11 @@ static hipError_t launch_tiles(const LinearArgs& a, const LinearPlan& p, hipStre
 template <int FORM, bool EXTRAS = false>
 static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
     const LinearPlan p = plan_linear(a.M, a.N, a.K);
-    return p.shape == T256 ? launch_tiles<T256, FORM, EXTRAS>(a, p, stream) : launch_tiles<T128, FORM, EXTRAS>(a, p, stream);
+    switch (p.shape) {
+        case T256: return launch_tiles<T256, FORM, EXTRAS>(a, p, stream);
+        case T128: return launch_tiles<T128, FORM, EXTRAS>(a, p, stream);
+        default: return launch_tiles<T64, FORM, EXTRAS>(a, p, stream);
+    }
 }
 
 size_t linear_workspace(uint32_t M, uint32_t N, uint32_t K) { return plan_linear(M, N, K).workspace(); }

@@ -6,7 +6,7 @@
 namespace skiparse {
 
 // Tiles of C that workgroups take; LINEAR_SHAPES of them.
-enum LinearShape : int { T256 = 0, T128 = 1, LINEAR_SHAPES = 2 };
+enum LinearShape : int { T256 = 0, T128 = 1, T64 = 2, LINEAR_SHAPES = 3 };
 struct LinearTile {
     uint32_t m, n;      // rows and channels of a tile
     uint32_t per_cu;    // workgroups that a CU holds
@@ -16,7 +16,7 @@ struct LinearTile {
 constexpr uint32_t LINEAR_CUS = 256;
 constexpr uint32_t LINEAR_STEP = 64, LINEAR_STEPS = 2 * LINEAR_STEP;  // k is walked in pairs of steps
 constexpr uint32_t LINEAR_MAX_PARTS = 16;
-constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {{256, 256, 1, 7.f, 1.4f, 1.0f}, {128, 128, 2, 4.f, 0.9f, 0.5f}};
+constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {{256, 256, 1, 7.f, 1.4f, 1.0f}, {128, 128, 2, 4.f, 0.9f, 0.5f}, {64, 64, 4, 3.f, 0.6f, 0.3f}};
 constexpr float LINEAR_JOIN = 4.f, LINEAR_JOIN_BYTES = 2.0e-7f;  // us of the launch that joins parts, and of a byte that goes through memory
 
 // Tiles in the order of their numbers: `whole` of them are one workgroup each, every other one `parts` workgroups of `per` of k.  Their sums are joined by a second launch.
