@@ -664,6 +664,7 @@ static int linear_common(int B, int T, int H, int W, int in_features, int out_fe
         if (rc != SKIPARSE_OK) return rc;
         if (features >= (1 << 23)) return SKIPARSE_ESHAPE;
     }
+    if ((uint64_t)in_features * (uint64_t)out_features >= (1ull << 40)) return SKIPARSE_ESHAPE;
     if (dtype != SKIPARSE_BF16 || in_features % 8 != 0 || out_features % 8 != 0) return SKIPARSE_EUNSUPPORTED;
     *rows = (size_t)B * sh.n_tok;
     return SKIPARSE_OK;
@@ -682,7 +683,7 @@ static bool touches(Span x, std::initializer_list<Span> others) {
 
 size_t skiparse_linear_workspace_bytes(int rows, int in_features, int out_features) {
     if (rows < 1 || in_features < 1 || out_features < 1) return 0;
-    return linear_workspace((uint32_t)rows, (uint32_t)out_features, (uint32_t)in_features);
+    return linear_workspace(LINEAR_FWD, (uint32_t)rows, (uint32_t)out_features, (uint32_t)in_features);
 }
 
 int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, void* out, void* pre, void* pre_scales, int B, int T, int H, int W,
@@ -701,7 +702,7 @@ int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const vo
     const Span sp = {pre, rows * N * (pre_scales ? 1 : 2)}, ss = {pre_scales, checkpoint_scales(rows, N)}, sr = {residual, rows * N * 2};
     if (touches(so, {sx, sw, sb, sp, ss}) || (residual && residual != out && overlap2(out, so.bytes, residual, sr.bytes))) return SKIPARSE_EINVAL;
     if (touches(sp, {sx, sw, sb, ss, sr}) || touches(ss, {sx, sw, sb, sr})) return SKIPARSE_EINVAL;
-    const size_t need = linear_workspace((uint32_t)rows, (uint32_t)N, (uint32_t)K);
+    const size_t need = linear_workspace(LINEAR_FWD, (uint32_t)rows, (uint32_t)N, (uint32_t)K, pre_scales != nullptr);
     if (need && (!workspace || workspace_bytes < need || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
     if (touches({need ? workspace : nullptr, need}, {sx, sw, sb, sr, so, sp, ss})) return SKIPARSE_EINVAL;
     LinearArgs a = {};
@@ -726,7 +727,7 @@ static LinearBwdSpace linear_bwd_space(size_t rows, size_t K, size_t N, bool dz,
     l.dz = dz ? align256(rows * N * 2) : 0;
     l.x = x ? align256(rows * K * 2) : 0;
     l.db = db ? align256((size_t)linear_rows_parts((uint32_t)rows) * N * sizeof(float)) : 0;
-    const size_t px = dx ? linear_workspace((uint32_t)rows, (uint32_t)K, (uint32_t)N) : 0, pw = dw ? linear_workspace((uint32_t)N, (uint32_t)K, (uint32_t)rows) : 0;
+    const size_t px = dx ? linear_workspace(LINEAR_DX, (uint32_t)rows, (uint32_t)K, (uint32_t)N) : 0, pw = dw ? linear_workspace(LINEAR_DW, (uint32_t)N, (uint32_t)K, (uint32_t)rows) : 0;
     l.parts = px > pw ? px : pw;  // one product after the other
     l.total = l.dz + l.x + l.db + l.parts;
     return l;

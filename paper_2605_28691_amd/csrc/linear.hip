@@ -84,47 +84,6 @@ __device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char
     return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Workgroup -> tile.  Workgroup id % 8 is the XCD; each XCD has a contiguous range of an order in which TILE_GROUP tiles of m are walked together along n, so that the 32
-// tiles that it works on at once share operands in its L2.
-constexpr uint32_t TILE_GROUP = 4;
-struct TileMap {
-    Div32 group;       // tiles of a group: TILE_GROUP * tiles_n
-    Div32 size, last;  // tiles of m in a group, in the last one
-    Div32 rest;        // tiles that are cut along k
-    uint32_t tiles_m, whole, parts, per;
-    static __device__ inline uint32_t of_xcd(uint32_t id, uint32_t total) {
-        const uint32_t xcd = id & 7u, over = total & 7u;  // the first `over` XCDs have one more
-        return xcd * (total >> 3) + (xcd < over ? xcd : over) + (id >> 3);
-    }
-    // tile number `lin`
-    __device__ inline void tile(uint32_t lin, uint32_t& tm, uint32_t& tn) const {
-        const uint32_t g = group.div(lin), in = lin - g * group.d, first = g * TILE_GROUP;
-        const bool full = first + TILE_GROUP <= tiles_m;
-        tn = full ? size.div(in) : last.div(in);
-        tm = first + in - tn * (full ? size.d : last.d);
-    }
-    // workgroup `id`: its tile, its range of k, and for a part its number among the parts, else ~0
-    __device__ inline void at(uint32_t id, uint32_t K, uint32_t& tm, uint32_t& tn, uint32_t& k0, uint32_t& k1, uint32_t& slot) const {
-        k0 = 0u;
-        k1 = K;
-        slot = ~0u;
-        if (id < whole) {
-            tile(of_xcd(id, whole), tm, tn);
-            return;
-        }
-        const uint32_t lin = of_xcd(id - whole, rest.d * parts);  // neighbours: tiles that walk the same k
-        const uint32_t part = rest.div(lin), r = lin - part * rest.d;
-        tile(whole + r, tm, tn);
-        k0 = part * per;
-        k1 = K - k0 < per ? K : k0 + per;
-        slot = r * parts + part;
-    }
-};
-static TileMap make_tile_map(const LinearPlan& p) {
-    const uint32_t over = p.tiles_m % TILE_GROUP;
-    return {make_div32(TILE_GROUP * p.tiles_n), make_div32(TILE_GROUP), make_div32(over ? over : 1u), make_div32(p.rest ? p.rest : 1u), p.tiles_m, p.whole, p.parts, p.per};
-}
-
 // Exchange of the odd rows of 16 lanes of `a` with the even ones of `b` (v_permlane16_swap; its own inverse).
 __device__ __attribute__((always_inline)) inline void swap_rows(uint32_t& a, uint32_t& b) {
     const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
@@ -502,8 +461,103 @@ static hipError_t launch_tiles(const LinearArgs& a, const LinearPlan& p, hipStre
     return hipGetLastError();
 }
 
+// x w^T for up to LINEAR_THIN_ROWS rows, which reads w once and is bound by that: a wavefront has CH channels, and reads 512 of k of each at once, whole lines; rows of x are read
+// with them and come out of the caches.  Its sums, ROWS for every channel, are added up over the lanes at the end.  (5120 -> 5120, one row: 9.5 us, 15.6 in
+// tiles of 64 x 64, cut in six; reading w as the products' fragments, 64 bytes of 16 rows at once, 15.6.)
+constexpr int THIN_WAVES = 4;
+template <int CH, int ROWS>
+__global__ __launch_bounds__(64 * THIN_WAVES) void linear_thin_kernel(LinearArgs a) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    constexpr int AT_ONCE = CH * ROWS >= 8 ? 1 : 2;  // times 512 of k
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n0 = (blockIdx.x * THIN_WAVES + wave) * CH;
+    if (n0 >= a.N) return;
+    const uint32_t ld = a.K * 2u;
+    uint32_t xo[ROWS];
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) {
+        const uint32_t row = (uint32_t)m < a.M ? (uint32_t)m : a.M - 1u;
+        xo[m] = (a.order == 0 ? row : a.order == 1 ? source_row<TO_SPARSE>(a.rows, row, 0u) : source_row<TO_ORIGINAL>(a.rows, row, 0u)) * ld;
+    }
+    float acc[CH][ROWS];
+#pragma unroll
+    for (int c = 0; c < CH; c++)
+#pragma unroll
+        for (int m = 0; m < ROWS; m++) acc[c][m] = 0.f;
+#if defined(__HIP_DEVICE_COMPILE__)
+    // N is a multiple of 8, so a wavefront's channels are all there
+    const auto wb = __builtin_amdgcn_make_buffer_rsrc((char*)a.q + (size_t)n0 * ld, 0, LIN_RECORDS, 0x27000);
+    const auto xb = __builtin_amdgcn_make_buffer_rsrc((char*)a.p, 0, LIN_RECORDS, 0x27000);
+    for (uint32_t k = 0; k < a.K; k += 512u * AT_ONCE) {
+        u32x4 w[AT_ONCE][CH], x[AT_ONCE][ROWS];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) {
+            const uint32_t at = k + 512u * u + lane * 8u;  // behind the end: zeros
+#pragma unroll
+            for (int c = 0; c < CH; c++) w[u][c] = __builtin_amdgcn_raw_buffer_load_b128(wb, at < a.K ? at * 2u + c * ld : LIN_OUTSIDE, 0, 0);
+#pragma unroll
+            for (int m = 0; m < ROWS; m++) x[u][m] = __builtin_amdgcn_raw_buffer_load_b128(xb, at < a.K ? at * 2u + xo[m] : LIN_OUTSIDE, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                auto value = [&](const u32x4& v) __attribute__((always_inline)) -> float { return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16); };
+                float xv[ROWS];
+#pragma unroll
+                for (int m = 0; m < ROWS; m++) xv[m] = value(x[u][m]);
+#pragma unroll
+                for (int c = 0; c < CH; c++) {
+                    const float wv = value(w[u][c]);
+#pragma unroll
+                    for (int m = 0; m < ROWS; m++) acc[c][m] = fmaf(wv, xv[m], acc[c][m]);
+                }
+            }
+    }
+#endif
+    // lane c * ROWS + m takes the sum of channel c and row m
+    float z = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; c++)
+#pragma unroll
+        for (int m = 0; m < ROWS; m++) {
+            float s = acc[c][m];
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
+            if (lane == (uint32_t)(c * ROWS + m)) z = s;
+        }
+    const uint32_t n = n0 + lane / ROWS, m = lane % ROWS;
+    if (lane >= CH * ROWS || m >= a.M) return;
+    const LinearEpilogue& e = a.e;
+    const size_t at = (size_t)m * a.N + n;
+    if (e.bias != nullptr) z += (float)((const __bf16*)e.bias)[n];
+    if (e.pre != nullptr) ((__bf16*)e.pre)[at] = (__bf16)z;
+    z = act_value(e.act, z);
+    if (e.residual != nullptr) z += (float)((const __bf16*)e.residual)[at];
+    ((__bf16*)e.out)[at] = (__bf16)z;
+}
+
+template <int CH, int ROWS>
+static hipError_t launch_thin(const LinearArgs& a, hipStream_t stream) {
+    constexpr uint32_t per = CH * THIN_WAVES;
+    linear_thin_kernel<CH, ROWS><<<(a.N + per - 1u) / per, 64 * THIN_WAVES, 0, stream>>>(a);
+    return hipGetLastError();
+}
+template <int CH>
+static hipError_t launch_thin(const LinearArgs& a, hipStream_t stream) {
+    return a.M == 1u ? launch_thin<CH, 1>(a, stream) : a.M == 2u ? launch_thin<CH, 2>(a, stream) : launch_thin<CH, 4>(a, stream);
+}
+static hipError_t launch_thin(const LinearArgs& a, hipStream_t stream) {
+    switch (thin_channels(a.N)) {
+        case 1: return launch_thin<1>(a, stream);
+        case 2: return launch_thin<2>(a, stream);
+        default: return launch_thin<4>(a, stream);
+    }
+}
+
 template <int FORM, bool EXTRAS = false>
 static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
+    if (FORM == LINEAR_FWD && linear_thin(a.M, a.N, a.K) && a.e.pre_scales == nullptr) return launch_thin(a, stream);
     const LinearPlan p = plan_linear(a.M, a.N, a.K);
     switch (p.shape) {
         case T256: return launch_tiles<T256, FORM, EXTRAS>(a, p, stream);
@@ -512,7 +566,9 @@ static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
     }
 }
 
-size_t linear_workspace(uint32_t M, uint32_t N, uint32_t K) { return plan_linear(M, N, K).workspace(); }
+size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K, bool checkpoint) {
+    return form == LINEAR_FWD && linear_thin(M, N, K) && !checkpoint ? 0u : plan_linear(M, N, K).workspace();
+}
 
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream) {
     switch (form) {

@@ -3,21 +3,34 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "index_map.h"
+
 namespace skiparse {
 
 // Tiles of C that workgroups take; LINEAR_SHAPES of them.
 enum LinearShape : int { T256 = 0, T128 = 1, T64 = 2, LINEAR_SHAPES = 3 };
 struct LinearTile {
-    uint32_t m, n;      // rows and channels of a tile
-    uint32_t per_cu;    // workgroups that a CU holds
-    float fixed;        // us of a workgroup outside its walk over k
-    float step, last;   // us a step of 64 of k with all CUs busy, and with few
+    uint32_t m, n;    // rows and channels of a tile
+    uint32_t per_cu;  // workgroups that a CU holds
+    float fixed;      // us of a workgroup outside its walk over k
+    float few;        // us a step of 64 of k with few workgroups on the chip,
+    float step[4];    // and with 1, 2, .. on every CU (the clock falls as the chip fills)
 };
 constexpr uint32_t LINEAR_CUS = 256;
 constexpr uint32_t LINEAR_STEP = 64, LINEAR_STEPS = 2 * LINEAR_STEP;  // k is walked in pairs of steps
 constexpr uint32_t LINEAR_MAX_PARTS = 16;
-constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {{256, 256, 1, 7.f, 1.4f, 1.0f}, {128, 128, 2, 4.f, 0.9f, 0.5f}, {64, 64, 4, 3.f, 0.6f, 0.3f}};
-constexpr float LINEAR_JOIN = 4.f, LINEAR_JOIN_BYTES = 2.0e-7f;  // us of the launch that joins parts, and of a byte that goes through memory
+// Fitted to 48 products of 16 sizes (1 to 19,200 rows, 256 to 8192 channels, the three forms), each with every tile and up to 8 numbers of parts: what the rule takes is 2.8 % slower
+// than the best of these in the mean, 23 % at most (300 x 2048 x 2048, 16 us instead of 13).  For example, us, 256 / 128 / 64, uncut: 1024^3 24 / 10.0 / 7.1, 6426 x 1000 -> 4008
+// 62 / 78 / 107, 10,000 x 4304 -> 336 84 / 44 / 73; cut best: 128 x 5120 -> 5120 32 / 21 / 20, 1536 x 32,760 -> 1536 133 / 156 / -.
+constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {
+    {256, 256, 1, 7.6f, 0.945f, {1.3f}}, {128, 128, 2, 2.58f, 0.308f, {0.57f, 0.88f}}, {64, 64, 4, 1.45f, 0.241f, {0.302f, 0.39f, 0.61f, 0.883f}}};
+constexpr float LINEAR_JOIN = 3.2f, LINEAR_JOIN_BYTE = 2.3e-7f;  // us of the launch that joins parts, and of a byte that goes through memory
+
+// us a step with `units` workgroups running, at most a full round
+inline float linear_step(const LinearTile& t, uint64_t units) {
+    if (units <= LINEAR_CUS) return t.few + (t.step[0] - t.few) * (float)units / (float)LINEAR_CUS;
+    return t.step[(units - 1u) / LINEAR_CUS];
+}
 
 // Tiles in the order of their numbers: `whole` of them are one workgroup each, every other one `parts` workgroups of `per` of k.  Their sums are joined by a second launch.
 struct LinearPlan {
@@ -35,16 +48,15 @@ inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K) {
         const uint64_t tiles_m = ((uint64_t)M + t.m - 1u) / t.m, tiles_n = ((uint64_t)N + t.n - 1u) / t.n, tiles = tiles_m * tiles_n;
         const uint64_t slots = (uint64_t)LINEAR_CUS * t.per_cu, rounds = tiles / slots, rest = tiles - rounds * slots;
         const uint32_t pairs = (uint32_t)(((uint64_t)K + LINEAR_STEPS - 1u) / LINEAR_STEPS);
-        const float walk = 2.f * (float)pairs, full = (float)rounds * (t.fixed + walk * t.step);
+        const float full = t.step[t.per_cu - 1u];
         for (uint32_t parts = 1; parts <= LINEAR_MAX_PARTS && parts <= pairs; parts++) {
             if (rest == 0 && parts > 1) break;
             const uint32_t per = (pairs + parts - 1u) / parts;
             if (parts > 1 && (uint64_t)(parts - 1u) * per >= pairs) continue;  // the last part would be empty
-            const uint64_t units = rest * parts, again = (units + slots - 1u) / slots;
-            const uint64_t running = units < slots ? units : slots;
-            const float step = t.last + (t.step - t.last) * (float)running / (float)slots;
-            float cost = full + (float)again * (t.fixed + 2.f * (float)per * step);
-            if (parts > 1) cost += LINEAR_JOIN + LINEAR_JOIN_BYTES * (float)(units * t.m * t.n * 4u);
+            const uint64_t units = rest * parts, again = units / slots, left = units - again * slots;
+            float cost = (float)rounds * (t.fixed + 2.f * (float)pairs * full) + (float)again * (t.fixed + 2.f * (float)per * full);
+            if (left) cost += t.fixed + 2.f * (float)per * linear_step(t, left);
+            if (parts > 1) cost += LINEAR_JOIN + LINEAR_JOIN_BYTE * (float)(units * t.m * t.n * 4u);
             if (best_cost == 0.f || cost < best_cost) {
                 best_cost = cost;
                 best = {shape, (uint32_t)tiles_m, (uint32_t)tiles_n, (uint32_t)(parts > 1 ? tiles - rest : tiles), (uint32_t)(parts > 1 ? rest : 0), parts, per * LINEAR_STEPS};
@@ -52,6 +64,57 @@ inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K) {
         }
     }
     return best;
+}
+
+// Whether x w^T with M rows goes to the kernel for few rows.
+constexpr uint32_t LINEAR_THIN_ROWS = 4;
+inline bool linear_thin(uint32_t M, uint32_t N, uint32_t K) {
+    (void)N; (void)K;
+    return M <= LINEAR_THIN_ROWS;
+}
+
+// Channels of a wavefront there: as many as leave 2048 wavefronts.
+inline uint32_t thin_channels(uint32_t N) { return N >= 8192u ? 4u : N >= 4096u ? 2u : 1u; }
+
+// Workgroup -> tile.  Workgroup id % 8 is the XCD; each XCD has a contiguous range of an order in which TILE_GROUP tiles of m are walked together along n, so that the 32
+// tiles that it works on at once share operands in its L2.
+constexpr uint32_t TILE_GROUP = 4;
+struct TileMap {
+    Div32 group;       // tiles of a group: TILE_GROUP * tiles_n
+    Div32 size, last;  // tiles of m in a group, in the last one
+    Div32 rest;        // tiles that are cut along k
+    uint32_t tiles_m, whole, parts, per;
+    static __host__ __device__ inline uint32_t of_xcd(uint32_t id, uint32_t total) {
+        const uint32_t xcd = id & 7u, over = total & 7u;  // the first `over` XCDs have one more
+        return xcd * (total >> 3) + (xcd < over ? xcd : over) + (id >> 3);
+    }
+    // tile number `lin`
+    __host__ __device__ inline void tile(uint32_t lin, uint32_t& tm, uint32_t& tn) const {
+        const uint32_t g = group.div(lin), in = lin - g * group.d, first = g * TILE_GROUP;
+        const bool full = first + TILE_GROUP <= tiles_m;
+        tn = full ? size.div(in) : last.div(in);
+        tm = first + in - tn * (full ? size.d : last.d);
+    }
+    // workgroup `id`: its tile, its range of k, and for a part its number among the parts, else ~0
+    __host__ __device__ inline void at(uint32_t id, uint32_t K, uint32_t& tm, uint32_t& tn, uint32_t& k0, uint32_t& k1, uint32_t& slot) const {
+        k0 = 0u;
+        k1 = K;
+        slot = ~0u;
+        if (id < whole) {
+            tile(of_xcd(id, whole), tm, tn);
+            return;
+        }
+        const uint32_t lin = of_xcd(id - whole, rest.d * parts);  // neighbours: tiles that walk the same k
+        const uint32_t part = rest.div(lin), r = lin - part * rest.d;
+        tile(whole + r, tm, tn);
+        k0 = part * per;
+        k1 = K - k0 < per ? K : k0 + per;
+        slot = r * parts + part;
+    }
+};
+inline TileMap make_tile_map(const LinearPlan& p) {
+    const uint32_t over = p.tiles_m % TILE_GROUP;
+    return {make_div32(TILE_GROUP * p.tiles_n), make_div32(TILE_GROUP), make_div32(over ? over : 1u), make_div32(p.rest ? p.rest : 1u), p.tiles_m, p.whole, p.parts, p.per};
 }
 
 }  // namespace skiparse
