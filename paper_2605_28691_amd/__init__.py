@@ -463,10 +463,10 @@ def skiparse_attn_fwd_fp8(q8, k8, v8, sq, sk, sv, T: int, H: int, W: int, s: int
 
 
 def _here(*tensors) -> None:
-    """Calls go to the current device's stream: a tensor of another device is refused."""
+    """Calls go to the current device's stream: a tensor of another device is refused.  (One on the CPU is refused where its address is asked for.)"""
     device = torch.cuda.current_device() if _get_device is None else _get_device()
     for t in tensors:
-        if t is not None and t.device.index not in (None, device):
+        if t is not None and t.get_device() not in (device, -1):
             raise ValueError(f"tensor on {t.device}, but the current device is {device}")
 
 
@@ -512,34 +512,32 @@ def skiparse_rope(q: torch.Tensor, k: torch.Tensor | None, table: RopeTable, T: 
     """Turns the first channels of every head of q and k by their tokens' places: (q', k'), k' None without a k.  q, k: [B][T*H*W][heads][D], or
     [s*s*B][T*H*W/(s*s)][heads][D] for order "to_original" and "stay_sparse"; `at`: the table's place of the grid's first token along t, h, w.  inverse=True is the
     gradient.  Where rows keep their places, q_out=q and k_out=k turn in place."""
-    n = T * H * W
-    if q.dim() != 4:
-        raise ValueError("q has four dimensions")
-    rows = q.shape[0] * q.shape[1]
-    heads, D = q.shape[2], q.shape[3]
-    s2 = s * s
-    sparse_in = order in ("to_original", "stay_sparse")
-    if n < 1 or s < 1 or rows % n or (q.shape[1] * s2 if sparse_in else q.shape[1]) != n:
+    B, n_in, heads, D = q.shape
+    n, s2 = T * H * W, s * s
+    sparse_in = order == "to_original" or order == "stay_sparse"
+    rows = B * n_in
+    if n < 1 or s < 1 or rows % n or (n_in * s2 if sparse_in else n_in) != n:
         raise ValueError("token axis does not match the grid")
     B = rows // n
     if k is not None and (k.shape != q.shape or k.dtype != q.dtype):
         raise ValueError("q and k differ in shape or type")
-    if table.data.dtype != torch.float32 or table.data.numel() != 2 * sum(n_ * (r // 2) for n_, r in zip(table.lengths, table.axes)):
+    data, (lt, lh, lw), (rt, rh, rw) = table
+    if data.dtype != torch.float32 or data.numel() != 2 * (lt * (rt // 2) + lh * (rh // 2) + lw * (rw // 2)):
         raise ValueError("the table is float32 and as long as its lengths and axes say")
-    shape = q.shape if order in ("same", "stay_sparse") else (s2 * B, n // s2, heads, D) if order == "to_sparse" else (B, n, heads, D)
+    shape = (s2 * B, n // s2, heads, D) if order == "to_sparse" else (B, n, heads, D) if order == "to_original" else q.shape
     q_out = _into(q_out, shape, q)
     k_out = None if k is None else _into(k_out, shape, q)
-    _here(q, k, q_out, k_out, table.data)
-    _skiparse_rope(q, k, q_out, k_out, table.data, B, heads, T, H, W, D, *table.axes, *table.lengths, *at, s, PATTERNS[pattern], ORDERS[order],
+    _here(q, k, q_out, k_out, data)
+    _skiparse_rope(q, k, q_out, k_out, data, B, heads, T, H, W, D, rt, rh, rw, lt, lh, lw, *at, s, PATTERNS[pattern], ORDERS[order],
                    ROPE_LAYOUTS[layout], 1 if inverse else 0, _DTYPES[q.dtype], _stream())
     return q_out, k_out
 
 
 def _into(out, shape, like, dtype=None):
     """`out`, or a new tensor of that shape; one that is passed has to have it."""
-    dtype = dtype or like.dtype
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+    dtype = dtype or like.dtype
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
         raise ValueError(f"an output of shape {tuple(shape)} and type {dtype} is needed")
     return out
@@ -596,10 +594,10 @@ def _linear_rows(lead, order: str, T: int, H: int, W: int, s: int):
     return (B, T, H, W), (s2 * B, n // s2) if order == "to_sparse" else (B, n)
 
 
-def _typed(dtype, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and t.dtype != dtype:
-            raise ValueError(f"{name} must be {dtype}")
+def _bf16(what: str, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != torch.bfloat16:
+            raise ValueError(f"{what} must be bfloat16")
 
 
 def skiparse_linear_fwd(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None, act: str = "none",
@@ -611,7 +609,7 @@ def skiparse_linear_fwd(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | N
     K, (N, Kw) = x.shape[-1], w.shape
     if K != Kw or (bias is not None and tuple(bias.shape) != (N,)):
         raise ValueError("x, w and bias do not fit each other")
-    _typed(torch.bfloat16, x=x, w=w, bias=bias, residual=residual)
+    _bf16("x, w, bias and residual", x, w, bias, residual)
     grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
     shape = (*lead, N)
     out = _into(out, shape, x)
@@ -664,8 +662,8 @@ def skiparse_linear_bwd(dy: torch.Tensor, x, w: torch.Tensor, pre=None, act: str
     if isinstance(x, Checkpoint):
         _checked(x, xc.shape, "x")
     else:
-        _typed(torch.bfloat16, x=x)
-    _typed(torch.bfloat16, dy=dy, w=w, dx_add=dx_add)
+        _bf16("x", x)
+    _bf16("dy, w and dx_add", dy, w, dx_add)
     grid, lead = _linear_rows(xc.shape[:-1], order, T, H, W, s)
     if tuple(dy.shape) != (*lead, N) or (dx_add is not None and dx_add.shape != xc.shape):
         raise ValueError("dy or dx_add does not have its rows")

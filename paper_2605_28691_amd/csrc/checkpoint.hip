@@ -23,7 +23,7 @@ __device__ inline bool piece_at(const CkptArgs& a, uint64_t i, uint64_t& elem, u
     block = i >> 2;
     elem = i * 8u;
     if (!RAGGED) return true;
-    const uint64_t row = i / a.per_row.d;
+    const uint64_t row = a.pieces >> 32 ? i / a.per_row.d : a.per_row.div((uint32_t)i);  // the same way for the whole launch
     const uint32_t c = (uint32_t)(i - row * a.per_row.d) * 8u;
     elem = row * a.cols + c;
     return c < a.cols;

@@ -7,8 +7,9 @@
 // when it is made, so that far positions cost nothing here.
 //
 // A wavefront has CH = head_dim / 8 lanes a head and as many heads at once as fit; a lane's place in the head, and with it its cosines, is the same in all
-// ROPE_ITERS rounds, so one look-up serves them.  Fewer heads than fit: several tokens a wavefront.  The pairs of the half layout lie R / 2 channels apart, in another
-// lane's chunk: the wavefront passes its chunks through LDS.
+// rounds, so one look-up serves them.  Fewer heads than fit: several tokens a wavefront.  The pairs of the half layout lie R / 2 channels apart, in another
+// lane's chunk: the wavefront passes its chunks through LDS, and reads whole chunks there where R / 2 is some of them (channel by channel 824 us instead of 649 in an earlier
+// state, 80,640 tokens x 40 heads).  3.3 GB, q and k of that size into the sparse layout, take 587 us (5.6 TB/s; a plain copy 4.9).
 #include "kernels.h"
 
 namespace skiparse {
@@ -17,7 +18,13 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 constexpr int ROPE_WAVES = 4;
-constexpr int ROPE_ITERS = 4;  // rounds of a wavefront: loads in flight before the first use
+// Rounds of a wavefront that are loaded at once, and wavefronts that are left where it takes more of them, so that one look-up of the cosines serves all (us, q and k of 80,640
+// tokens x 40 heads into the sparse layout / half layout in place / 32,760 x 12 half layout; 4 rounds a look-up 595 / 614 / 84.3, as many as leave 16,384 wavefronts, 3 at
+// once 599 / 594 / 75.1, 4 598 / 593 / 75.5, 5 587 / 582 / 75.4).
+constexpr int ROPE_ITERS = 5;
+constexpr uint64_t ROPE_MIN_WAVES = 16384;
+// Tensors beyond this pass by the caches: what is smaller is still there when the next kernel reads it (us, cached / past: 110 MB moved 21.4 / 27.9, 400 MB 79.0 / 70.3, 1.6 GB 634 / 596).
+constexpr uint64_t ROPE_CACHED_BYTES = 128ull << 20;
 
 struct RopeDev {
     const void* x[2];
@@ -29,7 +36,7 @@ struct RopeDev {
     uint32_t n_rows, heads, ch, per_wave;  // per_wave: heads at once
     uint32_t tokens;         // tokens a wavefront
     uint32_t rounds;         // rounds of one tensor over its heads; those of the second follow
-    uint32_t total_rounds;
+    uint32_t total_rounds, rounds_per_wave;
     uint32_t R, head_dim;
     uint32_t end_t, end_h;   // pairs below end_t turn with t, below end_h with h
     uint32_t n_t, n_h, n_w;  // pairs of an axis
@@ -70,9 +77,13 @@ struct Chunk<float> {
 // MAP: which way rows go; a move within the sparse layout (ROPE_STAY) and within the original order have source row = destination row.
 enum RopeMap : int { ROPE_SAME = 0, ROPE_TO_SPARSE = 1, ROPE_TO_ORIGINAL = 2, ROPE_STAY = 3 };
 
-template <typename T, int MAP, bool HALF>
+// How a head's pairs lie: next to each other, R / 2 apart by whole chunks, R / 2 apart anyhow.
+enum RopePairs : int { PAIRS_NEXT = 0, PAIRS_CHUNKS = 1, PAIRS_APART = 2 };
+
+template <typename T, int MAP, int PAIRS, bool NT>
 __global__ __launch_bounds__(64 * ROPE_WAVES) void rope_kernel(RopeDev a) {
     using C = Chunk<T>;
+    constexpr bool HALF = PAIRS != PAIRS_NEXT;
     __shared__ __attribute__((aligned(16))) char stage_all[HALF ? ROPE_WAVES * 64 * 16 * C::N : 16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t id = blockIdx.x * ROPE_WAVES + wave;
@@ -91,23 +102,29 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void rope_kernel(RopeDev a) {
         if (MAP == ROPE_TO_SPARSE) src = n;
         if (MAP == ROPE_TO_ORIGINAL) src = source_row<TO_ORIGINAL>(a.rows, row, 0u);
     }
-    // all loads first
-    u32x4 p[ROPE_ITERS][C::N];
-    uint64_t at[ROPE_ITERS];
-    bool on[ROPE_ITERS];
     const uint64_t row_len = (uint64_t)a.heads * a.head_dim;
-#pragma unroll
-    for (int i = 0; i < ROPE_ITERS; i++) {
-        const uint32_t r = part * ROPE_ITERS + i, second = r >= a.rounds ? 1u : 0u;
+    u32x4 p[ROPE_ITERS][C::N];
+    // where the lane's chunk of round r lies in its token's row; false: none of the wavefront's
+    auto place = [&](uint32_t r, uint32_t& second, uint64_t& at) __attribute__((always_inline)) -> bool {
+        second = r >= a.rounds ? 1u : 0u;
         const uint32_t head = head0 + (r - second * a.rounds) * a.per_wave;
-        on[i] = lane_on && r < a.total_rounds && head < a.heads;
-        at[i] = (uint64_t)head * a.head_dim + c * 8u;
-        if (on[i]) {
-            const u32x4* from = (const u32x4*)((const T*)a.x[second] + (uint64_t)src * row_len + at[i]);
+        at = (uint64_t)head * a.head_dim + c * 8u;
+        return lane_on && r < a.total_rounds && head < a.heads;
+    };
+    // all loads of ROPE_ITERS rounds at once
+    auto load = [&](uint32_t first) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < C::N; j++) p[i][j] = from[j];
+        for (int i = 0; i < ROPE_ITERS; i++) {
+            uint32_t second;
+            uint64_t at;
+            if (!place(first + i, second, at)) continue;
+            const u32x4* from = (const u32x4*)((const T*)a.x[second] + (uint64_t)src * row_len + at);
+#pragma unroll
+            for (int j = 0; j < C::N; j++) p[i][j] = NT ? __builtin_nontemporal_load(from + j) : from[j];
         }
-    }
+    };
+    const uint32_t first = part * a.rounds_per_wave, end = first + a.rounds_per_wave < a.total_rounds ? first + a.rounds_per_wave : a.total_rounds;
+    load(first);
     // the cosines and sines of the lane's channels
     const uint32_t in_grid = n - a.n_tok.div(n) * a.n_tok.d;
     const uint32_t t = a.hw.div(in_grid), in_frame = in_grid - t * a.hw.d, h = a.w.div(in_frame), w = in_frame - h * a.w.d;
@@ -132,51 +149,77 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void rope_kernel(RopeDev a) {
         }
     }
     char* const stage = HALF ? stage_all + wave * (64 * 16 * C::N) : nullptr;
+    for (uint32_t r0 = first;;) {
 #pragma unroll
-    for (int i = 0; i < ROPE_ITERS; i++) {
-        const uint32_t r = part * ROPE_ITERS + i, second = r >= a.rounds ? 1u : 0u;
-        if (r >= a.total_rounds) break;  // a whole wavefront
-        float v[8];
-        if (HALF) {
-            // other lanes may have read the region last; the wavefront's LDS accesses take effect in order
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+        for (int i = 0; i < ROPE_ITERS; i++) {
+            const uint32_t r = r0 + i;
+            if (r >= end) break;  // a whole wavefront
+            uint32_t second;
+            uint64_t at;
+            const bool on = place(r, second, at);
+            float v[8];
+            if (HALF) {
+                // other lanes may have read the region last; the wavefront's LDS accesses take effect in order
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int j = 0; j < C::N; j++) *(u32x4*)(stage + lane * (16 * C::N) + 16 * j) = p[i][j];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            const char* const head = stage + (lane - c) * (16 * C::N);
+                for (int j = 0; j < C::N; j++) *(u32x4*)(stage + lane * (16 * C::N) + 16 * j) = p[i][j];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                const char* const head = stage + (lane - c) * (16 * C::N);
+                if (PAIRS == PAIRS_CHUNKS) {
+                    const uint32_t hc = half >> 3, oc = !lane_on || c >= 2u * hc ? c : c < hc ? c + hc : c - hc;
+                    u32x4 o[C::N];
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const uint32_t ch = c * 8u + e, other = !lane_on || ch >= a.R ? ch : ch < half ? ch + half : ch - half;
-                v[e] = C::get(p[i], e) * cs[e] + C::at(head, other) * sn[e];
+                    for (int j = 0; j < C::N; j++) o[j] = *(const u32x4*)(head + oc * (16 * C::N) + 16 * j);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] = C::get(p[i], e) * cs[e] + C::get(o, e) * sn[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const uint32_t ch = c * 8u + e, other = !lane_on || ch >= a.R ? ch : ch < half ? ch + half : ch - half;
+                        v[e] = C::get(p[i], e) * cs[e] + C::at(head, other) * sn[e];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float x0 = C::get(p[i], 2 * e), x1 = C::get(p[i], 2 * e + 1);
+                    v[2 * e] = x0 * cs[e] - x1 * sn[e];
+                    v[2 * e + 1] = x0 * sn[e] + x1 * cs[e];
+                }
             }
-        } else {
+            C::put(p[i], v, turned);
+            if (on) {
+                u32x4* to = (u32x4*)((T*)a.y[second] + (uint64_t)row * row_len + at);
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const float x0 = C::get(p[i], 2 * e), x1 = C::get(p[i], 2 * e + 1);
-                v[2 * e] = x0 * cs[e] - x1 * sn[e];
-                v[2 * e + 1] = x0 * sn[e] + x1 * cs[e];
+                for (int j = 0; j < C::N; j++) {
+                    if (NT) __builtin_nontemporal_store(p[i][j], to + j);
+                    else to[j] = p[i][j];
+                }
             }
         }
-        C::put(p[i], v, turned);
-        if (on[i]) {
-            u32x4* to = (u32x4*)((T*)a.y[second] + (uint64_t)row * row_len + at[i]);
-#pragma unroll
-            for (int j = 0; j < C::N; j++) to[j] = p[i][j];
-        }
+        r0 += ROPE_ITERS;
+        if (r0 >= end) break;
+        load(r0);
     }
 }
 
-template <typename T, bool HALF>
+template <typename T, int PAIRS, bool NT>
 static hipError_t launch_rope_t(const RopeDev& d, int map, uint32_t blocks, hipStream_t stream) {
     switch (map) {
-        case ROPE_SAME: rope_kernel<T, ROPE_SAME, HALF><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
-        case ROPE_TO_SPARSE: rope_kernel<T, ROPE_TO_SPARSE, HALF><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
-        case ROPE_TO_ORIGINAL: rope_kernel<T, ROPE_TO_ORIGINAL, HALF><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
-        default: rope_kernel<T, ROPE_STAY, HALF><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
+        case ROPE_SAME: rope_kernel<T, ROPE_SAME, PAIRS, NT><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
+        case ROPE_TO_SPARSE: rope_kernel<T, ROPE_TO_SPARSE, PAIRS, NT><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
+        case ROPE_TO_ORIGINAL: rope_kernel<T, ROPE_TO_ORIGINAL, PAIRS, NT><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
+        default: rope_kernel<T, ROPE_STAY, PAIRS, NT><<<blocks, 64 * ROPE_WAVES, 0, stream>>>(d); break;
     }
     return hipGetLastError();
+}
+template <typename T>
+static hipError_t launch_rope_t(const RopeDev& d, int map, int pairs, bool nt, uint32_t blocks, hipStream_t stream) {
+    if (pairs == PAIRS_NEXT) return nt ? launch_rope_t<T, PAIRS_NEXT, true>(d, map, blocks, stream) : launch_rope_t<T, PAIRS_NEXT, false>(d, map, blocks, stream);
+    if (pairs == PAIRS_CHUNKS) return nt ? launch_rope_t<T, PAIRS_CHUNKS, true>(d, map, blocks, stream) : launch_rope_t<T, PAIRS_CHUNKS, false>(d, map, blocks, stream);
+    return launch_rope_t<T, PAIRS_APART, false>(d, map, blocks, stream);
 }
 
 hipError_t launch_rope(const RopeArgs& r, hipStream_t stream) {
@@ -203,7 +246,13 @@ hipError_t launch_rope(const RopeArgs& r, hipStream_t stream) {
     }
     d.rounds = d.tokens > 1u ? 1u : (d.heads + d.per_wave - 1u) / d.per_wave;
     d.total_rounds = d.rounds * (r.k ? 2u : 1u);
-    const uint32_t parts = (d.total_rounds + ROPE_ITERS - 1u) / ROPE_ITERS;
+    // a look-up of the cosines serves as many rounds as leave ROPE_MIN_WAVES wavefronts
+    const uint64_t groups = ((uint64_t)d.n_rows + d.tokens - 1u) / d.tokens;
+    const uint32_t fours = (d.total_rounds + ROPE_ITERS - 1u) / ROPE_ITERS;
+    uint64_t per = groups * fours / ROPE_MIN_WAVES;
+    per = per < 1u ? 1u : per < fours ? per : fours;
+    d.rounds_per_wave = (uint32_t)per * ROPE_ITERS;
+    const uint32_t parts = (d.total_rounds + d.rounds_per_wave - 1u) / d.rounds_per_wave;
     d.parts = make_div32(parts);
     d.R = (uint32_t)(r.rt + r.rh + r.rw);
     d.n_t = (uint32_t)r.rt / 2u;
@@ -216,11 +265,12 @@ hipError_t launch_rope(const RopeArgs& r, hipStream_t stream) {
     d.off_h = (uint32_t)r.len_t * d.n_t + (uint32_t)r.h0 * d.n_h - d.end_t;
     d.off_w = (uint32_t)r.len_t * d.n_t + (uint32_t)r.len_h * d.n_h + (uint32_t)r.w0 * d.n_w - d.end_h;
     d.sign = r.inverse ? -1.f : 1.f;
-    const uint64_t groups = ((uint64_t)d.n_rows + d.tokens - 1u) / d.tokens;
     const uint64_t blocks = (groups * parts + ROPE_WAVES - 1u) / ROPE_WAVES;
     if (!fits_grid(blocks, 64 * ROPE_WAVES)) return hipErrorInvalidConfiguration;
-    if (r.f32) return r.half ? launch_rope_t<float, true>(d, r.order, (uint32_t)blocks, stream) : launch_rope_t<float, false>(d, r.order, (uint32_t)blocks, stream);
-    return r.half ? launch_rope_t<__bf16, true>(d, r.order, (uint32_t)blocks, stream) : launch_rope_t<__bf16, false>(d, r.order, (uint32_t)blocks, stream);
+    const int pairs = !r.half ? PAIRS_NEXT : d.R % 16u == 0 ? PAIRS_CHUNKS : PAIRS_APART;
+    const uint64_t bytes = (uint64_t)d.n_rows * d.heads * d.head_dim * (r.f32 ? 4u : 2u) * (r.k ? 2u : 1u);
+    const bool nt = bytes > ROPE_CACHED_BYTES;
+    return r.f32 ? launch_rope_t<float>(d, r.order, pairs, nt, (uint32_t)blocks, stream) : launch_rope_t<__bf16>(d, r.order, pairs, nt, (uint32_t)blocks, stream);
 }
 
 // ---- the table
@@ -243,10 +293,10 @@ __device__ inline double rope_turns(const RopeAxis& x, const RopeScaling& s, uin
 }
 
 constexpr uint32_t ROPE_TABLE_THREADS = 256;
-constexpr uint32_t ROPE_TABLE_ITEMS = 8;  // entries a thread
+constexpr uint32_t ROPE_TABLE_BLOCKS = 1024;  // at most, of an axis: a workgroup forms its axis' frequencies anew, which takes as long as some thousand entries
 
-// One launch a table; a workgroup forms the frequencies of its axis once.  Angles are reduced in 64 bits (to an eighth of a turn, and the quadrant), the
-// functions taken in 32.
+// One launch a table.  Angles are reduced in 64 bits to an eighth of a turn either way and the quadrant; sine and cosine of what is left are taken in 32 by their series, whose
+// first terms left out are 2e-9 and 1e-10 at the eighth.  Bound by the arithmetic: 131,072 x 64 pairs, 67 MB, 15.5 us (with the library's functions and eight entries a thread 22).
 __global__ __launch_bounds__(ROPE_TABLE_THREADS) void rope_table_kernel(f32x2* table, RopeAxis t, RopeAxis h, RopeAxis w, RopeScaling s) {
     __shared__ double freq[ROPE_MAX_PAIRS];
     const RopeAxis x = blockIdx.x < t.blocks ? t : blockIdx.x < t.blocks + h.blocks ? h : w;
@@ -255,16 +305,13 @@ __global__ __launch_bounds__(ROPE_TABLE_THREADS) void rope_table_kernel(f32x2* t
     for (uint32_t j = threadIdx.x; j < pairs; j += ROPE_TABLE_THREADS) freq[j] = rope_turns(x, s, j);
     __syncthreads();
     const uint32_t n = x.len * pairs;  // below 2^31
-    for (uint32_t u = 0; u < ROPE_TABLE_ITEMS; u++) {
-        const uint32_t i = (block * ROPE_TABLE_ITEMS + u) * ROPE_TABLE_THREADS + threadIdx.x;
-        if (i >= n) break;
+    for (uint32_t i = block * ROPE_TABLE_THREADS + threadIdx.x; i < n; i += x.blocks * ROPE_TABLE_THREADS) {
         const uint32_t place = x.pairs.div(i), j = i - place * pairs;
         const double turns = (double)place * freq[j], q = rint(turns * 4.0);
-        const float g = (float)((turns - q * 0.25) * 2.0);  // half turns, at most a quarter
-        float sn, cs;
-        sn = sinpif(g);
-        cs = cospif(g);
-        const int quadrant = (int)((long long)q & 3);
+        const float g = (float)((turns - q * 0.25) * 6.283185307179586477), g2 = g * g;
+        const float sn = g * fmaf(g2, fmaf(g2, fmaf(g2, fmaf(g2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), 1.f);
+        const float cs = fmaf(g2, fmaf(g2, fmaf(g2, fmaf(g2, fmaf(g2, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+        const int quadrant = (int)(uint32_t)(long long)q & 3;
         const float c0 = quadrant & 1 ? sn : cs, s0 = quadrant & 1 ? cs : sn;
         const float c1 = quadrant == 1 || quadrant == 2 ? -c0 : c0, s1 = quadrant >= 2 ? -s0 : s0;
         table[x.first + i] = f32x2{c1 * s.attention, s1 * s.attention};
@@ -277,7 +324,8 @@ hipError_t launch_rope_table(float* table, RopeAxis t, RopeAxis h, RopeAxis w, c
     for (RopeAxis* x : {&t, &h, &w}) {
         const uint32_t n = x->len * (x->r / 2u);
         x->first = first;
-        x->blocks = (n + ROPE_TABLE_THREADS * ROPE_TABLE_ITEMS - 1u) / (ROPE_TABLE_THREADS * ROPE_TABLE_ITEMS);
+        x->blocks = (n + ROPE_TABLE_THREADS - 1u) / ROPE_TABLE_THREADS;
+        if (x->blocks > ROPE_TABLE_BLOCKS) x->blocks = ROPE_TABLE_BLOCKS;
         x->pairs = make_div32(x->r ? x->r / 2u : 1u);
         first += n;
         blocks += x->blocks;

@@ -148,8 +148,11 @@ def test_binding_refusals(monkeypatch):
 
 def test_tensors_of_another_device_are_refused(monkeypatch):
     class Far:
-        class device:
-            index = 1
+        device = "cuda:1"
+
+        @staticmethod
+        def get_device():
+            return 1
 
     monkeypatch.setattr(sk, "_get_device", lambda: 0)
     sk._here(None, torch.zeros(1))
