@@ -299,3 +299,62 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("M, N", [(3, 96), (70, 72), (300, 520)])
+def test_kept_values_that_are_not_finite(M, N):
+    """In a checkpoint that a product writes they become NaN and leave the scale of their block to the others; as in one that is saved."""
+    import paper_2605_28691_amd as sk
+
+    K = 64
+    x, w, bias, _, _ = _inputs(M, K, N, M)
+    bias[5], bias[40], bias[41] = float("inf"), float("nan"), float("-inf")
+    out, pre = sk.skiparse_linear_fwd(x, w, bias, keep="bf16")
+    assert torch.equal(pre.isnan(), torch.isnan(bias).expand(M, N)) and torch.equal(pre.isfinite(), bias.isfinite().expand(M, N))
+    _, kept = sk.skiparse_linear_fwd(x, w, bias, keep="checkpoint")
+    got = sk.skiparse_checkpoint_load(kept, dtype=torch.float32)
+    assert torch.equal(got.isnan(), ~bias.isfinite().expand(M, N))
+    b0 = bias.clone()
+    b0[[5, 40, 41]] = 0
+    z = x.double() @ w.double().t() + b0.double()
+    z[:, [5, 40, 41]] = 0.0
+    sums = (K + 4) * ref.F32 * (x.double().abs() @ w.double().abs().t() + b0.double().abs())
+    step = torch.exp2(kept.scales.double() - 127).repeat_interleave(32, -1)[:, :N] * 2.0 ** -10
+    fine = bias.isfinite()
+    assert ((got.double() - z).abs() <= ref.E4M3 * z.abs() + step + 1.1 * sums)[:, fine].all()
+    blocks = -(-N // 32)
+    top = torch.nn.functional.pad(z.abs(), (0, blocks * 32 - N)).reshape(M, blocks, 32).amax(-1)
+    assert (torch.exp2(kept.scales.double() - 127) * 448 >= top * (1 - 1e-3)).all() and (torch.exp2(kept.scales.double() - 127) * 224 <= top * (1 + 1e-3)).all()
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("K, N", [(8, 8), (520, 4104), (1032, 8200), (5128, 24)])
+def test_few_rows(M, K, N):
+    """The kernel for up to four rows, with one, two and four channels a wavefront, and the first size beyond it; in the order they come and moved."""
+    import paper_2605_28691_amd as sk
+
+    x, w, bias, residual, _ = _inputs(M, K, N, M + K)
+    for act in ("none", "silu"):
+        out, pre = sk.skiparse_linear_fwd(x, w, bias, residual, act=act, keep="bf16")
+        z, sums = _check_forward(x, w, bias, residual, act, out)
+        _close(pre, z, ref.BF16 * z.abs() + sums, "pre")
+    if M == 4:
+        x4 = x.reshape(1, 4, K)
+        got = sk.skiparse_linear_fwd(x4, w, bias, order="to_sparse", T=1, H=2, W=2, s=2, pattern="token")
+        assert got.shape == (4, 1, N) and torch.equal(got.reshape(4, N), sk.skiparse_linear_fwd(x, w, bias))
+        back = sk.skiparse_linear_fwd(x4.reshape(4, 1, K), w, bias, order="to_original", T=1, H=2, W=2, s=2, pattern="token")
+        assert torch.equal(back.reshape(4, N), got.reshape(4, N))
+
+
+def test_rows_and_channels_at_the_edges_of_all_tiles():
+    """Results of the three tiles, whole and cut along k, with and without everything that the epilogue does."""
+    import paper_2605_28691_amd as sk
+
+    for M, K, N in ((513, 4096, 264), (1030, 2176, 1032), (5000, 192, 2056), (7700, 520, 1544), (2600, 7000, 520), (60, 9000, 72)):
+        x, w, bias, residual, dy = _inputs(M, K, N, M)
+        _check_forward(x, w, None, None, "none", sk.skiparse_linear_fwd(x, w))
+        out, kept = sk.skiparse_linear_fwd(x, w, bias, residual, act="silu", keep="checkpoint")
+        z, sums = _check_forward(x, w, bias, residual, "silu", out)
+        step = torch.exp2(kept.scales.double() - 127).repeat_interleave(32, -1)[:, :N] * 2.0 ** -10
+        assert ((ref.values(kept.codes, kept.scales) - z).abs() <= ref.E4M3 * z.abs() + step + 1.1 * sums).all()
+        _check_backward(dy, x.double(), w, None, "none", *sk.skiparse_linear_bwd(dy, x, w))
