@@ -2,8 +2,9 @@
 // the rows.  Bound by HBM bandwidth: dy and z are read once, dz written once; the sums are of the float32 values, before dz is rounded to bf16 for the products.
 // The rounding is off by 2^-9 of a value at most and independent from row to row, so in a product's result it is as large as that of its own output.
 //
-// A workgroup takes ROWS_PER_PART rows by 256 channels: 32 lanes of 8 channels, 8 rows at a time.  The sums of a part go to memory and are added up in order by a
-// second launch: the same bits every time, without atomics.
+// A workgroup takes the rows of a part by 256 channels: 32 lanes of 8 channels, 8 rows at a time.  One row a thread at a time is best: what is in flight lies close together then
+// (us, 6426 x 4008 with a checkpoint of z / 3840 x 5120 with z in bf16, both in parts of 32 rows: one row 30.2 / 28.0, two at once 34.1 / -, four 39.7 / 35.8; parts of 128 41.4
+// / -).  The sums of a part go to memory and are added up in order by a second launch: the same bits every time, without atomics.  80,640 x 5120, 2.1 GB, 430 us.
 #include "checkpoint.h"
 #include "kernels.h"
 #include "linear_act.h"
@@ -13,11 +14,12 @@ namespace skiparse {
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-constexpr uint32_t ROWS_PER_PART = 128, ROWS_AT_ONCE = 8;
+constexpr uint32_t LANES_X = 32, COLS = LANES_X * 8, ROWS_AT_ONCE = 256 / LANES_X;
+// Small problems need the workgroups, large ones' parts would cost traffic: 4 bytes written and read of every 32 rows' 64 and more.
+static uint32_t rows_per_part(uint32_t M) { return M < 32768u ? 32u : 128u; }
 
-uint32_t linear_rows_parts(uint32_t M) { return (M + ROWS_PER_PART - 1u) / ROWS_PER_PART; }
+uint32_t linear_rows_parts(uint32_t M) { return (M + rows_per_part(M) - 1u) / rows_per_part(M); }
 
 __device__ inline void unpack8(const u32x4& x, float (&v)[8]) {
 #pragma unroll
@@ -27,16 +29,17 @@ __device__ inline void unpack8(const u32x4& x, float (&v)[8]) {
     }
 }
 
-__global__ __launch_bounds__(256) void linear_rows_kernel(LinearRowsArgs a, uint32_t col_blocks) {
-    __shared__ float sums[ROWS_AT_ONCE][256];
+template <bool ACT, bool CHECKPOINT>
+__global__ __launch_bounds__(256) void linear_rows_kernel(LinearRowsArgs a, uint32_t col_blocks, uint32_t per_part) {
+    __shared__ float sums[ROWS_AT_ONCE][COLS];
     const uint32_t part = blockIdx.x / col_blocks, cb = blockIdx.x - part * col_blocks;
-    const uint32_t lane = threadIdx.x & 31u, ty = threadIdx.x >> 5;
-    const uint32_t n = cb * 256u + lane * 8u;
+    const uint32_t lane = threadIdx.x % LANES_X, ty = threadIdx.x / LANES_X;
+    const uint32_t n = cb * COLS + lane * 8u;
     const bool in = n < a.N;
     const uint32_t blocks = (a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK;
     float sum[8] = {};
-    for (uint32_t r = ty; r < ROWS_PER_PART; r += ROWS_AT_ONCE) {
-        const uint32_t row = part * ROWS_PER_PART + r;
+    for (uint32_t r = ty; r < per_part; r += ROWS_AT_ONCE) {
+        const uint32_t row = part * per_part + r;
         if (!in || row >= a.M) break;
         uint32_t from = row;
         if (a.order == 1) from = source_row<TO_SPARSE>(a.rows, row, 0u);
@@ -44,9 +47,9 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearRowsArgs a, uint
         const size_t at = (size_t)from * a.N + n;
         float g[8];
         unpack8(*(const u32x4*)((const unsigned short*)a.dy + at), g);
-        if (a.pre != nullptr) {
+        if (ACT) {
             float z[8];
-            if (a.pre_scales != nullptr) {
+            if (CHECKPOINT) {
                 const u32x2 c = *(const u32x2*)((const unsigned char*)a.pre + at);
                 const float up = ckpt_up(((const unsigned char*)a.pre_scales)[(size_t)from * blocks + n / CKPT_BLOCK]);
                 float lo[4], hi[4];
@@ -76,12 +79,13 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearRowsArgs a, uint
 #pragma unroll
     for (int e = 0; e < 8; e++) sums[ty][lane * 8u + e] = sum[e];
     __syncthreads();
-    const uint32_t c = cb * 256u + threadIdx.x;
+    const uint32_t c = cb * COLS + threadIdx.x;
     if (c >= a.N) return;
     float s = 0.f;
 #pragma unroll
     for (uint32_t i = 0; i < ROWS_AT_ONCE; i++) s += sums[i][threadIdx.x];
-    a.db_part[(size_t)part * a.N + c] = s;
+    if (gridDim.x == col_blocks) ((__bf16*)a.db)[c] = (__bf16)s;  // one part
+    else a.db_part[(size_t)part * a.N + c] = s;
 }
 
 // The parts' sums, 64 channels a workgroup, 16 parts at a time.
@@ -89,8 +93,10 @@ __global__ __launch_bounds__(1024) void linear_db_kernel(const float* __restrict
     __shared__ float sums[16][64];
     const uint32_t lane = threadIdx.x & 63u, ty = threadIdx.x >> 6, n = blockIdx.x * 64u + lane;
     float s = 0.f;
-    if (n < N)
+    if (n < N) {
+#pragma unroll 8
         for (uint32_t p = ty; p < parts; p += 16u) s += part[(size_t)p * N + n];
+    }
     sums[ty][lane] = s;
     __syncthreads();
     if (ty != 0u || n >= N) return;
@@ -101,11 +107,14 @@ __global__ __launch_bounds__(1024) void linear_db_kernel(const float* __restrict
 }
 
 hipError_t launch_linear_rows(const LinearRowsArgs& a, hipStream_t stream) {
-    const uint32_t col_blocks = (a.N + 255u) / 256u, parts = linear_rows_parts(a.M);
+    const uint32_t col_blocks = (a.N + COLS - 1u) / COLS, parts = linear_rows_parts(a.M);
     if (!fits_grid((uint64_t)col_blocks * parts, 256u)) return hipErrorInvalidConfiguration;
-    linear_rows_kernel<<<col_blocks * parts, 256, 0, stream>>>(a, col_blocks);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.db_part == nullptr) return e;
+    const uint32_t per = rows_per_part(a.M);
+    if (a.pre == nullptr) linear_rows_kernel<false, false><<<col_blocks * parts, 256, 0, stream>>>(a, col_blocks, per);
+    else if (a.pre_scales == nullptr) linear_rows_kernel<true, false><<<col_blocks * parts, 256, 0, stream>>>(a, col_blocks, per);
+    else linear_rows_kernel<true, true><<<col_blocks * parts, 256, 0, stream>>>(a, col_blocks, per);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.db_part == nullptr || parts == 1u) return e;
     linear_db_kernel<<<(a.N + 63u) / 64u, 1024, 0, stream>>>(a.db_part, (__bf16*)a.db, parts, a.N);
     return hipGetLastError();
 }
