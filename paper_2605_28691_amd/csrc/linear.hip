@@ -7,7 +7,7 @@
 //   * A workgroup is 4 wavefronts, 2 x 2, one a SIMD; at 256 x 256 each has 128 x 128 of C in 256 accumulation registers, so that a fragment read from LDS feeds 8
 //     products.
 //   * Tiles go from memory straight into LDS (buffer_load_dwordx4 ... lds), 64 of k a step, double buffered.  Operands with k along the row are laid out in rows of
-//     128 bytes and read 16 bytes at a time; transposed ones in rows of 256 and read with ds_read_b64_tr_b16; swizzles as in lds_layout.h.
+//     128 bytes and read 16 bytes at a time; transposed ones in rows of 256 and read with ds_read_b64_tr_b16; no read has bank conflicts.
 //   * Ends: a 16-byte piece behind the end of k is given an offset outside the buffer and reads as zero; transposed operands end with the buffer; rows
 //     past the last read the last one, columns past the last whatever lies there, and neither is stored.
 #include <type_traits>
@@ -31,6 +31,11 @@ constexpr uint32_t LIN_KT = 64;           // of k a step
 constexpr uint32_t LIN_OUTSIDE = ~0u;     // an offset outside every buffer
 constexpr uint32_t LIN_RECORDS = 0xfffffff0u;
 
+// Where 16-byte chunk c of row r of an operand in one piece lies: at c ^ row_swizzle(r).  A read of 16 bytes a lane is served 16 lanes at a time, 0-3, 12-15 and 20-27, then 4-11,
+// 16-19 and 28-31, and the same of the upper half: of a fragment rows 0-3 and 12-15 of one chunk with rows 4-11 of its neighbour, or the other way round; these touch every bank
+// once.  (With the attention's swizzle, for 32 rows of a chunk, half of the reads' clocks were conflicts.)
+__host__ __device__ constexpr uint32_t row_swizzle(uint32_t r) { return r >> 1 & 7u; }
+
 // One operand's side of a workgroup's tile: ROWS of m (or n).
 //   !T: a step, 64 of k, in one piece: rows of 128 bytes, whole lines of the caches (64 bytes of a line at a time, 8192^3 took 900 us instead of 846)
 //    T: halves of 32 rows of k, COLS columns each, which are free and filled again one after the other
@@ -49,7 +54,7 @@ struct Side {
             const uint32_t n = wave * INSTR + i;  // of the tile's
             if (!T) {
                 const uint32_t r = n * 8u + lane / 8u;
-                kofs[i] = ((lane % 8u) ^ lds_swizzle<64>(r)) * 8u;
+                kofs[i] = ((lane % 8u) ^ row_swizzle(r)) * 8u;
                 off[i] = row_off(r) + kofs[i] * 2u;
             } else {
                 constexpr uint32_t PER = 64 / LANES;  // rows at once
@@ -71,7 +76,7 @@ struct Side {
 template <bool T, uint32_t COLS>
 __device__ __attribute__((always_inline)) inline bf16x8 read_fragment(const char* buf, uint32_t row0, uint32_t half, uint32_t lane) {
     const uint32_t li = lane & 15u, g = lane >> 4;
-    if (!T) return *(const bf16x8*)(buf + (row0 + li) * 128u + ((4u * half + g) ^ lds_swizzle<64>(li)) * 16u);
+    if (!T) return *(const bf16x8*)(buf + (row0 + li) * 128u + ((4u * half + g) ^ row_swizzle(li)) * 16u);
     const char* const part = buf + row0 / COLS * (COLS * 64u);
     bf16x4 v[2];
 #pragma unroll

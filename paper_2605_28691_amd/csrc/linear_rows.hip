@@ -1,6 +1,6 @@
 // What stands in front of a linear layer's backward products: dz = dy act'(z), written in the order of the input's rows, and the bias's gradient, the sum of dz over
 // the rows.  Bound by HBM bandwidth: dy and z are read once, dz written once; the sums are of the float32 values, before dz is rounded to bf16 for the products.
-// The rounding is off by 2^-9 of a value at most and independent from row to row, so in a product's result it is as large as that of its own output.
+// The rounding is off by 2^-8 of a value at most and independent from row to row, so in a product's result it is as large as that of its own output.
 //
 // A workgroup takes the rows of a part by 256 channels: 32 lanes of 8 channels, 8 rows at a time.  One row a thread at a time is best: what is in flight lies close together then
 // (us, 6426 x 4008 with a checkpoint of z / 3840 x 5120 with z in bf16, both in parts of 32 rows: one row 30.2 / 28.0, two at once 34.1 / -, four 39.7 / 35.8; parts of 128 41.4
