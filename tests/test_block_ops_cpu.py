@@ -80,6 +80,15 @@ def test_linear_refusals(lib):
         assert _fwd(lib, **bad) == ESHAPE, bad
     for bad in (dict(dtype=1), dict(dtype=2), dict(K=60), dict(N=100)):
         assert _fwd(lib, **bad) == EUNSUPPORTED, bad
+    assert _fwd(lib, K=(1 << 23) - 8, N=(1 << 23) - 8, s=1) == ESHAPE  # weights of 2^40 elements and more
+    # a product that is cut along k needs the workspace, clear of everything else
+    large = dict(T=1, H=16, W=8, s=1, K=5120, N=5120)
+    need = lib.skiparse_linear_workspace_bytes(128, 5120, 5120)
+    assert need > 0
+    for bad in (dict(ws=None), dict(size=need - 1), dict(ws=ODD)):
+        assert _fwd(lib, **large, **bad) == EWORKSPACE, bad
+    for at in (0, 1, 2, 3, 4, 5, 6):
+        assert _fwd(lib, **large, ws=P[at]) == EINVAL, at
 
 
 def test_linear_backward_refusals(lib):
