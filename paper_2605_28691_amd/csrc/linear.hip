@@ -562,17 +562,18 @@ static hipError_t launch_thin(const LinearArgs& a, hipStream_t stream) {
 
 template <int FORM, bool EXTRAS = false>
 static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
-    if (FORM == LINEAR_FWD && linear_thin(a.M, a.N, a.K) && a.e.pre_scales == nullptr) return launch_thin(a, stream);
+    if (FORM == LINEAR_FWD && linear_thin(a.M) && a.e.pre_scales == nullptr) return launch_thin(a, stream);
     const LinearPlan p = plan_linear(a.M, a.N, a.K);
     switch (p.shape) {
         case T256: return launch_tiles<T256, FORM, EXTRAS>(a, p, stream);
         case T128: return launch_tiles<T128, FORM, EXTRAS>(a, p, stream);
+        case T128X256: return launch_tiles<T128X256, FORM, EXTRAS>(a, p, stream);
         default: return launch_tiles<T64, FORM, EXTRAS>(a, p, stream);
     }
 }
 
 size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K, bool checkpoint) {
-    return form == LINEAR_FWD && linear_thin(M, N, K) && !checkpoint ? 0u : plan_linear(M, N, K).workspace();
+    return form == LINEAR_FWD && linear_thin(M) && !checkpoint ? 0u : plan_linear(M, N, K).workspace();
 }
 
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream) {

@@ -8,7 +8,7 @@
 namespace skiparse {
 
 // Tiles of C that workgroups take; LINEAR_SHAPES of them.
-enum LinearShape : int { T256 = 0, T128 = 1, T64 = 2, LINEAR_SHAPES = 3 };
+enum LinearShape : int { T256 = 0, T128 = 1, T64 = 2, T128X256 = 3, LINEAR_SHAPES = 4 };
 struct LinearTile {
     uint32_t m, n;    // rows and channels of a tile
     uint32_t per_cu;  // workgroups that a CU holds
@@ -19,11 +19,12 @@ struct LinearTile {
 constexpr uint32_t LINEAR_CUS = 256;
 constexpr uint32_t LINEAR_STEP = 64, LINEAR_STEPS = 2 * LINEAR_STEP;  // k is walked in pairs of steps
 constexpr uint32_t LINEAR_MAX_PARTS = 16;
-// Fitted to 48 products of 16 sizes (1 to 19,200 rows, 256 to 8192 channels, the three forms), each with every tile and up to 8 numbers of parts: what the rule takes is 2.8 % slower
-// than the best of these in the mean, 23 % at most (300 x 2048 x 2048, 16 us instead of 13).  For example, us, 256 / 128 / 64, uncut: 1024^3 24 / 10.0 / 7.1, 6426 x 1000 -> 4008
-// 62 / 78 / 107, 10,000 x 4304 -> 336 84 / 44 / 73; cut best: 128 x 5120 -> 5120 32 / 21 / 20, 1536 x 32,760 -> 1536 133 / 156 / -.
+// Fitted to products of 28 sizes (1 to 32,760 rows, 256 to 20,480 channels, the three forms), each with every tile and several numbers of parts: over the last 36 of them what the
+// rule takes is 1 % slower than the best in the mean, 9 % at most.  For example, us, 256 / 128 / 64 / 128 x 256, uncut: 8190 x 1536 -> 1536 36 / 43 / 60 / 48, dx of
+// 6426 x 1000 -> 4008 82 / 71 / 120 / 53 (408 tiles of 128 are 80 % of a round of two a CU, 204 of 128 x 256 of a round of one; 256 x 128 64), 1000 x 2048 -> 2048
+// 40 / 17 / 18 / 25; cut best: 3840 x 5120 -> 5120 155 / 173 / 285 / 184.
 constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {
-    {256, 256, 1, 7.6f, 0.945f, {1.3f}}, {128, 128, 2, 2.58f, 0.308f, {0.57f, 0.88f}}, {64, 64, 4, 1.45f, 0.241f, {0.302f, 0.39f, 0.61f, 0.883f}}};
+    {256, 256, 1, 7.6f, 0.945f, {1.3f}}, {128, 128, 2, 2.58f, 0.308f, {0.57f, 0.88f}}, {64, 64, 4, 1.45f, 0.241f, {0.302f, 0.39f, 0.61f, 0.883f}}, {128, 256, 1, 4.29f, 0.587f, {0.809f}}};
 constexpr float LINEAR_JOIN = 3.2f, LINEAR_JOIN_BYTE = 2.3e-7f;  // us of the launch that joins parts, and of a byte that goes through memory
 
 // us a step with `units` workgroups running, at most a full round
@@ -68,10 +69,7 @@ inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K) {
 
 // Whether x w^T with M rows goes to the kernel for few rows.
 constexpr uint32_t LINEAR_THIN_ROWS = 4;
-inline bool linear_thin(uint32_t M, uint32_t N, uint32_t K) {
-    (void)N; (void)K;
-    return M <= LINEAR_THIN_ROWS;
-}
+inline bool linear_thin(uint32_t M) { return M <= LINEAR_THIN_ROWS; }
 
 // Channels of a wavefront there: as many as leave 2048 wavefronts.
 inline uint32_t thin_channels(uint32_t N) { return N >= 8192u ? 4u : N >= 4096u ? 2u : 1u; }

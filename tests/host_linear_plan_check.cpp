@@ -1,4 +1,4 @@
-// Cuts products of the linear layer into workgroups (paper_2605_28691_amd/csrc/linear_plan.h) on the host.  Reads M N K, one product a line; prints, for each, the tile's rows, whole
+// Cuts products of the linear layer into workgroups (paper_2605_28691_amd/csrc/linear_plan.h) on the host.  Reads M N K, one product a line; prints, for each, the tile's rows and channels, whole
 // tiles, cut tiles, parts, bytes of workspace, and "ok" where every place of C and k is some workgroup's once and every part has a slot of its own.  Built and run by
 // tests/test_linear_plan.py.
 #include <cstdio>
@@ -43,6 +43,6 @@ int main() {
             }
             if (at != K) bad = "end of k";
         }
-        printf("%u %u %u %u %zu %s\n", t.m, p.whole, p.rest, p.parts, p.workspace(), bad ? bad : "ok");
+        printf("%u %u %u %u %u %zu %s\n", t.m, t.n, p.whole, p.rest, p.parts, p.workspace(), bad ? bad : "ok");
     }
 }

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import _block_ref as ref
+from test_linear_plan import WIDE
 
 pytestmark = pytest.mark.gpu
 
@@ -347,7 +348,7 @@ def test_few_rows(M, K, N):
 
 
 def test_rows_and_channels_at_the_edges_of_all_tiles():
-    """Results of the three tiles, whole and cut along k, with and without everything that the epilogue does."""
+    """Results of the square tiles, whole and cut along k, with and without everything that the epilogue does."""
     import paper_2605_28691_amd as sk
 
     for M, K, N in ((513, 4096, 264), (1030, 2176, 1032), (5000, 192, 2056), (7700, 520, 1544), (2600, 7000, 520), (60, 9000, 72)):
@@ -357,4 +358,22 @@ def test_rows_and_channels_at_the_edges_of_all_tiles():
         z, sums = _check_forward(x, w, bias, residual, "silu", out)
         step = torch.exp2(kept.scales.double() - 127).repeat_interleave(32, -1)[:, :N] * 2.0 ** -10
         assert ((ref.values(kept.codes, kept.scales) - z).abs() <= ref.E4M3 * z.abs() + step + 1.1 * sums).all()
+        _check_backward(dy, x.double(), w, None, "none", *sk.skiparse_linear_bwd(dy, x, w))
+
+
+@pytest.mark.parametrize("M, N, K", WIDE)
+def test_wide_tiles(M, N, K):
+    """Products with tiles of 128 x 256: forward, and each of the gradients, whose rows, channels and sum are other sizes of the layer."""
+    import paper_2605_28691_amd as sk
+
+    x, w, bias, residual, _ = _inputs(M, K, N, M)
+    _check_forward(x, w, None, None, "none", sk.skiparse_linear_fwd(x, w))
+    out, kept = sk.skiparse_linear_fwd(x, w, bias, residual, act="gelu_tanh", keep="checkpoint")
+    z, sums = _check_forward(x, w, bias, residual, "gelu_tanh", out)
+    step = torch.exp2(kept.scales.double() - 127).repeat_interleave(32, -1)[:, :N] * 2.0 ** -10
+    assert ((ref.values(kept.codes, kept.scales) - z).abs() <= ref.E4M3 * z.abs() + step + 1.1 * sums).all()
+    x, w, _, _, dy = _inputs(M, N, K, M + 1)  # dx: M x N, summed over K
+    _check_backward(dy, x.double(), w, None, "none", *sk.skiparse_linear_bwd(dy, x, w))
+    if M % 8 == 0:
+        x, w, _, _, dy = _inputs(K, N, M, M + 2)  # dw: M x N, summed over K
         _check_backward(dy, x.double(), w, None, "none", *sk.skiparse_linear_bwd(dy, x, w))

@@ -38,11 +38,22 @@ def test_every_part_of_every_tile_once(plans):
 @needs_hipcc
 def test_both_ends_of_the_rule(plans):
     """Large products take the largest tiles, small ones the smallest; a last round that would leave most of the chip idle is cut, a full one is not."""
-    shape, whole, rest, parts, size, _ = (int(x) if x.isdigit() else x for x in plans([(32768, 2048, 4096)])[0])
-    assert (shape, whole, rest, parts, size) == (256, 1024, 0, 1, 0)
-    shape, whole, rest, parts, size, _ = (int(x) if x.isdigit() else x for x in plans([(1536, 1536, 32760)])[0])
-    assert whole == 0 and rest == (1536 // shape) ** 2 and parts > 2 and size == rest * parts * shape * shape * 4
+    m, n, whole, rest, parts, size, _ = (int(x) if x.isdigit() else x for x in plans([(32768, 2048, 4096)])[0])
+    assert (m, n, whole, rest, parts, size) == (256, 256, 1024, 0, 1, 0)
+    m, n, whole, rest, parts, size, _ = (int(x) if x.isdigit() else x for x in plans([(1536, 1536, 32760)])[0])
+    assert whole == 0 and rest == 1536 // m * (1536 // n) and parts > 2 and size == rest * parts * m * n * 4
     assert plans([(256, 256, 256)])[0][0] in ("64", "128")
+
+
+# products (rows, channels, sum) that take tiles of 128 x 256, one not cut and one cut; tests/test_gpu_linear.py has them in each form
+WIDE = [(6566, 536, 2056), (528, 3616, 4008)]
+
+
+@needs_hipcc
+def test_wide_tiles(plans):
+    """Where 128 x 128 would leave a fifth of a round empty, and 256 x 256 most of one."""
+    for size, got in zip(WIDE, plans(WIDE)):
+        assert got[:2] == ["128", "256"] and (got[4] == "1") == (size == WIDE[0]), (size, got)
 
 
 def test_workspace_is_what_the_plan_says():
