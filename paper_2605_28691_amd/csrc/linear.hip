@@ -466,103 +466,189 @@ static hipError_t launch_tiles(const LinearArgs& a, const LinearPlan& p, hipStre
     return hipGetLastError();
 }
 
-// x w^T for up to LINEAR_THIN_ROWS rows, which reads w once and is bound by that: a wavefront has CH channels, and reads 512 of k of each at once, whole lines; rows of x are read
-// with them and come out of the caches.  Its sums, ROWS for every channel, are added up over the lanes at the end.  (5120 -> 5120, one row: 9.5 us, 15.6 in
-// tiles of 64 x 64, cut in six; reading w as the products' fragments, 64 bytes of 16 rows at once, 15.6.)
-constexpr int THIN_WAVES = 4;
-template <int CH, int ROWS>
-__global__ __launch_bounds__(64 * THIN_WAVES) void linear_thin_kernel(LinearArgs a) {
+// x w^T for one row, which reads w once and is bound by that: a wavefront has CH channels, and reads 1024 of k of each at once, whole lines; x is read with them and comes out of the
+// caches.  Its sums are added up over the lanes at the end.  (5120 -> 5120: 9.5 us; reading w as the products' fragments, 64 bytes of 16 rows at once, 15.6.)
+constexpr int ROW_WAVES = 4;
+template <int CH>
+__global__ __launch_bounds__(64 * ROW_WAVES) void linear_row_kernel(LinearArgs a) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-    constexpr int AT_ONCE = CH * ROWS >= 8 ? 1 : 2;  // times 512 of k
+    constexpr int AT_ONCE = 2;  // times 512 of k
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t n0 = (blockIdx.x * THIN_WAVES + wave) * CH;
+    const uint32_t n0 = (blockIdx.x * ROW_WAVES + wave) * CH;
     if (n0 >= a.N) return;
     const uint32_t ld = a.K * 2u;
-    uint32_t xo[ROWS];
+    float acc[CH];
 #pragma unroll
-    for (int m = 0; m < ROWS; m++) {
-        const uint32_t row = (uint32_t)m < a.M ? (uint32_t)m : a.M - 1u;
-        xo[m] = (a.order == 0 ? row : a.order == 1 ? source_row<TO_SPARSE>(a.rows, row, 0u) : source_row<TO_ORIGINAL>(a.rows, row, 0u)) * ld;
-    }
-    float acc[CH][ROWS];
-#pragma unroll
-    for (int c = 0; c < CH; c++)
-#pragma unroll
-        for (int m = 0; m < ROWS; m++) acc[c][m] = 0.f;
+    for (int c = 0; c < CH; c++) acc[c] = 0.f;
 #if defined(__HIP_DEVICE_COMPILE__)
     // N is a multiple of 8, so a wavefront's channels are all there
     const auto wb = __builtin_amdgcn_make_buffer_rsrc((char*)a.q + (size_t)n0 * ld, 0, LIN_RECORDS, 0x27000);
     const auto xb = __builtin_amdgcn_make_buffer_rsrc((char*)a.p, 0, LIN_RECORDS, 0x27000);
     for (uint32_t k = 0; k < a.K; k += 512u * AT_ONCE) {
-        u32x4 w[AT_ONCE][CH], x[AT_ONCE][ROWS];
+        u32x4 w[AT_ONCE][CH], x[AT_ONCE];
 #pragma unroll
         for (int u = 0; u < AT_ONCE; u++) {
             const uint32_t at = k + 512u * u + lane * 8u;  // behind the end: zeros
 #pragma unroll
             for (int c = 0; c < CH; c++) w[u][c] = __builtin_amdgcn_raw_buffer_load_b128(wb, at < a.K ? at * 2u + c * ld : LIN_OUTSIDE, 0, 0);
-#pragma unroll
-            for (int m = 0; m < ROWS; m++) x[u][m] = __builtin_amdgcn_raw_buffer_load_b128(xb, at < a.K ? at * 2u + xo[m] : LIN_OUTSIDE, 0, 0);
+            x[u] = __builtin_amdgcn_raw_buffer_load_b128(xb, at < a.K ? at * 2u : LIN_OUTSIDE, 0, 0);
         }
 #pragma unroll
         for (int u = 0; u < AT_ONCE; u++)
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 auto value = [&](const u32x4& v) __attribute__((always_inline)) -> float { return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16); };
-                float xv[ROWS];
+                const float xv = value(x[u]);
 #pragma unroll
-                for (int m = 0; m < ROWS; m++) xv[m] = value(x[u][m]);
-#pragma unroll
-                for (int c = 0; c < CH; c++) {
-                    const float wv = value(w[u][c]);
-#pragma unroll
-                    for (int m = 0; m < ROWS; m++) acc[c][m] = fmaf(wv, xv[m], acc[c][m]);
-                }
+                for (int c = 0; c < CH; c++) acc[c] = fmaf(value(w[u][c]), xv, acc[c]);
             }
     }
 #endif
-    // lane c * ROWS + m takes the sum of channel c and row m
+    // lane c takes the sum of channel c
     float z = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; c++)
+    for (int c = 0; c < CH; c++) {
+        float s = acc[c];
 #pragma unroll
-        for (int m = 0; m < ROWS; m++) {
-            float s = acc[c][m];
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
-            if (lane == (uint32_t)(c * ROWS + m)) z = s;
-        }
-    const uint32_t n = n0 + lane / ROWS, m = lane % ROWS;
-    if (lane >= CH * ROWS || m >= a.M) return;
+        for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
+        if (lane == (uint32_t)c) z = s;
+    }
+    if (lane >= CH) return;
+    const uint32_t n = n0 + lane;
     const LinearEpilogue& e = a.e;
-    const size_t at = (size_t)m * a.N + n;
     if (e.bias != nullptr) z += (float)((const __bf16*)e.bias)[n];
-    if (e.pre != nullptr) ((__bf16*)e.pre)[at] = (__bf16)z;
+    if (e.pre != nullptr) ((__bf16*)e.pre)[n] = (__bf16)z;
     z = act_value(e.act, z);
-    if (e.residual != nullptr) z += (float)((const __bf16*)e.residual)[at];
-    ((__bf16*)e.out)[at] = (__bf16)z;
+    if (e.residual != nullptr) z += (float)((const __bf16*)e.residual)[n];
+    ((__bf16*)e.out)[n] = (__bf16)z;
 }
 
-template <int CH, int ROWS>
-static hipError_t launch_thin(const LinearArgs& a, hipStream_t stream) {
-    constexpr uint32_t per = CH * THIN_WAVES;
-    linear_thin_kernel<CH, ROWS><<<(a.N + per - 1u) / per, 64 * THIN_WAVES, 0, stream>>>(a);
+// x w^T for a few more rows, up to 16 FM: bound by reading w, which a workgroup does for 16 FN channels.  Its wavefronts take every fourth step of 64 of k, so that together they read
+// 512 bytes in a row, each through steps of its own in LDS (no barriers), FEW_DEEP of them on their way; their sums are added up, in order, at the end.  5 rows, 5120 -> 5120: 52 MB, 12.5 us (19.3 in tiles of
+// 64 x 64, cut in six).
+constexpr int FEW_WAVES = 4, FEW_DEEP = 4;
+template <int FM, int FN>
+__global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearArgs a) {
+    using SP = Side<16 * FM, false, 1>;
+    using SQ = Side<16 * FN, false, 1>;
+    constexpr int SIZE = SP::BYTES + SQ::BYTES, LOADS = SP::INSTR + SQ::INSTR;  // of a step
+    static_assert(SP::BYTES == FM * 2048 && SP::INSTR == 2 * FM, "rows of 128 bytes");
+    // separate arrays for the same reason as above
+    __shared__ __attribute__((aligned(1024))) char s0[FEW_WAVES * SIZE], s1[FEW_WAVES * SIZE], s2[FEW_WAVES * SIZE], s3[FEW_WAVES * SIZE];
+    __shared__ __attribute__((aligned(1024))) f32x4 sums[FEW_WAVES][FM * FN][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n0 = blockIdx.x * (16u * FN), ld = a.K * 2u;
+    SP sp;
+    SQ sq;
+    sp.init(0u, lane, ld, [&](uint32_t r) __attribute__((always_inline)) -> uint32_t {
+        const uint32_t m = r < a.M ? r : a.M - 1u;
+        return (a.order == 0 ? m : a.order == 1 ? source_row<TO_SPARSE>(a.rows, m, 0u) : source_row<TO_ORIGINAL>(a.rows, m, 0u)) * ld;
+    });
+    sq.init(0u, lane, ld, [&](uint32_t r) __attribute__((always_inline)) -> uint32_t {
+        const uint32_t last = a.N - 1u - n0;
+        return (r < last ? r : last) * ld;
+    });
+#pragma unroll
+    for (uint32_t i = 0; i < SP::INSTR; i++)
+        if (i * 8u + lane / 8u >= a.M) sp.kofs[i] = LIN_OUTSIDE;  // rows behind the last: zeros
+    const char *const p0 = (const char*)a.p, *const q0 = (const char*)a.q + (size_t)n0 * ld;
+    auto fill = [&](uint32_t k, char* all) __attribute__((always_inline)) {  // behind the end: zeros
+        char* const to = all + wave * SIZE;
+        const uint32_t left = k < a.K ? a.K - k : 0u;
+#pragma unroll
+        for (int i = 0; i < SQ::INSTR; i++) sq.issue(i, q0 + (size_t)k * 2u, LIN_RECORDS, left, to, 0u);
+#pragma unroll
+        for (int i = 0; i < SP::INSTR; i++) sp.issue(i, p0 + (size_t)k * 2u, LIN_RECORDS, left, to + SQ::BYTES, 0u);
+    };
+    f32x4 acc[FM * FN];
+#pragma unroll
+    for (int i = 0; i < FM * FN; i++) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr uint32_t STRIDE = FEW_WAVES * LIN_KT;
+    auto step = [&](uint32_t k, char* all) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((FEW_DEEP - 1) * LOADS) : "memory");
+        const char* const from = all + wave * SIZE;
+        bf16x8 q[2][FN], p[2][FM];
+#pragma unroll
+        for (uint32_t h = 0; h < 2; h++) {
+#pragma unroll
+            for (int j = 0; j < FN; j++) q[h][j] = read_fragment<false, SQ::COLS>(from, 16u * j, h, lane);
+#pragma unroll
+            for (int i = 0; i < FM; i++) p[h][i] = read_fragment<false, SP::COLS>(from + SQ::BYTES, 16u * i, h, lane);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the step is in registers, and may be filled again
+        __builtin_amdgcn_sched_barrier(0);
+        fill(k + FEW_DEEP * STRIDE, all);
+#pragma unroll
+        for (uint32_t h = 0; h < 2; h++)
+#pragma unroll
+            for (int i = 0; i < FM * FN; i++) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[h][i % FN], p[h][i / FN], acc[i], 0, 0, 0);
+    };
+    uint32_t k = wave * LIN_KT;
+    fill(k, s0);
+    fill(k + STRIDE, s1);
+    fill(k + 2u * STRIDE, s2);
+    fill(k + 3u * STRIDE, s3);
+    for (; k < a.K; k += FEW_DEEP * STRIDE) {
+        step(k, s0);
+        step(k + STRIDE, s1);
+        step(k + 2u * STRIDE, s2);
+        step(k + 3u * STRIDE, s3);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < FM * FN; i++) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    // wavefront i finishes block i: lane l has row l % 16 and channels 4 (l / 16) .. + 3
+    static_assert(FM * FN <= FEW_WAVES, "a block a wavefront");
+    const uint32_t m = wave / FN * 16u + (lane & 15u), n = n0 + wave % FN * 16u + 4u * (lane >> 4);
+    if (wave >= (uint32_t)(FM * FN) || m >= a.M || n >= a.N) return;
+    f32x4 z = sums[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < FEW_WAVES; w++) z += sums[w][wave][lane];
+    const LinearEpilogue& e = a.e;
+    const size_t at = (size_t)m * a.N + n;
+    auto add = [&](const void* t, size_t from) __attribute__((always_inline)) {
+        const bf16x4 x = *(const bf16x4*)((const __bf16*)t + from);
+#pragma unroll
+        for (int c = 0; c < 4; c++) z[c] += (float)x[c];
+    };
+    auto store = [&](void* t) __attribute__((always_inline)) {
+        bf16x4 x;
+#pragma unroll
+        for (int c = 0; c < 4; c++) x[c] = (__bf16)z[c];
+        *(bf16x4*)((__bf16*)t + at) = x;
+    };
+    if (e.bias != nullptr) add(e.bias, n);
+    if (e.pre != nullptr) store(e.pre);
+#pragma unroll
+    for (int c = 0; c < 4; c++) z[c] = act_value(e.act, z[c]);
+    if (e.residual != nullptr) add(e.residual, at);
+    store(e.out);
+}
+
+template <int CH>
+static hipError_t launch_row(const LinearArgs& a, hipStream_t stream) {
+    constexpr uint32_t per = CH * ROW_WAVES;
+    linear_row_kernel<CH><<<(a.N + per - 1u) / per, 64 * ROW_WAVES, 0, stream>>>(a);
     return hipGetLastError();
 }
-template <int CH>
-static hipError_t launch_thin(const LinearArgs& a, hipStream_t stream) {
-    return a.M == 1u ? launch_thin<CH, 1>(a, stream) : a.M == 2u ? launch_thin<CH, 2>(a, stream) : launch_thin<CH, 4>(a, stream);
+template <int FM, int FN>
+static hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
+    linear_few_kernel<FM, FN><<<(a.N + 16u * FN - 1u) / (16u * FN), 64 * FEW_WAVES, 0, stream>>>(a);
+    return hipGetLastError();
 }
-static hipError_t launch_thin(const LinearArgs& a, hipStream_t stream) {
-    switch (thin_channels(a.N)) {
-        case 1: return launch_thin<1>(a, stream);
-        case 2: return launch_thin<2>(a, stream);
-        default: return launch_thin<4>(a, stream);
+static hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
+    if (a.M == 1u) {  // moved or not, row 0
+        const uint32_t channels = row_channels(a.N);
+        return channels == 1u ? launch_row<1>(a, stream) : channels == 2u ? launch_row<2>(a, stream) : launch_row<4>(a, stream);
     }
+    if (few_blocks(a.M, a.N, a.K) == 2u) return a.M <= 16u ? launch_few<1, 2>(a, stream) : launch_few<2, 2>(a, stream);
+    return a.M <= 16u ? launch_few<1, 1>(a, stream) : launch_few<2, 1>(a, stream);
 }
 
 template <int FORM, bool EXTRAS = false>
 static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
-    if (FORM == LINEAR_FWD && linear_thin(a.M) && a.e.pre_scales == nullptr) return launch_thin(a, stream);
+    if (FORM == LINEAR_FWD && linear_few(a.M, a.K) && a.e.pre_scales == nullptr) return launch_few(a, stream);
     const LinearPlan p = plan_linear(a.M, a.N, a.K);
     switch (p.shape) {
         case T256: return launch_tiles<T256, FORM, EXTRAS>(a, p, stream);
@@ -573,7 +659,7 @@ static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
 }
 
 size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K, bool checkpoint) {
-    return form == LINEAR_FWD && linear_thin(M) && !checkpoint ? 0u : plan_linear(M, N, K).workspace();
+    return form == LINEAR_FWD && linear_few(M, K) && !checkpoint ? 0u : plan_linear(M, N, K).workspace();
 }
 
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream) {

@@ -67,12 +67,18 @@ inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K) {
     return best;
 }
 
-// Whether x w^T with M rows goes to the kernel for few rows.
-constexpr uint32_t LINEAR_THIN_ROWS = 4;
-inline bool linear_thin(uint32_t M) { return M <= LINEAR_THIN_ROWS; }
+// Whether x w^T with M rows goes to the kernels for few rows, which read w once and write no checkpoint.  (us, these / tiles: 5120 -> 5120, 5 rows 12.5 / 19.3, 16 rows 14.4 / 19.4,
+// 32 rows 17.8 / 19.7; 1536 -> 8960, 16 rows 8.4 / 12.8, 32 rows 11.3 / 12.9; 13,824 -> 5120, 16 rows 32.1 / 37.0, 32 rows 39.5 / 37.1; 64 -> 11,200, 16 rows 5.9 / 5.9, 32 rows
+// 6.9 / 5.9.)
+inline bool linear_few(uint32_t M, uint32_t K) { return M <= 16u || (M <= 32u && K >= 512u); }
 
-// Channels of a wavefront there: as many as leave 2048 wavefronts.
-inline uint32_t thin_channels(uint32_t N) { return N >= 8192u ? 4u : N >= 4096u ? 2u : 1u; }
+// One row: channels of a wavefront, as many as leave 2048 wavefronts.
+inline uint32_t row_channels(uint32_t N) { return N >= 8192u ? 4u : N >= 4096u ? 2u : 1u; }
+
+// More: blocks of 16 channels of a workgroup.  Two halve what is read of x; one leaves more workgroups, and a CU has two of them, of which one can begin while the other ends.
+// (us, two / one: 5120 -> 5120, 2 rows 12.2 / 13.9, 16 rows 14.4 / 17.0; 5120 -> 13,824, 16 rows 30.4 / 32.9; 1536 -> 8960, 2 rows 9.4 / 8.1, 16 rows 9.7 / 8.4, 17 rows
+// 11.0 / 11.8; 8960 -> 1536, 16 rows 11.9 / 8.7.)
+inline uint32_t few_blocks(uint32_t M, uint32_t N, uint32_t K) { return N >= 4096u && (K >= 4096u || M > 16u) ? 2u : 1u; }
 
 // Workgroup -> tile.  Workgroup id % 8 is the XCD; each XCD has a contiguous range of an order in which TILE_GROUP tiles of m are walked together along n, so that the 32
 // tiles that it works on at once share operands in its L2.

@@ -328,10 +328,11 @@ def test_kept_values_that_are_not_finite(M, N):
     assert (torch.exp2(kept.scales.double() - 127) * 448 >= top * (1 - 1e-3)).all() and (torch.exp2(kept.scales.double() - 127) * 224 <= top * (1 + 1e-3)).all()
 
 
-@pytest.mark.parametrize("M", [1, 2, 3, 4, 5])
-@pytest.mark.parametrize("K, N", [(8, 8), (520, 4104), (1032, 8200), (5128, 24)])
+@pytest.mark.parametrize("M", [1, 2, 4, 5, 15, 16, 17, 31, 32, 33])
+@pytest.mark.parametrize("K, N", [(8, 8), (72, 40), (520, 4104), (1032, 8200), (4104, 4120), (5128, 24)])
 def test_few_rows(M, K, N):
-    """The kernel for up to four rows, with one, two and four channels a wavefront, and the first size beyond it; in the order they come and moved."""
+    """The kernel for one row, with one, two and four channels a wavefront; those for up to 16 and 32, with 16 and 32 channels a workgroup; and the first size beyond them; in the order
+    they come and moved."""
     import paper_2605_28691_amd as sk
 
     x, w, bias, residual, _ = _inputs(M, K, N, M + K)
