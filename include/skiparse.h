@@ -276,6 +276,7 @@ int skiparse_checkpoint_load(const void* codes, const void* scales, void* out, i
  *   x: bf16 with x_scales NULL, or a checkpoint.  pre, pre_scales: what the forward call kept, not read for SKIPARSE_ACT_NONE.
  *   dz is rounded to bf16 for the products (db is not), sums in float32, the results rounded once.  workspace: skiparse_linear_bwd_workspace_bytes() bytes
  *   (x_checkpoint: whether x is one), NULL where that is 0.
+ * A workspace holds nothing between calls; calls that may overlap (two streams, two captured graphs) need one each.
  */
 enum { SKIPARSE_ACT_NONE = 0, SKIPARSE_ACT_GELU_TANH = 1, SKIPARSE_ACT_SILU = 2 };
 size_t skiparse_linear_workspace_bytes(int rows, int in_features, int out_features);

@@ -10,6 +10,7 @@
 //     128 bytes and read 16 bytes at a time; transposed ones in rows of 256 and read with ds_read_b64_tr_b16; no read has bank conflicts.
 //   * Ends: a 16-byte piece behind the end of k is given an offset outside the buffer and reads as zero; transposed operands end with the buffer; rows
 //     past the last read the last one, columns past the last whatever lies there, and neither is stored.
+// Bound by the matrix cores at the board's power limit: 8192^3 720 us (1526 TFLOP/s), 743 both operands transposed; 80,640 x 5120 -> 5120 2992 us (1413).
 #include <type_traits>
 #include <utility>
 
@@ -100,8 +101,8 @@ __device__ __attribute__((always_inline)) inline void swap_rows(uint32_t& a, uin
 // The way out, a row of 16 by 16 FN channels of C at a time.  In the accumulators of two neighbouring blocks lane l has row l % 16 and channels 4 (l / 16) .. + 3 of each; after
 // swap_rows() 8 channels in a row of one of them, block l / 16 % 2, from 8 (l / 32): so that memory is moved 16 bytes a lane and 64 of a row at once.  The one wavefront that a
 // SIMD has issues an instruction in five clocks, so it is their number that costs: addresses are offsets in buffers, which drop what lies behind the last row, and a channel behind
-// the last one has an offset behind every buffer.  (32,760 x 1536 -> 1536: through LDS in whole rows 137 us, this way with 64-bit addresses and tests 134, without any
-// epilogue 106.)
+// the last one has an offset behind every buffer.  (32,760 x 1536 -> 1536, when it was chosen: through LDS in whole rows 137 us, this way with 64-bit addresses and tests 134; now 116,
+// 106 without any epilogue.)
 template <int FN, int FORM, bool EXTRAS>
 struct Out {
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
