@@ -87,3 +87,20 @@ def test_many_short_rows():
     assert ((dw.double() - want).abs() <= ref.BF16 * want.abs() + 8 * M ** 0.5 * ref.F32 * size).all()
     want, size = dy.double().sum(0), dy.double().abs().sum(0)
     assert ((db.double() - want).abs() <= ref.BF16 * want.abs() + 8 * M ** 0.5 * ref.F32 * size).all()
+
+
+@pytest.mark.parametrize("M", [1, 5, 20, 40])
+def test_weights_beyond_32_bits(M):
+    """Few rows against 4.4 GB of weights: the kernels that read them once, and tiles."""
+    import paper_2605_28691_amd as sk
+
+    K, N = 1 << 22, 520
+    w = _fill(torch.empty(N, K, dtype=torch.bfloat16, device="cuda"), 3)
+    x = torch.randn(M, K, device="cuda").bfloat16()
+    out = sk.skiparse_linear_fwd(x, w)
+    for i in range(0, N, 104):
+        part = w[i : i + 104].double()
+        want, size = x.double() @ part.t(), x.double().abs() @ part.abs().t()
+        assert ((out[:, i : i + 104].double() - want).abs() <= ref.BF16 * want.abs() + (K + 4) * ref.F32 * size).all()
+        # 8 times the root of K roundings, each at most 2^-24 of the sum of sizes at that point
+        assert ((out[:, i : i + 104].double() - want).abs() <= ref.BF16 * want.abs() + 8 * K ** 0.5 * ref.F32 * size).all()

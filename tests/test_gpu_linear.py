@@ -340,12 +340,14 @@ def test_few_rows(M, K, N):
         out, pre = sk.skiparse_linear_fwd(x, w, bias, residual, act=act, keep="bf16")
         z, sums = _check_forward(x, w, bias, residual, act, out)
         _close(pre, z, ref.BF16 * z.abs() + sums, "pre")
-    if M == 4:
-        x4 = x.reshape(1, 4, K)
-        got = sk.skiparse_linear_fwd(x4, w, bias, order="to_sparse", T=1, H=2, W=2, s=2, pattern="token")
-        assert got.shape == (4, 1, N) and torch.equal(got.reshape(4, N), sk.skiparse_linear_fwd(x, w, bias))
-        back = sk.skiparse_linear_fwd(x4.reshape(4, 1, K), w, bias, order="to_original", T=1, H=2, W=2, s=2, pattern="token")
-        assert torch.equal(back.reshape(4, N), got.reshape(4, N))
+    if M in (4, 16, 32):
+        T, H, W = M // 4 if M < 32 else 4, 2, 2 if M < 32 else 4
+        at = dict(T=T, H=H, W=W, s=2, pattern="token")
+        still = sk.skiparse_linear_fwd(x, w, bias)
+        got = sk.skiparse_linear_fwd(x.reshape(1, M, K), w, bias, order="to_sparse", **at)
+        assert got.shape == (4, M // 4, N) and torch.equal(got, ref.moved(still.reshape(1, M, N), "to_sparse", (1, T, H, W), 2, "token"))
+        back = sk.skiparse_linear_fwd(x.reshape(4, M // 4, K), w, bias, order="to_original", **at)
+        assert torch.equal(back, ref.moved(still.reshape(4, M // 4, N), "to_original", (1, T, H, W), 2, "token"))
 
 
 def test_rows_and_channels_at_the_edges_of_all_tiles():
