@@ -380,3 +380,83 @@ def test_wide_tiles(M, N, K):
     if M % 8 == 0:
         x, w, _, _, dy = _inputs(K, N, M, M + 2)  # dw: M x N, summed over K
         _check_backward(dy, x.double(), w, None, "none", *sk.skiparse_linear_bwd(dy, x, w))
+
+
+@pytest.mark.parametrize("skip", [1, 2, 3])
+@pytest.mark.parametrize("M, K, N", [(1, 72, 40), (70, 104, 136), (300, 200, 520)])
+def test_scales_at_any_address(M, K, N, skip):
+    """A checkpoint's scales lie at any address: written by save and by the product, read by load and by the backward pass; and nothing round them is touched."""
+    import paper_2605_28691_amd as sk
+
+    def at(scales):
+        buf = torch.full((scales.numel() + 64,), 0xAB, dtype=torch.uint8, device="cuda")
+        inner = buf[skip : skip + scales.numel()].view(scales.shape)
+        assert inner.data_ptr() % 4 == skip
+        return buf, inner
+
+    def untouched(buf, n):
+        return bool((buf[:skip] == 0xAB).all() and (buf[skip + n :] == 0xAB).all())
+
+    x, w, bias, _, dy = _inputs(M, K, N, M)
+    want = sk.skiparse_checkpoint_save(x)
+    buf, scales = at(want.scales)
+    kept = sk.skiparse_checkpoint_save(x, out=sk.Checkpoint(torch.empty_like(want.codes), scales))
+    assert torch.equal(kept.scales, want.scales) and torch.equal(kept.codes, want.codes) and untouched(buf, scales.numel())
+    assert torch.equal(sk.skiparse_checkpoint_load(kept), sk.skiparse_checkpoint_load(want))
+    out, pre = sk.skiparse_linear_fwd(x, w, bias, act="silu", keep="checkpoint")
+    buf, scales = at(pre.scales)
+    got, odd = sk.skiparse_linear_fwd(x, w, bias, act="silu", keep="checkpoint", pre=sk.Checkpoint(torch.empty_like(pre.codes), scales))
+    assert torch.equal(got, out) and torch.equal(odd.scales, pre.scales) and torch.equal(odd.codes, pre.codes) and untouched(buf, scales.numel())
+    for a, b in zip(sk.skiparse_linear_bwd(dy, want, w, pre=pre, act="silu"), sk.skiparse_linear_bwd(dy, kept, w, pre=odd, act="silu")):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("M, K, N", [(5, 64, 40), (20, 520, 4104), (70, 104, 136), (6566, 2056, 536)])
+def test_what_lies_behind_the_results_is_left_alone(M, K, N):
+    """Results in the middle of larger buffers: bytes in front of them and behind the last row stay, in every form, with everything that the epilogue writes."""
+    import paper_2605_28691_amd as sk
+
+    def room(*shape, dtype=torch.bfloat16):
+        n = 1
+        for d in shape:
+            n *= d
+        buf = torch.full((n + 4096,), 7, dtype=dtype, device="cuda")
+        return buf, buf[2048 : 2048 + n].view(shape)
+
+    def untouched(buf, n):
+        return bool((buf[:2048] == 7).all() and (buf[2048 + n :] == 7).all())
+
+    x, w, bias, residual, dy = _inputs(M, K, N, M)
+    pairs = [room(M, N), room(M, N, dtype=torch.uint8), room(M, -(-N // 32), dtype=torch.uint8), room(M, N), room(M, K), room(N, K), room(N)]
+    out, codes, scales, pre, dx, dw, db = (p[1] for p in pairs)
+    sk.skiparse_linear_fwd(x, w, bias, residual, act="gelu_tanh", keep="checkpoint", out=out, pre=sk.Checkpoint(codes, scales))
+    first = out.clone()
+    sk.skiparse_linear_fwd(x, w, bias, residual, act="gelu_tanh", keep="bf16", out=out, pre=pre)
+    sk.skiparse_linear_bwd(dy, x, w, pre=sk.Checkpoint(codes, scales), act="gelu_tanh", dx=dx, dw=dw, db=db)
+    for buf, t in pairs:
+        assert untouched(buf, t.numel())
+    assert float((first.double() - out.double()).norm()) <= 2 * ref.BF16 * float(out.double().norm())
+
+
+@pytest.mark.parametrize("M, K, N", [(40, 5120, 520), (528, 4008, 3616), (3000, 1536, 1536)])
+def test_workspaces_of_exactly_their_size(M, K, N):
+    """Products that are cut along k, forward and backward, in the bytes that they ask for: nothing behind these is touched, and dirty workspaces give the same results."""
+    import paper_2605_28691_amd as sk
+
+    x, w, bias, residual, dy = _inputs(M, K, N, M)
+    kept = sk.skiparse_checkpoint_save(x)
+    pre = (2 * torch.randn_like(dy.float())).bfloat16()
+    n = sk.skiparse_linear_workspace_bytes(M, K, N)
+    nb = sk.skiparse_linear_bwd_workspace_bytes(M, K, N, act="silu", x_checkpoint=True)
+    assert nb > 0
+    want = sk.skiparse_linear_fwd(x, w, bias, residual), *sk.skiparse_linear_bwd(dy, kept, w, pre=pre, act="silu")
+    for byte in (0xFF, 0x7F):
+        buf = torch.full((max(n, nb) + 4096,), byte, dtype=torch.uint8, device="cuda")
+        got = [sk.skiparse_linear_fwd(x, w, bias, residual, workspace=buf[:n] if n else None)]
+        assert (buf[n:] == byte).all()
+        buf.fill_(byte)
+        got += sk.skiparse_linear_bwd(dy, kept, w, pre=pre, act="silu", workspace=buf[:nb])
+        assert (buf[nb:] == byte).all()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(RuntimeError):
+        sk.skiparse_linear_bwd(dy, kept, w, pre=pre, act="silu", workspace=buf[: nb - 256])
