@@ -1,6 +1,6 @@
 // 8-bit activation checkpoints (format: checkpoint.h): what a training step keeps of a bf16 or float32 tensor until its backward pass, in 33 / 64 of the
 // bytes of bf16.  Bound by HBM bandwidth.  A lane has 8 channels, four lanes a block, whose maximum takes two exchanges between neighbours.
-// (32,760 x 1536 loaded into bf16, 153 MB, 23.3 us; 6426 x 1000 in float32 saved, 32 MB, 8.5.)
+// (80,640 x 5120 of bf16, 1.25 GB: saved in 206 us, loaded in 203, 6.1 TB/s.)
 #include "checkpoint.h"
 #include "kernels.h"
 
@@ -10,9 +10,12 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 constexpr int CKPT_THREADS = 256;
-constexpr int CKPT_UNROLL = 4;  // 8-channel pieces a lane
+// Pieces of 8 channels that a lane saves: few in flight are best but for large tensors (us, 1 / 2 / 4 a lane: 6426 x 1000 in float32 7.1 / 7.2 / 8.5, 3840 x 5120 in bf16 11.6 / 12.2 /
+// 14.1, 32,760 x 1536 30.4 / 29.7 / 34.4, 80,640 x 5120 216 / 201 / 213).  A lane loads one (32,760 x 1536 28.0 / 29.3 / 31.3).
+constexpr uint64_t CKPT_TWO = 1ull << 22;  // from this many pieces on, two a lane
 
 struct CkptArgs {
+    uint64_t first;    // piece that a launch begins with
     uint64_t pieces;   // 8-channel places of all rows, those behind the end of a short last block included
     Div32 per_row;     // of a row: 4 * blocks
     uint32_t cols;
@@ -63,14 +66,14 @@ __device__ inline void store8(float* p, const float (&v)[8]) {
     *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 
-template <typename T, bool RAGGED>
+template <typename T, bool RAGGED, int UNROLL>
 __global__ __launch_bounds__(CKPT_THREADS) void checkpoint_save_kernel(const T* __restrict__ x, unsigned char* __restrict__ codes, unsigned char* __restrict__ scales, CkptArgs a) {
-    const uint64_t first = (uint64_t)blockIdx.x * (CKPT_THREADS * CKPT_UNROLL) + threadIdx.x;
-    float v[CKPT_UNROLL][8];
-    uint64_t elem[CKPT_UNROLL], block[CKPT_UNROLL];
-    bool real[CKPT_UNROLL];
+    const uint64_t first = a.first + (uint64_t)blockIdx.x * (CKPT_THREADS * UNROLL) + threadIdx.x;
+    float v[UNROLL][8];
+    uint64_t elem[UNROLL], block[UNROLL];
+    bool real[UNROLL];
 #pragma unroll
-    for (int u = 0; u < CKPT_UNROLL; u++) {
+    for (int u = 0; u < UNROLL; u++) {
         const uint64_t i = first + u * CKPT_THREADS;
         real[u] = i < a.pieces && piece_at<RAGGED>(a, i, elem[u], block[u]);
 #pragma unroll
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(CKPT_THREADS) void checkpoint_save_kernel(const T* 
         if (real[u]) load8(x + elem[u], v[u]);
     }
 #pragma unroll
-    for (int u = 0; u < CKPT_UNROLL; u++) {
+    for (int u = 0; u < UNROLL; u++) {
         uint32_t m = 0u;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
@@ -101,68 +104,61 @@ __global__ __launch_bounds__(CKPT_THREADS) void checkpoint_save_kernel(const T* 
 
 template <typename T, bool RAGGED>
 __global__ __launch_bounds__(CKPT_THREADS) void checkpoint_load_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales, T* __restrict__ out, CkptArgs a) {
-    const uint64_t first = (uint64_t)blockIdx.x * (CKPT_THREADS * CKPT_UNROLL) + threadIdx.x;
-    u32x2 c[CKPT_UNROLL];
-    uint32_t byte[CKPT_UNROLL];
-    uint64_t elem[CKPT_UNROLL], block;
-    bool real[CKPT_UNROLL];
-#pragma unroll
-    for (int u = 0; u < CKPT_UNROLL; u++) {
-        const uint64_t i = first + u * CKPT_THREADS;
-        real[u] = i < a.pieces && piece_at<RAGGED>(a, i, elem[u], block);
-        if (real[u]) {
-            c[u] = *(const u32x2*)(codes + elem[u]);
-            byte[u] = scales[block];
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < CKPT_UNROLL; u++) {
-        if (!real[u]) continue;
-        const float up = ckpt_up(byte[u]);
-        float lo[4], hi[4];
-        ckpt_values(c[u][0], up, lo);
-        ckpt_values(c[u][1], up, hi);
-        const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        store8(out + elem[u], v);
-    }
+    const uint64_t i = a.first + (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x;
+    uint64_t elem, block;
+    if (i >= a.pieces || !piece_at<RAGGED>(a, i, elem, block)) return;
+    const u32x2 c = *(const u32x2*)(codes + elem);
+    const float up = ckpt_up(scales[block]);
+    float lo[4], hi[4];
+    ckpt_values(c[0], up, lo);
+    ckpt_values(c[1], up, hi);
+    const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    store8(out + elem, v);
 }
 
 static CkptArgs make_args(uint32_t rows, uint32_t cols) {
     const uint32_t blocks = (cols + CKPT_BLOCK - 1u) / CKPT_BLOCK;
-    return {(uint64_t)rows * blocks * 4u, make_div32(blocks * 4u), cols};
+    return {0u, (uint64_t)rows * blocks * 4u, make_div32(blocks * 4u), cols};
 }
 
-template <typename T>
-static hipError_t save_t(const void* x, void* codes, void* scales, const CkptArgs& a, uint32_t blocks, hipStream_t stream) {
-    if (a.cols % CKPT_BLOCK) checkpoint_save_kernel<T, true><<<blocks, CKPT_THREADS, 0, stream>>>((const T*)x, (unsigned char*)codes, (unsigned char*)scales, a);
-    else checkpoint_save_kernel<T, false><<<blocks, CKPT_THREADS, 0, stream>>>((const T*)x, (unsigned char*)codes, (unsigned char*)scales, a);
-    return hipGetLastError();
-}
-template <typename T>
-static hipError_t load_t(const void* codes, const void* scales, void* out, const CkptArgs& a, uint32_t blocks, hipStream_t stream) {
-    if (a.cols % CKPT_BLOCK) checkpoint_load_kernel<T, true><<<blocks, CKPT_THREADS, 0, stream>>>((const unsigned char*)codes, (const unsigned char*)scales, (T*)out, a);
-    else checkpoint_load_kernel<T, false><<<blocks, CKPT_THREADS, 0, stream>>>((const unsigned char*)codes, (const unsigned char*)scales, (T*)out, a);
-    return hipGetLastError();
+// f(arguments, workgroups of `each` pieces) for every launch: a grid has less than 2^32 threads
+template <typename F>
+static hipError_t in_launches(CkptArgs a, uint64_t each, F f) {
+    constexpr uint64_t AT_ONCE = 1ull << 31;
+    for (; a.first < a.pieces; a.first += AT_ONCE) {
+        const uint64_t left = a.pieces - a.first, n = left < AT_ONCE ? left : AT_ONCE;
+        f(a, (uint32_t)((n + each - 1) / each));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
-static bool ckpt_grid(const CkptArgs& a, uint32_t* blocks) {
-    const uint64_t n = (a.pieces + CKPT_THREADS * CKPT_UNROLL - 1) / (CKPT_THREADS * CKPT_UNROLL);
-    *blocks = (uint32_t)n;
-    return fits_grid(n, CKPT_THREADS);
+template <typename T, bool RAGGED>
+static hipError_t save_t(const void* x, void* codes, void* scales, const CkptArgs& all, hipStream_t stream) {
+    const bool two = all.pieces >= CKPT_TWO;
+    return in_launches(all, two ? 2 * CKPT_THREADS : CKPT_THREADS, [&](const CkptArgs& a, uint32_t blocks) {
+        if (two) checkpoint_save_kernel<T, RAGGED, 2><<<blocks, CKPT_THREADS, 0, stream>>>((const T*)x, (unsigned char*)codes, (unsigned char*)scales, a);
+        else checkpoint_save_kernel<T, RAGGED, 1><<<blocks, CKPT_THREADS, 0, stream>>>((const T*)x, (unsigned char*)codes, (unsigned char*)scales, a);
+    });
+}
+template <typename T>
+static hipError_t load_t(const void* codes, const void* scales, void* out, const CkptArgs& all, hipStream_t stream) {
+    return in_launches(all, CKPT_THREADS, [&](const CkptArgs& a, uint32_t blocks) {
+        if (a.cols % CKPT_BLOCK) checkpoint_load_kernel<T, true><<<blocks, CKPT_THREADS, 0, stream>>>((const unsigned char*)codes, (const unsigned char*)scales, (T*)out, a);
+        else checkpoint_load_kernel<T, false><<<blocks, CKPT_THREADS, 0, stream>>>((const unsigned char*)codes, (const unsigned char*)scales, (T*)out, a);
+    });
 }
 
 hipError_t launch_checkpoint_save(const void* x, void* codes, void* scales, uint32_t rows, uint32_t cols, bool f32, hipStream_t stream) {
     const CkptArgs a = make_args(rows, cols);
-    uint32_t blocks;
-    if (!ckpt_grid(a, &blocks)) return hipErrorInvalidConfiguration;
-    return f32 ? save_t<float>(x, codes, scales, a, blocks, stream) : save_t<__bf16>(x, codes, scales, a, blocks, stream);
+    if (cols % CKPT_BLOCK) return f32 ? save_t<float, true>(x, codes, scales, a, stream) : save_t<__bf16, true>(x, codes, scales, a, stream);
+    return f32 ? save_t<float, false>(x, codes, scales, a, stream) : save_t<__bf16, false>(x, codes, scales, a, stream);
 }
 
 hipError_t launch_checkpoint_load(const void* codes, const void* scales, void* out, uint32_t rows, uint32_t cols, bool f32, hipStream_t stream) {
     const CkptArgs a = make_args(rows, cols);
-    uint32_t blocks;
-    if (!ckpt_grid(a, &blocks)) return hipErrorInvalidConfiguration;
-    return f32 ? load_t<float>(codes, scales, out, a, blocks, stream) : load_t<__bf16>(codes, scales, out, a, blocks, stream);
+    return f32 ? load_t<float>(codes, scales, out, a, stream) : load_t<__bf16>(codes, scales, out, a, stream);
 }
 
 }  // namespace skiparse

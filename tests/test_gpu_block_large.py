@@ -104,3 +104,21 @@ def test_weights_beyond_32_bits(M):
         assert ((out[:, i : i + 104].double() - want).abs() <= ref.BF16 * want.abs() + (K + 4) * ref.F32 * size).all()
         # 8 times the root of K roundings, each at most 2^-24 of the sum of sizes at that point
         assert ((out[:, i : i + 104].double() - want).abs() <= ref.BF16 * want.abs() + 8 * K ** 0.5 * ref.F32 * size).all()
+
+
+def test_checkpoints_in_more_than_one_launch():
+    """More places of 8 channels than a launch takes: 9 * 10^8 rows of 8 channels, whose blocks of 32 are a quarter full."""
+    import paper_2605_28691_amd as sk
+
+    rows = 900_000_001
+    x = torch.empty(rows, 8, dtype=torch.bfloat16, device="cuda")
+    x.copy_(torch.linspace(-3, 3, 8, device="cuda").bfloat16().expand_as(x))
+    x[::3] *= 0.25
+    kept = sk.skiparse_checkpoint_save(x)
+    at = torch.cat([torch.arange(i - 3, i + 3, device="cuda") for i in (3, 1 << 29, 1 << 28, 3 << 28, rows - 3)])  # 4 places a row: 2^31 of them are 2^29 rows
+    codes, scales, values = ref.checkpoint(x[at].double())
+    assert torch.equal(kept.codes[at], codes) and torch.equal(kept.scales[at], scales)
+    got = sk.skiparse_checkpoint_load(kept)
+    assert torch.equal(got[at].double(), values)
+    assert bool((kept.scales[::3] == kept.scales[0]).all() and (kept.scales[1::3] == kept.scales[1]).all() and (kept.scales[2::3] == kept.scales[1]).all())
+    assert torch.equal(got[2::3], got[1:2].expand_as(got[2::3])) and torch.equal(got[::3], got[:1].expand_as(got[::3]))
