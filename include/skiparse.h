@@ -238,6 +238,8 @@ enum { SKIPARSE_ORDER_SAME = 0, SKIPARSE_ORDER_TO_SPARSE = 1, SKIPARSE_ORDER_TO_
  *                           axis' trained places (YaRN's "NTK-by-parts")
  *   cos and sin are multiplied by `attention` (1, or YaRN's correction of the logits).  Angles are formed in 64 bits.  factor >= 1, fast > slow, trained >= 1 for
  *   YaRN; theta > 0; at most 512 channels an axis.
+ * skiparse_rope_table_ex: the same with arguments in 64 bits.  A factor such as 1.3 is none of the 32-bit numbers, and the nearest of them turns place 131,072 by 4e-3 too much or too little:
+ *   what skiparse_rope_table is given is taken as it is, so it is for numbers that 32 bits hold.
  * skiparse_rope: q and, if k is not NULL, k (same shape) -> q_out, k_out.  len_t, len_h, len_w: the table's places; t0, h0, w0: where the grid begins in them
  *   (t0 + T <= len_t for an axis with channels, as when frames follow others).  inverse = 1 turns back and is the gradient: (dq, dk) -> gradients in front of the rotation,
  *   with `order` the other way round.  Where rows keep their places q_out may be q, and k_out k; nothing else may overlap.  dtype bf16 or float32; head_dim a multiple of 8 up to 512.
@@ -248,6 +250,8 @@ enum { SKIPARSE_ROPE_PLAIN = 0, SKIPARSE_ROPE_LINEAR = 1, SKIPARSE_ROPE_NTK = 2,
 size_t skiparse_rope_table_bytes(int T, int H, int W, int rt, int rh, int rw);
 int skiparse_rope_table(float* table, int T, int H, int W, int rt, int rh, int rw, float theta, int scaling, float factor_t, float factor_h, float factor_w,
                         int trained_t, int trained_h, int trained_w, float fast, float slow, float attention, void* stream);
+int skiparse_rope_table_ex(float* table, int T, int H, int W, int rt, int rh, int rw, double theta, int scaling, double factor_t, double factor_h, double factor_w,
+                           int trained_t, int trained_h, int trained_w, double fast, double slow, double attention, void* stream);
 int skiparse_rope(const void* q, const void* k, void* q_out, void* k_out, const float* table, int B, int heads, int T, int H, int W, int head_dim, int rt, int rh,
                   int rw, int len_t, int len_h, int len_w, int t0, int h0, int w0, int s, int pattern, int order, int layout, int inverse, int dtype, void* stream);
 

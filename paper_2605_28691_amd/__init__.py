@@ -49,7 +49,7 @@ def lib() -> ctypes.CDLL:
                 f"{_LIB_PATH} is missing: build it first (python -m paper_2605_28691_amd.build); there is no fallback path"
             )
         L = ctypes.CDLL(_LIB_PATH)
-        i, vp, f, u, sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_float, ctypes.c_uint, ctypes.c_size_t
+        i, vp, f, d, u, sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_float, ctypes.c_double, ctypes.c_uint, ctypes.c_size_t
         L.skiparse_permute.restype = i
         L.skiparse_permute.argtypes = [vp, vp] + [i] * 9 + [vp]
         L.skiparse_unpermute.restype = i
@@ -98,6 +98,8 @@ def lib() -> ctypes.CDLL:
         L.skiparse_rope_table_bytes.argtypes = [i] * 6
         L.skiparse_rope_table.restype = i
         L.skiparse_rope_table.argtypes = [vp] + [i] * 6 + [f, i] + [f] * 3 + [i] * 3 + [f] * 3 + [vp]
+        L.skiparse_rope_table_ex.restype = i
+        L.skiparse_rope_table_ex.argtypes = [vp] + [i] * 6 + [d, i] + [d] * 3 + [i] * 3 + [d] * 3 + [vp]
         L.skiparse_rope.restype = i
         L.skiparse_rope.argtypes = [vp] * 5 + [i] * 21 + [vp]
         L.skiparse_checkpoint_save.restype = i
@@ -167,7 +169,7 @@ _TENSORS = {
     "skiparse_attn_bwd_static": (*_QKVO, (4, "dout"), (5, "lse"), (6, "dq"), (7, "dk"), (8, "dv")),
     "skiparse_quantize_fp8_ex": ((0, "x"), (1, "x8"), (2, "scales")),
     "skiparse_attn_fwd_fp8_ex": ((0, "q8"), (1, "k8"), (2, "v8"), (3, "sq"), (4, "sk"), (5, "sv"), (6, "out")),
-    "skiparse_rope_table": ((0, "table"),),
+    "skiparse_rope_table_ex": ((0, "table"),),
     "skiparse_rope": ((0, "q"), (1, "k"), (2, "q_out"), (3, "k_out"), (4, "table")),
     "skiparse_checkpoint_save": ((0, "x"), (1, "codes"), (2, "scales")),
     "skiparse_checkpoint_load": ((0, "codes"), (1, "scales"), (2, "out")),
@@ -495,8 +497,8 @@ def skiparse_rope_table(lengths, axes, theta: float = 10000.0, scaling: str = "n
     _here(out)
     ft, fh, fw = _triple(factor)
     nt, nh, nw = _triple(trained)
-    _skiparse_rope_table(out, T, H, W, rt, rh, rw, float(theta), ROPE_SCALINGS[scaling], float(ft), float(fh), float(fw), nt, nh, nw, float(fast), float(slow),
-                         float(attention), _stream())
+    _skiparse_rope_table_ex(out, T, H, W, rt, rh, rw, float(theta), ROPE_SCALINGS[scaling], float(ft), float(fh), float(fw), nt, nh, nw, float(fast),
+                            float(slow), float(attention), _stream())
     return RopeTable(out, (T, H, W), (rt, rh, rw))
 
 

@@ -560,14 +560,19 @@ size_t skiparse_rope_table_bytes(int T, int H, int W, int rt, int rh, int rw) { 
 
 int skiparse_rope_table(float* table, int T, int H, int W, int rt, int rh, int rw, float theta, int scaling, float factor_t, float factor_h, float factor_w,
                         int trained_t, int trained_h, int trained_w, float fast, float slow, float attention, void* stream) {
+    return skiparse_rope_table_ex(table, T, H, W, rt, rh, rw, theta, scaling, factor_t, factor_h, factor_w, trained_t, trained_h, trained_w, fast, slow, attention, stream);
+}
+
+int skiparse_rope_table_ex(float* table, int T, int H, int W, int rt, int rh, int rw, double theta, int scaling, double factor_t, double factor_h, double factor_w,
+                           int trained_t, int trained_h, int trained_w, double fast, double slow, double attention, void* stream) {
     if (!table || misaligned(table)) return SKIPARSE_EINVAL;
-    if (T < 1 || H < 1 || W < 1 || rt < 0 || rh < 0 || rw < 0 || (rt | rh | rw) % 2 != 0 || rt + rh + rw == 0) return SKIPARSE_EINVAL;
+    if (T < 1 || H < 1 || W < 1 || rt < 0 || rh < 0 || rw < 0 || (rt | rh | rw) % 2 != 0 || (rt | rh | rw) == 0) return SKIPARSE_EINVAL;
     if (rt > 2 * (int)ROPE_MAX_PAIRS || rh > 2 * (int)ROPE_MAX_PAIRS || rw > 2 * (int)ROPE_MAX_PAIRS) return SKIPARSE_EUNSUPPORTED;
     if (rope_pairs(T, H, W, rt, rh, rw) == 0) return SKIPARSE_ESHAPE;
     if (scaling < SKIPARSE_ROPE_PLAIN || scaling > SKIPARSE_ROPE_YARN) return SKIPARSE_EINVAL;
-    const float limit = 3.0e38f;  // not finite, or not a number: refused
-    if (!(theta > 0.f && theta < limit) || !(attention > -limit && attention < limit)) return SKIPARSE_EINVAL;
-    const float factor[3] = {factor_t, factor_h, factor_w};
+    const double limit = 3.0e38;  // not finite, or not a number: refused
+    if (!(theta > 0. && theta < limit) || !(attention > -limit && attention < limit)) return SKIPARSE_EINVAL;
+    const double factor[3] = {factor_t, factor_h, factor_w};
     const int trained[3] = {trained_t, trained_h, trained_w}, r[3] = {rt, rh, rw}, len[3] = {T, H, W};
     RopeAxis axis[3] = {};
     for (int i = 0; i < 3; i++) {
@@ -576,11 +581,11 @@ int skiparse_rope_table(float* table, int T, int H, int W, int rt, int rh, int r
         axis[i].factor = factor[i];
         axis[i].trained = (uint32_t)trained[i];
         if (scaling == SKIPARSE_ROPE_PLAIN || r[i] == 0) continue;
-        if (!(factor[i] >= 1.f && factor[i] < limit)) return SKIPARSE_EINVAL;
+        if (!(factor[i] >= 1. && factor[i] < limit)) return SKIPARSE_EINVAL;
         if (scaling == SKIPARSE_ROPE_YARN && trained[i] < 1) return SKIPARSE_EINVAL;
     }
     if (scaling == SKIPARSE_ROPE_YARN && !(fast > slow && fast < limit && slow > -limit)) return SKIPARSE_EINVAL;
-    const RopeScaling sc = {scaling, theta, fast, slow, attention};
+    const RopeScaling sc = {scaling, theta, fast, slow, (float)attention};  // the last one multiplies what is stored in 32 bits
     return finish(launch_rope_table(table, axis[0], axis[1], axis[2], sc, (hipStream_t)stream));
 }
 

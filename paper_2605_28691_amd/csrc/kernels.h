@@ -179,14 +179,15 @@ constexpr uint32_t ROPE_MAX_PAIRS = 256;
 enum RopeScale : int { ROPE_PLAIN = 0, ROPE_LINEAR = 1, ROPE_NTK = 2, ROPE_YARN = 3 };
 struct RopeAxis {
     uint32_t len, r;      // places, channels
-    float factor;
+    double factor;
     uint32_t trained;     // places that the model was trained on
     uint32_t first, blocks;  // set by the launcher: first entry, workgroups
     Div32 pairs;
 };
 struct RopeScaling {
     int kind;
-    float theta, fast, slow, attention;
+    double theta, fast, slow;
+    float attention;
 };
 hipError_t launch_rope_table(float* table, RopeAxis t, RopeAxis h, RopeAxis w, const RopeScaling& s, hipStream_t stream);
 

@@ -63,6 +63,14 @@ struct Arg<float> {
         return true;
     }
 };
+template <>
+struct Arg<double> {
+    static bool get(PyObject* o, double& v) {
+        if (!PyFloat_CheckExact(o)) return false;
+        v = PyFloat_AS_DOUBLE(o);
+        return true;
+    }
+};
 template <typename P>
 struct Arg<P*> {
     static bool get(PyObject* o, P*& v) {
@@ -170,7 +178,7 @@ constexpr unsigned at(int i, I... more) { return 1u << i | at(more...); }
     X(skiparse_attn_bwd_static, NEVER) \
     X(skiparse_quantize_fp8_ex, NEVER) \
     X(skiparse_attn_fwd_fp8_ex, NEVER) \
-    X(skiparse_rope_table, NEVER) \
+    X(skiparse_rope_table_ex, NEVER) \
     X(skiparse_rope, at(1, 3)) \
     X(skiparse_checkpoint_save, NEVER) \
     X(skiparse_checkpoint_load, NEVER) \

@@ -278,16 +278,16 @@ hipError_t launch_rope(const RopeArgs& r, hipStream_t stream) {
 // Frequency of pair j of an axis of r channels, in turns (2 pi) a place.
 __device__ inline double rope_turns(const RopeAxis& x, const RopeScaling& s, uint32_t j) {
     const double r = (double)x.r;
-    double base = (double)s.theta;
-    if (s.kind == ROPE_NTK && x.r > 2) base *= pow((double)x.factor, r / (r - 2.0));
+    double base = s.theta;
+    if (s.kind == ROPE_NTK && x.r > 2) base *= pow(x.factor, r / (r - 2.0));
     double f = pow(base, -2.0 * (double)j / r) * 0.15915494309189533577;  // 1 / (2 pi)
-    if (s.kind == ROPE_LINEAR) f /= (double)x.factor;
+    if (s.kind == ROPE_LINEAR) f /= x.factor;
     if (s.kind == ROPE_YARN) {
         // by how often the pair turns within the trained length: often -> as it is, seldom -> stretched, linear in between (YaRN, "NTK-by-parts")
         const double turns = (double)x.trained * f;
-        double g = (turns - (double)s.slow) / ((double)s.fast - (double)s.slow);
+        double g = (turns - s.slow) / (s.fast - s.slow);
         g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
-        f = f * g + f / (double)x.factor * (1.0 - g);
+        f = f * g + f / x.factor * (1.0 - g);
     }
     return f;
 }
