@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import importlib
+import operator
 import os
 from typing import NamedTuple
 
@@ -186,17 +187,41 @@ _OPTIONAL = {
 }
 
 
+# What an integer argument holds.  ctypes cuts a larger one to it without a word, so that 2^32 + 1 rows would be one row.
+_RANGES = {ctypes.c_int: (-(1 << 31), 1 << 31), ctypes.c_uint: (0, 1 << 32), ctypes.c_size_t: (0, 1 << 64)}
+
+
+def _fit(name: str, types, args) -> None:
+    for i, (t, a) in enumerate(zip(types, args)):
+        if t in _RANGES:
+            try:
+                n = operator.index(a)
+            except TypeError:  # no integer: the call says so
+                continue
+            if not _RANGES[t][0] <= n < _RANGES[t][1]:
+                raise ValueError(f"{name}: argument {i}, {n}, does not fit the {8 * ctypes.sizeof(t)} bits that the library has for it")
+
+
+def _size(name: str, *sizes) -> int:
+    """A number of bytes that the library computes."""
+    f = getattr(lib(), name)
+    _fit(name, f.argtypes, sizes)
+    return int(f(*sizes))
+
+
 def _failed(code: int, name: str) -> None:
     _check(code, name.removesuffix("_ex"))
 
 
 def _general(name: str, *args) -> None:
     """The call by way of ctypes, which takes every integer-like argument and names what it refuses."""
+    f = getattr(lib(), name)
+    _fit(name, f.argtypes, args)
     args = list(args)
     for i, what in _TENSORS[name]:
         if not (args[i] is None and i in _OPTIONAL.get(name, ())):
             args[i] = _dev(args[i], what)
-    _failed(getattr(lib(), name)(*args), name)
+    _failed(f(*args), name)
 
 
 # The entry points themselves: by ctypes until the library is opened, then natively marshalled where there is a module for this Python and
@@ -309,7 +334,7 @@ def dense_attn_fwd(q, k, v, T: int, H: int, W: int, scale: float = 0.0, out: tor
 
 
 def skiparse_workspace_bytes(B, heads, T, H, W, D, s, fused: bool) -> int:
-    return int(lib().skiparse_workspace_bytes(B, heads, T, H, W, D, s, BF16, FUSED if fused else 0))
+    return _size("skiparse_workspace_bytes", B, heads, T, H, W, D, s, BF16, FUSED if fused else 0)
 
 
 def skiparse_attn_fwd(q, k, v, T: int, H: int, W: int, s: int, pattern: str, scale: float = 0.0, fused: bool = True,
@@ -354,7 +379,7 @@ _INTS = (int,) * 9
 
 @functools.lru_cache(maxsize=256)
 def _bytes_of_ints(name: str, *sizes: int) -> int:
-    return int(getattr(lib(), name)(*sizes))
+    return _size(name, *sizes)
 
 
 def _bytes(name: str, *sizes) -> int:
@@ -362,7 +387,7 @@ def _bytes(name: str, *sizes) -> int:
     own value, while a one-element tensor is looked up by identity and may change, and 8.0, which the call refuses, is found under 8."""
     if tuple(map(type, sizes)) == _INTS:
         return _bytes_of_ints(name, *sizes)
-    return int(getattr(lib(), name)(*sizes))
+    return _size(name, *sizes)
 
 
 def skiparse_lse_shape(B, heads, T, H, W, D, s, pattern: str, pad: bool = False):
@@ -503,7 +528,7 @@ def skiparse_rope_table(lengths, axes, theta: float = 10000.0, scaling: str = "n
 
 
 def _table_bytes(T, H, W, rt, rh, rw) -> int:
-    n = int(lib().skiparse_rope_table_bytes(T, H, W, rt, rh, rw))
+    n = _size("skiparse_rope_table_bytes", T, H, W, rt, rh, rw)
     if n == 0:
         raise ValueError("lengths are positive, channels even, and a table has less than 2^31 pairs")
     return n
@@ -634,7 +659,7 @@ def skiparse_linear_fwd(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | N
 
 @functools.lru_cache(maxsize=256)
 def _space_bytes(name: str, *sizes: int) -> int:
-    return int(getattr(lib(), name)(*sizes))
+    return _size(name, *sizes)
 
 
 def _space(workspace, like, name: str, *sizes):
@@ -646,11 +671,11 @@ def _space(workspace, like, name: str, *sizes):
 
 
 def skiparse_linear_workspace_bytes(rows: int, in_features: int, out_features: int) -> int:
-    return int(lib().skiparse_linear_workspace_bytes(rows, in_features, out_features))
+    return _size("skiparse_linear_workspace_bytes", rows, in_features, out_features)
 
 
 def skiparse_linear_bwd_workspace_bytes(rows: int, in_features: int, out_features: int, order: str = "same", act: str = "none", x_checkpoint: bool = False) -> int:
-    return int(lib().skiparse_linear_bwd_workspace_bytes(rows, in_features, out_features, ORDERS[order], ACTS[act], 1 if x_checkpoint else 0))
+    return _size("skiparse_linear_bwd_workspace_bytes", rows, in_features, out_features, ORDERS[order], ACTS[act], 1 if x_checkpoint else 0)
 
 
 def skiparse_linear_bwd(dy: torch.Tensor, x, w: torch.Tensor, pre=None, act: str = "none", order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1,

@@ -5,7 +5,7 @@
 // launch (a fill of a tensor by torch, one launch as well, takes 4.0), the result's tensor 1.1 and the checks and look-ups in Python 0.5.  By way of ctypes, with
 // an address asked for tensor by tensor in Python, the call took 2 us more.  Here an argument costs nanoseconds.
 //
-// Only plain arguments are taken: torch.Tensor itself, on the GPU and contiguous, int and float themselves.  With anything else, and to turn a
+// Only plain arguments are taken: torch.Tensor itself, on the GPU and contiguous, int itself within the range of the C type, float itself.  With anything else, and to turn a
 // code into an exception, the module calls the functions that the binding has given it, so that what those accept, refuse and raise does not
 // depend on this module.
 //
@@ -35,24 +35,30 @@ template <>
 struct Arg<int> {
     static bool get(PyObject* o, int& v) {
         if (!PyLong_CheckExact(o)) return false;
-        v = (int)PyLong_AsUnsignedLongMask(o);  // as ctypes does, without a range check
-        return true;
+        int over;
+        const long n = PyLong_AsLongAndOverflow(o, &over);
+        v = (int)n;
+        return over == 0 && v == n;
     }
 };
 template <>
 struct Arg<unsigned> {
     static bool get(PyObject* o, unsigned& v) {
         if (!PyLong_CheckExact(o)) return false;
-        v = (unsigned)PyLong_AsUnsignedLongMask(o);
-        return true;
+        int over;
+        const long n = PyLong_AsLongAndOverflow(o, &over);
+        v = (unsigned)n;
+        return over == 0 && (long)v == n;
     }
 };
 template <>
 struct Arg<size_t> {
     static bool get(PyObject* o, size_t& v) {
         if (!PyLong_CheckExact(o)) return false;
-        v = (size_t)PyLong_AsUnsignedLongLongMask(o);
-        return true;
+        int over;
+        const long n = PyLong_AsLongAndOverflow(o, &over);
+        v = (size_t)n;
+        return over == 0 && n >= 0;
     }
 };
 template <>

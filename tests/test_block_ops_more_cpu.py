@@ -28,3 +28,37 @@ def test_rope_table_takes_its_base_and_factors_in_64_bits():
         assert call(**bad) == EINVAL, bad
     # channels whose sum passes 31 bits
     assert call(r=(2147483646, 2147483646, 2147483646)) == EUNSUPPORTED
+
+
+def test_integers_beyond_the_c_types_are_refused(monkeypatch):
+    """2^32 + 1 rows are not one row: what a C type does not hold is refused, by the calls and by the functions of sizes, and not cut."""
+    meta = lambda *s, dtype=torch.bfloat16: torch.empty(s, dtype=dtype, device="meta")  # noqa: E731
+    monkeypatch.setattr(sk, "_stream", lambda: 0)
+    monkeypatch.setattr(sk, "_here", lambda *t: None)
+    for rows in ((1 << 32) + 1, 1 << 31, (1 << 32) + 128):
+        x, w = meta(rows, 8), meta(16, 8)
+        with pytest.raises(ValueError, match="does not fit the 32 bits"):
+            sk.skiparse_checkpoint_save(x)
+        with pytest.raises(ValueError, match="does not fit the 32 bits"):
+            sk.skiparse_checkpoint_load(sk.Checkpoint(meta(rows, 8, dtype=torch.uint8), meta(rows, 1, dtype=torch.uint8)))
+        with pytest.raises(ValueError, match="does not fit the 32 bits"):
+            sk.skiparse_linear_fwd(x, w)
+        with pytest.raises(ValueError, match="does not fit the 32 bits"):
+            sk.skiparse_linear_bwd(meta(rows, 16), x, w)
+        for f in (sk.skiparse_linear_workspace_bytes, sk.skiparse_linear_bwd_workspace_bytes):
+            with pytest.raises(ValueError, match="does not fit the 32 bits"):
+                f(rows, 5120, 5120)
+        with pytest.raises(ValueError, match="does not fit the 32 bits"):
+            sk.skiparse_rope_table((1, 1, rows), (0, 0, 8), device="meta")
+        with pytest.raises(ValueError, match="does not fit the 32 bits"):
+            sk.skiparse_workspace_bytes(rows, 1, 1, 8, 8, 64, 2, False)
+        with pytest.raises(ValueError, match="does not fit the 32 bits"):
+            sk.skiparse_lse_shape(rows, 1, 1, 8, 8, 64, 2, "token")
+    table = sk.RopeTable(meta(2 * 16 * 4, dtype=torch.float32), (1, 1, 16), (0, 0, 8))
+    q = meta(1, 4, 1, 8)
+    with pytest.raises(ValueError, match="does not fit the 32 bits"):
+        sk.skiparse_rope(q, None, table, 1, 1, 4, at=(0, 0, 1 << 32))
+    with pytest.raises(ValueError, match="does not fit the 64 bits"):  # bytes of a workspace
+        sk._general("skiparse_linear_fwd", q, q, None, None, q, None, None, 1, 1, 1, 4, 8, 8, 1, 0, 0, 0, 0, None, -1, 0)
+    with pytest.raises(ctypes.ArgumentError):  # no integer
+        sk.skiparse_linear_workspace_bytes(4.0, 8, 8)
