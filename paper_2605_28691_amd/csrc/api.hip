@@ -8,6 +8,7 @@
 #include <mutex>
 
 #include "kernels.h"
+#include "linear_plan.h"
 
 using namespace skiparse;
 
@@ -702,6 +703,7 @@ int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const vo
     for (const void* p : {x, w, bias, residual, (const void*)out, (const void*)pre})
         if (p && misaligned(p)) return SKIPARSE_EINVAL;
     const size_t K = (size_t)in_features, N = (size_t)out_features;
+    if (!linear_fits(rows, N)) return SKIPARSE_ESHAPE;
     if (moved && rows * K * 2 >= (1ull << 32) - 64) return SKIPARSE_ESHAPE;  // rows that move are addressed with 32-bit byte offsets
     const Span sx = {x, rows * K * 2}, sw = {w, N * K * 2}, sb = {bias, N * 2}, so = {out, rows * N * 2};
     const Span sp = {pre, rows * N * (pre_scales ? 1 : 2)}, ss = {pre_scales, checkpoint_scales(rows, N)}, sr = {residual, rows * N * 2};
@@ -731,7 +733,7 @@ static LinearBwdSpace linear_bwd_space(size_t rows, size_t K, size_t N, bool dz,
     LinearBwdSpace l;
     l.dz = dz ? align256(rows * N * 2) : 0;
     l.x = x ? align256(rows * K * 2) : 0;
-    l.db = db ? align256((size_t)linear_rows_parts((uint32_t)rows) * N * sizeof(float)) : 0;
+    l.db = db ? align256((size_t)linear_rows_parts((uint32_t)rows, (uint32_t)N) * N * sizeof(float)) : 0;
     const size_t px = dx ? linear_workspace(LINEAR_DX, (uint32_t)rows, (uint32_t)K, (uint32_t)N) : 0, pw = dw ? linear_workspace(LINEAR_DW, (uint32_t)N, (uint32_t)K, (uint32_t)rows) : 0;
     l.parts = px > pw ? px : pw;  // one product after the other
     l.total = l.dz + l.x + l.db + l.parts;
@@ -758,6 +760,7 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
     if (!dw) x = x_scales = nullptr;
     if (!dx) w = nullptr;
     const size_t K = (size_t)in_features, N = (size_t)out_features;
+    if ((dx && !linear_fits(rows, K)) || (dw && !linear_fits(N, K))) return SKIPARSE_ESHAPE;  // before the first launch: a call that is refused has written nothing
     const LinearBwdSpace l = linear_bwd_space(rows, K, N, (dx || dw) && (moved || act != SKIPARSE_ACT_NONE), x_scales != nullptr, db != nullptr, dx != nullptr, dw != nullptr);
     if (l.total && (!workspace || workspace_bytes < l.total || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
     const Span sy = {dy, rows * N * 2}, sx = {x, rows * K * (x_scales ? 1 : 2)}, sxs = {x_scales, checkpoint_scales(rows, K)}, sw = {w, N * K * 2};

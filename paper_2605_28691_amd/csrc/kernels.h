@@ -221,14 +221,13 @@ struct LinearRowsArgs {
     const void* pre;         // null: no activation; bf16, or codes with pre_scales
     const void* pre_scales;
     void* dz;                // bf16 [rows][N] in the input's order, or null
-    float* db_part;          // [linear_rows_parts()][N], or null
+    float* db_part;          // [linear_rows_parts(M, N)][N], or null
     void* db;                // bf16 [N]
     uint32_t M, N;
     int act;
     int order;               // from the output's order back to the input's
     RowArgs rows;
 };
-uint32_t linear_rows_parts(uint32_t M);
 hipError_t launch_linear_rows(const LinearRowsArgs& a, hipStream_t stream);
 
 }  // namespace skiparse

@@ -19,6 +19,7 @@ struct LinearTile {
 constexpr uint32_t LINEAR_CUS = 256;
 constexpr uint32_t LINEAR_STEP = 64, LINEAR_STEPS = 2 * LINEAR_STEP;  // k is walked in pairs of steps
 constexpr uint32_t LINEAR_MAX_PARTS = 16;
+constexpr uint64_t LINEAR_GRID = 1ull << 24;  // a launch has fewer workgroups of 256: a grid, fewer than 2^32 threads
 // Fitted to products of 28 sizes (1 to 32,760 rows, 256 to 20,480 channels, the three forms), each with every tile and several numbers of parts: over the last 36 of them what the
 // rule takes is 1 % slower than the best in the mean, 9 % at most.  For example, us, 256 / 128 / 64 / 128 x 256, uncut: 8190 x 1536 -> 1536 36 / 43 / 60 / 48, dx of
 // 6426 x 1000 -> 4008 82 / 71 / 120 / 53 (408 tiles of 128 are 80 % of a round of two a CU, 204 of 128 x 256 of a round of one; 256 x 128 64), 1000 x 2048 -> 2048
@@ -40,6 +41,21 @@ struct LinearPlan {
     size_t workspace() const { return parts > 1 ? (size_t)rest * parts * LINEAR_TILE[shape].m * LINEAR_TILE[shape].n * 4u : 0u; }
 };
 
+// Whether a result of M x N can be written by one launch: by the largest tiles, uncut, if at all.
+inline bool linear_fits(uint64_t M, uint64_t N) { return ((M + 255u) / 256u) * ((N + 255u) / 256u) < LINEAR_GRID; }
+
+// Rows of a part of the pass in front of the backward's products, 256 channels a workgroup.  Small problems need the workgroups, large ones' parts would cost traffic: 4 bytes written
+// and read of every 32 rows' 64 and more; beyond that as many as fit one launch.
+inline uint32_t linear_rows_per_part(uint32_t M, uint32_t N) {
+    uint32_t per = M < 32768u ? 32u : 128u;
+    while (((uint64_t)M + per - 1u) / per * (((uint64_t)N + 255u) / 256u) >= LINEAR_GRID) per *= 2u;
+    return per;
+}
+inline uint32_t linear_rows_parts(uint32_t M, uint32_t N) {
+    const uint32_t per = linear_rows_per_part(M, N);
+    return (uint32_t)(((uint64_t)M + per - 1u) / per);
+}
+
 // The last round of workgroups over the CUs is seldom full: its tiles are cut along k, into as many parts as make it shortest.
 inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K) {
     LinearPlan best = {};
@@ -55,6 +71,7 @@ inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K) {
             const uint32_t per = (pairs + parts - 1u) / parts;
             if (parts > 1 && (uint64_t)(parts - 1u) * per >= pairs) continue;  // the last part would be empty
             const uint64_t units = rest * parts, again = units / slots, left = units - again * slots;
+            if (tiles - rest + units >= LINEAR_GRID) break;
             float cost = (float)rounds * (t.fixed + 2.f * (float)pairs * full) + (float)again * (t.fixed + 2.f * (float)per * full);
             if (left) cost += t.fixed + 2.f * (float)per * linear_step(t, left);
             if (parts > 1) cost += LINEAR_JOIN + LINEAR_JOIN_BYTE * (float)(units * t.m * t.n * 4u);

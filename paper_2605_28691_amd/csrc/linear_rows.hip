@@ -8,6 +8,7 @@
 #include "checkpoint.h"
 #include "kernels.h"
 #include "linear_act.h"
+#include "linear_plan.h"
 
 namespace skiparse {
 
@@ -16,10 +17,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 
 constexpr uint32_t LANES_X = 32, COLS = LANES_X * 8, ROWS_AT_ONCE = 256 / LANES_X;
-// Small problems need the workgroups, large ones' parts would cost traffic: 4 bytes written and read of every 32 rows' 64 and more.
-static uint32_t rows_per_part(uint32_t M) { return M < 32768u ? 32u : 128u; }
-
-uint32_t linear_rows_parts(uint32_t M) { return (M + rows_per_part(M) - 1u) / rows_per_part(M); }
+static_assert(COLS == 256, "what linear_rows_per_part() counts on");
 
 __device__ inline void unpack8(const u32x4& x, float (&v)[8]) {
 #pragma unroll
@@ -107,9 +105,9 @@ __global__ __launch_bounds__(1024) void linear_db_kernel(const float* __restrict
 }
 
 hipError_t launch_linear_rows(const LinearRowsArgs& a, hipStream_t stream) {
-    const uint32_t col_blocks = (a.N + COLS - 1u) / COLS, parts = linear_rows_parts(a.M);
+    const uint32_t col_blocks = (a.N + COLS - 1u) / COLS, parts = linear_rows_parts(a.M, a.N);
     if (!fits_grid((uint64_t)col_blocks * parts, 256u)) return hipErrorInvalidConfiguration;
-    const uint32_t per = rows_per_part(a.M);
+    const uint32_t per = linear_rows_per_part(a.M, a.N);
     if (a.pre == nullptr) linear_rows_kernel<false, false><<<col_blocks * parts, 256, 0, stream>>>(a, col_blocks, per);
     else if (a.pre_scales == nullptr) linear_rows_kernel<true, false><<<col_blocks * parts, 256, 0, stream>>>(a, col_blocks, per);
     else linear_rows_kernel<true, true><<<col_blocks * parts, 256, 0, stream>>>(a, col_blocks, per);

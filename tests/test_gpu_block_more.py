@@ -35,3 +35,37 @@ def test_integers_beyond_the_c_types_do_not_reach_the_library():
     for flags in (-1, 1 << 32):
         with pytest.raises(ValueError, match="does not fit the 32 bits"):
             sk._skiparse_attn_fwd(q, q, q, torch.empty_like(q), 1, 1, 1, 2, 2, 64, 2, 0, 0.0, 0, flags, None, 0, sk._stream())
+
+
+def test_more_rows_than_small_tiles_fit_a_grid():
+    """2^30 + 5 rows of 8 channels: 2^24 tiles of 64 rows, and more, are not a launch; larger tiles are.  All rows are looked at, 17 GB a tensor."""
+    import paper_2605_28691_amd as sk
+
+    M, step = (1 << 30) + 5, 1 << 25
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, dy = (torch.empty(M, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (x, dy):
+        for i in range(0, M, step):
+            t[i : i + step] = torch.randn(min(step, M - i), 8, generator=g, device="cuda")
+    w = torch.randn(8, 8, generator=g, device="cuda").bfloat16()
+    w64 = w.double()
+    close = lambda got, want, size: bool(((got.double() - want).abs() <= ref.BF16 * want.abs() + 12 * ref.F32 * size).all())  # noqa: E731
+    out = sk.skiparse_linear_fwd(x, w)
+    for i in range(0, M, step):
+        a = x[i : i + step].double()
+        assert close(out[i : i + step], a @ w64.t(), a.abs() @ w64.abs().t()), i
+    del out
+    dx, dw, db = sk.skiparse_linear_bwd(dy, x, w)
+    sums = [torch.zeros(8, 8, dtype=torch.float64, device="cuda") for _ in range(2)] + [torch.zeros(8, dtype=torch.float64, device="cuda") for _ in range(2)]
+    for i in range(0, M, step):
+        a, b = dy[i : i + step].double(), x[i : i + step].double()
+        assert close(dx[i : i + step], a @ w64, a.abs() @ w64.abs()), i
+        for n in range(8):  # one channel of dy at a time: as a product of 2^25 terms an element it is the library's slowest
+            v = a[:, n : n + 1] * b
+            sums[0][n] += v.sum(0)
+            sums[1][n] += v.abs_().sum(0)
+        sums[2] += a.sum(0)
+        sums[3] += a.abs_().sum(0)
+    # at most M roundings of partial sums, each at most 2^-24 of the sum of sizes, in any direction: 8 times the root of their number
+    for got, want, size in ((dw, *sums[:2]), (db, *sums[2:])):
+        assert ((got.double() - want).abs() <= ref.BF16 * want.abs() + 8 * M ** 0.5 * ref.F32 * size).all()
