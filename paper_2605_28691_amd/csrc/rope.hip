@@ -25,6 +25,7 @@ constexpr int ROPE_ITERS = 5;
 constexpr uint64_t ROPE_MIN_WAVES = 16384;
 // Tensors beyond this pass by the caches: what is smaller is still there when the next kernel reads it (us, cached / past: 110 MB moved 21.4 / 27.9, 400 MB 79.0 / 70.3, 1.6 GB 634 / 596).
 constexpr uint64_t ROPE_CACHED_BYTES = 128ull << 20;
+constexpr uint64_t ROPE_AT_ONCE = 1ull << 23;  // workgroups of a launch: a grid has less than 2^32 threads
 
 struct RopeDev {
     const void* x[2];
@@ -42,6 +43,7 @@ struct RopeDev {
     uint32_t n_t, n_h, n_w;  // pairs of an axis
     uint32_t off_t, off_h, off_w;  // where an axis begins in the table, places before the grid's first left out, minus its first pair
     float sign;
+    uint32_t first;          // workgroup that a launch begins with
 };
 
 template <typename T>
@@ -86,7 +88,7 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void rope_kernel(RopeDev a) {
     constexpr bool HALF = PAIRS != PAIRS_NEXT;
     __shared__ __attribute__((aligned(16))) char stage_all[HALF ? ROPE_WAVES * 64 * 16 * C::N : 16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t id = blockIdx.x * ROPE_WAVES + wave;
+    const uint32_t id = (a.first + blockIdx.x) * ROPE_WAVES + wave;
     const uint32_t group = a.parts.div(id), part = id - group * a.parts.d;
     const uint32_t row0 = group * a.tokens;
     if (row0 >= a.n_rows) return;  // a whole wavefront
@@ -266,11 +268,17 @@ hipError_t launch_rope(const RopeArgs& r, hipStream_t stream) {
     d.off_w = (uint32_t)r.len_t * d.n_t + (uint32_t)r.len_h * d.n_h + (uint32_t)r.w0 * d.n_w - d.end_h;
     d.sign = r.inverse ? -1.f : 1.f;
     const uint64_t blocks = (groups * parts + ROPE_WAVES - 1u) / ROPE_WAVES;
-    if (!fits_grid(blocks, 64 * ROPE_WAVES)) return hipErrorInvalidConfiguration;
     const int pairs = !r.half ? PAIRS_NEXT : d.R % 16u == 0 ? PAIRS_CHUNKS : PAIRS_APART;
     const uint64_t bytes = (uint64_t)d.n_rows * d.heads * d.head_dim * (r.f32 ? 4u : 2u) * (r.k ? 2u : 1u);
     const bool nt = bytes > ROPE_CACHED_BYTES;
-    return r.f32 ? launch_rope_t<float>(d, r.order, pairs, nt, (uint32_t)blocks, stream) : launch_rope_t<__bf16>(d, r.order, pairs, nt, (uint32_t)blocks, stream);
+    static_assert(ROPE_AT_ONCE * 64 * ROPE_WAVES < 1ull << 32, "a grid");
+    for (uint64_t first = 0; first < blocks; first += ROPE_AT_ONCE) {
+        d.first = (uint32_t)first;
+        const uint32_t n = (uint32_t)(blocks - first < ROPE_AT_ONCE ? blocks - first : ROPE_AT_ONCE);
+        const hipError_t e = r.f32 ? launch_rope_t<float>(d, r.order, pairs, nt, n, stream) : launch_rope_t<__bf16>(d, r.order, pairs, nt, n, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // ---- the table

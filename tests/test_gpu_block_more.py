@@ -69,3 +69,29 @@ def test_more_rows_than_small_tiles_fit_a_grid():
     # at most M roundings of partial sums, each at most 2^-24 of the sum of sizes, in any direction: 8 times the root of their number
     for got, want, size in ((dw, *sums[:2]), (db, *sums[2:])):
         assert ((got.double() - want).abs() <= ref.BF16 * want.abs() + 8 * M ** 0.5 * ref.F32 * size).all()
+
+
+def test_more_tokens_than_a_launch_of_positions_has_wavefronts():
+    """67 million tokens of one head of 264 channels, a wavefront each: 2^24 workgroups, and more, are not a launch."""
+    import paper_2605_28691_amd as sk
+
+    B, W, D, step = 65729, 1021, 264, 1 << 22
+    rows = B * W
+    assert rows > 1 << 26
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q = torch.empty(rows, D, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, rows, step):
+        q[i : i + step] = torch.randn(min(step, rows - i), D, generator=g, device="cuda")
+    table = sk.skiparse_rope_table((1, 1, W), (0, 0, 260))
+    out = torch.full_like(q, float("nan"))
+    sk.skiparse_rope(q.view(B, W, 1, D), None, table, 1, 1, W, q_out=out.view(B, W, 1, D))
+    for i in range(0, rows, step):
+        assert bool(out[i : i + step].isfinite().all()), i
+    at = torch.cat([torch.randint(0, rows, (20_000,), generator=g, device="cuda")] + [torch.arange(max(0, i - 8), min(rows, i + 8), device="cuda") for i in (0, 1 << 25, 1 << 26, rows)])
+    x = q[at].double()
+    z = torch.view_as_complex(x[:, :260].reshape(-1, 130, 2)) * torch.view_as_complex(table.data.view(W, 130, 2)[at % W].double())
+    want = torch.cat((torch.view_as_real(z).reshape(-1, 260), x[:, 260:]), 1)
+    got = out[at].double()
+    # one rounding of the result; products and their sum in float32
+    assert bool(((got - want).abs() <= ref.BF16 * want.abs() + 8 * ref.F32 * x.abs().amax(1, keepdim=True)).all())
+    assert torch.equal(got[:, 260:], x[:, 260:])
