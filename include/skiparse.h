@@ -271,7 +271,7 @@ int skiparse_checkpoint_load(const void* codes, const void* scales, void* out, i
  * `order`, out, residual and pre on the other: a projection in front of a chain of sparse blocks writes the sparse layout, the one behind it reads it.
  *   act: SKIPARSE_ACT_NONE, SKIPARSE_ACT_GELU_TANH (z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2), SKIPARSE_ACT_SILU (z / (1 + exp(-z)))
  *   pre: NULL, or where z is kept for the backward pass: bf16 [rows][out_features] with pre_scales NULL, or the codes and scales of a checkpoint.
- * Sums in float32; out is rounded once.  The order of a row's sums, and so its last bits, may depend on how many rows share the call.  out may be residual; nothing else may overlap.  in_features and out_features multiples of 8 below 2^23; with rows that move
+ * Sums in float32; out is rounded once.  The order of a row's sums, and so its last bits, may depend on how many rows share the call, and on nothing else of it: what is kept changes no bit of out.  out may be residual; nothing else may overlap.  in_features and out_features multiples of 8 below 2^23; with rows that move
  * x is less than 4 GiB; a result (out, dx, dw) has less than 2^24 tiles of 256 x 256, the last ones of a side counted as whole.  workspace: skiparse_linear_workspace_bytes() bytes, NULL where that is 0.
  *
  * skiparse_linear_bwd: gradients for a loss with dL/dout = dy (rows as out's).  dz = dy act'(z),

@@ -709,7 +709,7 @@ int skiparse_linear_fwd(const void* x, const void* w, const void* bias, const vo
     const Span sp = {pre, rows * N * (pre_scales ? 1 : 2)}, ss = {pre_scales, checkpoint_scales(rows, N)}, sr = {residual, rows * N * 2};
     if (touches(so, {sx, sw, sb, sp, ss}) || (residual && residual != out && overlap2(out, so.bytes, residual, sr.bytes))) return SKIPARSE_EINVAL;
     if (touches(sp, {sx, sw, sb, ss, sr}) || touches(ss, {sx, sw, sb, sr})) return SKIPARSE_EINVAL;
-    const size_t need = linear_workspace(LINEAR_FWD, (uint32_t)rows, (uint32_t)N, (uint32_t)K, pre_scales != nullptr);
+    const size_t need = linear_workspace(LINEAR_FWD, (uint32_t)rows, (uint32_t)N, (uint32_t)K);
     if (need && (!workspace || workspace_bytes < need || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
     if (touches({need ? workspace : nullptr, need}, {sx, sw, sb, sr, so, sp, ss})) return SKIPARSE_EINVAL;
     LinearArgs a = {};

@@ -212,7 +212,7 @@ struct LinearArgs {
     RowArgs rows;
     float* partial;  // linear_workspace() bytes
 };
-size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K, bool checkpoint = true);  // checkpoint: one is written
+size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K);
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream);
 
 // The passes over rows in front of a backward's products.

@@ -467,17 +467,31 @@ static hipError_t launch_tiles(const LinearArgs& a, const LinearPlan& p, hipStre
     return hipGetLastError();
 }
 
+// the largest |x| of four, not counting what is not finite, as the bits of its float
+__device__ inline uint32_t ckpt_largest(const f32x4& x) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const uint32_t s = ckpt_size(x[e]);
+        m = s > m ? s : m;
+    }
+    return m;
+}
+
 // x w^T for one row, which reads w once and is bound by that: a wavefront has CH channels, and reads 1024 of k of each at once, whole lines; x is read with them and comes out of the
 // caches.  Its sums are added up over the lanes at the end.  (5120 -> 5120: 9.5 us; reading w as the products' fragments, 64 bytes of 16 rows at once, 15.6.)
-constexpr int ROW_WAVES = 4;
-template <int CH>
-__global__ __launch_bounds__(64 * ROW_WAVES) void linear_row_kernel(LinearArgs a) {
+// KEPT: z is kept as a checkpoint, of whose blocks of 32 channels a workgroup has one.  A channel's sum does not depend on either.  (us with a checkpoint written, so / in tiles: 5120 -> 5120
+// 13.1 / 21.8, 1536 -> 8960 9.3 / 20.3, 8960 -> 1536 15.3 / 19.4, 64 -> 11,200 4.3 / 4.4.)
+constexpr int row_waves(int channels, bool kept) { return kept ? CKPT_BLOCK / channels : 4; }
+template <int CH, bool KEPT>
+__global__ __launch_bounds__(64 * row_waves(CH, KEPT)) void linear_row_kernel(LinearArgs a) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
     constexpr int AT_ONCE = 2;  // times 512 of k
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t n0 = (blockIdx.x * ROW_WAVES + wave) * CH;
-    if (n0 >= a.N) return;
-    const uint32_t ld = a.K * 2u;
+    const uint32_t n0 = (blockIdx.x * row_waves(CH, KEPT) + wave) * CH;
+    if (!KEPT && n0 >= a.N) return;
+    __shared__ __attribute__((aligned(16))) float block[KEPT ? CKPT_BLOCK : 4];
+    const uint32_t ld = a.K * 2u, end = !KEPT || n0 < a.N ? a.K : 0u;  // a wavefront behind the last channel reads nothing, and has zeros
     float acc[CH];
 #pragma unroll
     for (int c = 0; c < CH; c++) acc[c] = 0.f;
@@ -485,7 +499,7 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void linear_row_kernel(LinearArgs a
     // N is a multiple of 8, so a wavefront's channels are all there
     const auto wb = __builtin_amdgcn_make_buffer_rsrc((char*)a.q + (size_t)n0 * ld, 0, LIN_RECORDS, 0x27000);
     const auto xb = __builtin_amdgcn_make_buffer_rsrc((char*)a.p, 0, LIN_RECORDS, 0x27000);
-    for (uint32_t k = 0; k < a.K; k += 512u * AT_ONCE) {
+    for (uint32_t k = 0; k < end; k += 512u * AT_ONCE) {
         u32x4 w[AT_ONCE][CH], x[AT_ONCE];
 #pragma unroll
         for (int u = 0; u < AT_ONCE; u++) {
@@ -514,11 +528,29 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void linear_row_kernel(LinearArgs a
         for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
         if (lane == (uint32_t)c) z = s;
     }
-    if (lane >= CH) return;
     const uint32_t n = n0 + lane;
+    const bool on = lane < CH && (!KEPT || n0 < a.N);
     const LinearEpilogue& e = a.e;
-    if (e.bias != nullptr) z += (float)((const __bf16*)e.bias)[n];
-    if (e.pre != nullptr) ((__bf16*)e.pre)[n] = (__bf16)z;
+    if (on && e.bias != nullptr) z += (float)((const __bf16*)e.bias)[n];
+    if (KEPT) {
+        if (lane < CH) block[wave * CH + lane] = z;
+        __syncthreads();
+        if (threadIdx.x < CKPT_BLOCK / 4u) {  // 4 channels each, the block's largest from all of them
+            const f32x4 own = *(const f32x4*)(block + threadIdx.x * 4u);
+            const uint32_t c = blockIdx.x * CKPT_BLOCK + threadIdx.x * 4u;
+            uint32_t top = ckpt_largest(own);
+#pragma unroll
+            for (int off = 1; off <= 4; off <<= 1) {
+                const uint32_t o = (uint32_t)__shfl_xor((int)top, off);
+                top = o > top ? o : top;
+            }
+            const uint32_t byte = ckpt_byte(top);
+            if (c < a.N) *(uint32_t*)((unsigned char*)e.pre + c) = ckpt_codes(own[0], own[1], own[2], own[3], ckpt_down(byte));
+            if (threadIdx.x == 0u) ((unsigned char*)e.pre_scales)[blockIdx.x] = (unsigned char)byte;
+        }
+    }
+    if (!on) return;
+    if (!KEPT && e.pre != nullptr) ((__bf16*)e.pre)[n] = (__bf16)z;
     z = act_value(e.act, z);
     if (e.residual != nullptr) z += (float)((const __bf16*)e.residual)[n];
     ((__bf16*)e.out)[n] = (__bf16)z;
@@ -527,8 +559,11 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void linear_row_kernel(LinearArgs a
 // x w^T for a few more rows, up to 16 FM: bound by reading w, which a workgroup does for 16 FN channels.  Its wavefronts take every fourth step of 64 of k, so that together they read
 // 512 bytes in a row, each through steps of its own in LDS (no barriers), FEW_DEEP of them on their way; their sums are added up, in order, at the end.  5 rows, 5120 -> 5120: 52 MB, 12.5 us (19.3 in tiles of
 // 64 x 64, cut in six).
+// KEPT: z is kept as a checkpoint, of whose blocks of 32 channels a workgroup has one, two blocks of its own.  A channel's sum is the same in every form, so that what is kept changes no bit
+// of the result.  (us with a checkpoint written, so / in tiles, whose order of the sums is another: 5120 -> 5120, 2 rows 14.5 / 22.2, 16 rows 18.2 / 22.1, 32 rows 20.7 / 22.6; 1536 -> 8960, 16 rows
+// 13.5 / 20.4; 8960 -> 1536, 2 rows 16.1 / 19.4, 16 rows 20.0 / 19.3, 32 rows 25.1 / 19.6; with two halves of four wavefronts, 16 channels each, 18.1, 24.4 and 32.7.)
 constexpr int FEW_WAVES = 4, FEW_DEEP = 4;
-template <int FM, int FN>
+template <int FM, int FN, bool KEPT>
 __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearArgs a) {
     using SP = Side<16 * FM, false, 1>;
     using SQ = Side<16 * FN, false, 1>;
@@ -602,54 +637,79 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearArgs a
     // wavefront i finishes block i: lane l has row l % 16 and channels 4 (l / 16) .. + 3
     static_assert(FM * FN <= FEW_WAVES, "a block a wavefront");
     const uint32_t m = wave / FN * 16u + (lane & 15u), n = n0 + wave % FN * 16u + 4u * (lane >> 4);
-    if (wave >= (uint32_t)(FM * FN) || m >= a.M || n >= a.N) return;
-    f32x4 z = sums[0][wave][lane];
-#pragma unroll
-    for (int w = 1; w < FEW_WAVES; w++) z += sums[w][wave][lane];
+    if (wave >= (uint32_t)(FM * FN)) return;
     const LinearEpilogue& e = a.e;
     const size_t at = (size_t)m * a.N + n;
-    auto add = [&](const void* t, size_t from) __attribute__((always_inline)) {
+    auto add = [&](f32x4& z, const void* t, size_t from) __attribute__((always_inline)) {
         const bf16x4 x = *(const bf16x4*)((const __bf16*)t + from);
 #pragma unroll
         for (int c = 0; c < 4; c++) z[c] += (float)x[c];
     };
+    auto sum = [&](uint32_t b, uint32_t c) __attribute__((always_inline)) -> f32x4 {  // of block b, the lane's channels from c
+        f32x4 z = sums[0][b][lane];
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; w++) z += sums[w][b][lane];
+        if (e.bias != nullptr && c < a.N) add(z, e.bias, c);
+        return z;
+    };
+    f32x4 z = sum(wave, n);
+    if (KEPT) {
+        static_assert(!KEPT || FN * 16 == CKPT_BLOCK, "a block of a checkpoint: two wavefronts' channels");
+        // the other's sums are formed here as well, in the same order: lanes l, l + 16, l + 32, l + 48 have a row's block then
+        const f32x4 other = sum(wave ^ 1u, n ^ 16u);
+        uint32_t top = n < a.N ? ckpt_largest(z) : 0u;
+        const uint32_t o = (n ^ 16u) < a.N ? ckpt_largest(other) : 0u;
+        top = o > top ? o : top;
+#pragma unroll
+        for (int off = 16; off <= 32; off <<= 1) {
+            const uint32_t far = (uint32_t)__shfl_xor((int)top, off);
+            top = far > top ? far : top;
+        }
+        const uint32_t byte = ckpt_byte(top);
+        if (m < a.M && n < a.N) *(uint32_t*)((unsigned char*)e.pre + at) = ckpt_codes(z[0], z[1], z[2], z[3], ckpt_down(byte));
+        if (m < a.M && (n & 16u) == 0u && lane < 16u) ((unsigned char*)e.pre_scales)[(size_t)m * ((a.N + CKPT_BLOCK - 1u) / CKPT_BLOCK) + blockIdx.x] = (unsigned char)byte;
+    }
+    if (m >= a.M || n >= a.N) return;
     auto store = [&](void* t) __attribute__((always_inline)) {
         bf16x4 x;
 #pragma unroll
         for (int c = 0; c < 4; c++) x[c] = (__bf16)z[c];
         *(bf16x4*)((__bf16*)t + at) = x;
     };
-    if (e.bias != nullptr) add(e.bias, n);
-    if (e.pre != nullptr) store(e.pre);
+    if (!KEPT && e.pre != nullptr) store(e.pre);
 #pragma unroll
     for (int c = 0; c < 4; c++) z[c] = act_value(e.act, z[c]);
-    if (e.residual != nullptr) add(e.residual, at);
+    if (e.residual != nullptr) add(z, e.residual, at);
     store(e.out);
 }
 
-template <int CH>
+template <int CH, bool KEPT = false>
 static hipError_t launch_row(const LinearArgs& a, hipStream_t stream) {
-    constexpr uint32_t per = CH * ROW_WAVES;
-    linear_row_kernel<CH><<<(a.N + per - 1u) / per, 64 * ROW_WAVES, 0, stream>>>(a);
+    constexpr uint32_t waves = row_waves(CH, KEPT), per = CH * waves;
+    linear_row_kernel<CH, KEPT><<<(a.N + per - 1u) / per, 64 * waves, 0, stream>>>(a);
     return hipGetLastError();
 }
-template <int FM, int FN>
+template <int FM, int FN, bool KEPT = false>
 static hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
-    linear_few_kernel<FM, FN><<<(a.N + 16u * FN - 1u) / (16u * FN), 64 * FEW_WAVES, 0, stream>>>(a);
+    constexpr uint32_t per = 16u * FN;
+    linear_few_kernel<FM, FN, KEPT><<<(a.N + per - 1u) / per, 64 * FEW_WAVES, 0, stream>>>(a);
     return hipGetLastError();
 }
 static hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
+    const bool kept = a.e.pre_scales != nullptr;
     if (a.M == 1u) {  // moved or not, row 0
+        if (kept) return launch_row<4, true>(a, stream);
         const uint32_t channels = row_channels(a.N);
         return channels == 1u ? launch_row<1>(a, stream) : channels == 2u ? launch_row<2>(a, stream) : launch_row<4>(a, stream);
     }
+    if (kept) return a.M <= 16u ? launch_few<1, 2, true>(a, stream) : launch_few<2, 2, true>(a, stream);
     if (few_blocks(a.M, a.N, a.K) == 2u) return a.M <= 16u ? launch_few<1, 2>(a, stream) : launch_few<2, 2>(a, stream);
     return a.M <= 16u ? launch_few<1, 1>(a, stream) : launch_few<2, 1>(a, stream);
 }
 
 template <int FORM, bool EXTRAS = false>
 static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
-    if (FORM == LINEAR_FWD && linear_few(a.M, a.K) && a.e.pre_scales == nullptr) return launch_few(a, stream);
+    if (FORM == LINEAR_FWD && linear_few(a.M, a.K)) return launch_few(a, stream);
     const LinearPlan p = plan_linear(a.M, a.N, a.K);
     switch (p.shape) {
         case T256: return launch_tiles<T256, FORM, EXTRAS>(a, p, stream);
@@ -659,8 +719,8 @@ static hipError_t launch_form(const LinearArgs& a, hipStream_t stream) {
     }
 }
 
-size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K, bool checkpoint) {
-    return form == LINEAR_FWD && linear_few(M, K) && !checkpoint ? 0u : plan_linear(M, N, K).workspace();
+size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K) {
+    return form == LINEAR_FWD && linear_few(M, K) ? 0u : plan_linear(M, N, K).workspace();
 }
 
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream) {

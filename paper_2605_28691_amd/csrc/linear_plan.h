@@ -84,7 +84,7 @@ inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K) {
     return best;
 }
 
-// Whether x w^T with M rows goes to the kernels for few rows, which read w once and write no checkpoint.  (us, these / tiles: 5120 -> 5120, 5 rows 12.5 / 19.3, 16 rows 14.4 / 19.4,
+// Whether x w^T with M rows goes to the kernels for few rows, which read w once, whatever is kept.  (us, these / tiles: 5120 -> 5120, 5 rows 12.5 / 19.3, 16 rows 14.4 / 19.4,
 // 32 rows 17.8 / 19.7; 1536 -> 8960, 16 rows 8.4 / 12.8, 32 rows 11.3 / 12.9; 13,824 -> 5120, 16 rows 32.1 / 37.0, 32 rows 39.5 / 37.1; 64 -> 11,200, 16 rows 5.9 / 5.9, 32 rows
 // 6.9 / 5.9.)
 inline bool linear_few(uint32_t M, uint32_t K) { return M <= 16u || (M <= 32u && K >= 512u); }
