@@ -622,6 +622,9 @@ def _linear_rows(lead, order: str, T: int, H: int, W: int, s: int):
     return (B, T, H, W), (s2 * B, n // s2) if order == "to_sparse" else (B, n)
 
 
+_BACK = {"same": "same", "to_sparse": "to_original", "to_original": "to_sparse"}
+
+
 def _bf16(what: str, *tensors) -> None:
     for t in tensors:
         if t is not None and t.dtype != torch.bfloat16:
@@ -678,23 +681,28 @@ def skiparse_linear_bwd_workspace_bytes(rows: int, in_features: int, out_feature
     return _size("skiparse_linear_bwd_workspace_bytes", rows, in_features, out_features, ORDERS[order], ACTS[act], 1 if x_checkpoint else 0)
 
 
-def skiparse_linear_bwd(dy: torch.Tensor, x, w: torch.Tensor, pre=None, act: str = "none", order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1,
+def skiparse_linear_bwd(dy: torch.Tensor, x, w: torch.Tensor | None, pre=None, act: str = "none", order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1,
                         pattern: str = "token", need_dx: bool = True, need_dw: bool = True, need_db: bool = True, dx_add: torch.Tensor | None = None,
                         dx: torch.Tensor | None = None, dw: torch.Tensor | None = None, db: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Gradients (dx, dw, db) of skiparse_linear_fwd for dL/dresult = dy; None for one that is not needed.  x: what the forward call had, or its Checkpoint; pre: what
-    keep returned, bf16 or a Checkpoint (act "none" needs none).  dx = dz w + dx_add; dx_add may be dx.  The residual's gradient is dy."""
-    N, K = w.shape
+    keep returned, bf16 or a Checkpoint (act "none" needs none).  dx = dz w + dx_add; dx_add may be dx.  The residual's gradient is dy.  x is read for dw, w for dx: None
+    will do for one that is not."""
+    if (need_dx and w is None) or (need_dw and x is None):
+        raise ValueError("dx needs w, and dw x")
+    N = dy.shape[-1]
     xc = x.codes if isinstance(x, Checkpoint) else x
-    if xc.shape[-1] != K or dy.shape[-1] != N:
+    K = w.shape[-1] if w is not None else xc.shape[-1] if xc is not None else 8  # db alone has nothing to do with it
+    if (xc is not None and xc.shape[-1] != K) or (w is not None and tuple(w.shape) != (N, K)):
         raise ValueError("dy, x and w do not fit each other")
     if isinstance(x, Checkpoint):
         _checked(x, xc.shape, "x")
     else:
         _bf16("x", x)
     _bf16("dy, w and dx_add", dy, w, dx_add)
-    grid, lead = _linear_rows(xc.shape[:-1], order, T, H, W, s)
-    if tuple(dy.shape) != (*lead, N) or (dx_add is not None and dx_add.shape != xc.shape):
-        raise ValueError("dy or dx_add does not have its rows")
+    grid, back = _linear_rows(dy.shape[:-1], _BACK[order], T, H, W, s)
+    shape = (*back, K)
+    if (xc is not None and tuple(xc.shape) != shape) or (dx_add is not None and tuple(dx_add.shape) != shape):
+        raise ValueError("dy, x or dx_add does not have its rows")
     codes = scales = None
     if act != "none":
         if pre is None:
@@ -703,7 +711,7 @@ def skiparse_linear_bwd(dy: torch.Tensor, x, w: torch.Tensor, pre=None, act: str
             codes, scales = _checked(pre, dy.shape, "pre")
         else:
             codes = _into(pre, dy.shape, dy)
-    dx = _into(dx, xc.shape, dy) if need_dx else None
+    dx = _into(dx, shape, dy) if need_dx else None
     dw = _into(dw, (N, K), dy) if need_dw else None
     db = _into(db, (N,), dy) if need_db else None
     xs = x.scales if isinstance(x, Checkpoint) else None

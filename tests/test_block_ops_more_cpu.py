@@ -62,3 +62,35 @@ def test_integers_beyond_the_c_types_are_refused(monkeypatch):
         sk._general("skiparse_linear_fwd", q, q, None, None, q, None, None, 1, 1, 1, 4, 8, 8, 1, 0, 0, 0, 0, None, -1, 0)
     with pytest.raises(ctypes.ArgumentError):  # no integer
         sk.skiparse_linear_workspace_bytes(4.0, 8, 8)
+
+
+def test_backward_asks_for_what_it_reads_only(monkeypatch):
+    """x is read for dw and w for dx, as in the C call: a program that wants one of them need not have kept the other."""
+    calls = []
+    monkeypatch.setattr(sk, "_stream", lambda: 0)
+    monkeypatch.setattr(sk, "_here", lambda *t: None)
+    monkeypatch.setattr(sk, "_skiparse_linear_bwd", lambda *a: calls.append(a))
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    dy, x, w = bf(5, 32), bf(5, 64), bf(32, 64)
+    dx, dw, db = sk.skiparse_linear_bwd(dy, None, w, need_dw=False)
+    assert dx.shape == x.shape and dw is None and db.shape == (32,)
+    a = calls.pop()
+    assert a[1] is None and a[3] is w and a[10:16] == (1, 1, 1, 5, 64, 32)
+    dx, dw, db = sk.skiparse_linear_bwd(dy, x, None, need_dx=False)
+    assert dx is None and dw.shape == w.shape
+    a = calls.pop()
+    assert a[1] is x and a[3] is None and a[14:16] == (64, 32)
+    assert sk.skiparse_linear_bwd(dy, None, None, need_dx=False, need_dw=False)[2].shape == (32,)
+    # rows that move: the other side's shape follows from dy's
+    dy = bf(4, 8, 32)
+    at = dict(order="to_sparse", T=2, H=4, W=4, s=2)
+    assert sk.skiparse_linear_bwd(dy, None, w, need_dw=False, **at)[0].shape == (1, 32, 64)
+    at["order"] = "to_original"
+    assert sk.skiparse_linear_bwd(dy.view(1, 32, 32), None, w, need_dw=False, dx_add=bf(4, 8, 64), **at)[0].shape == (4, 8, 64)
+    calls.clear()
+    for args, kw in (((dy, None, w), {}), ((dy, bf(4, 8, 64), None), {}), ((dy, None, w), dict(need_dx=False)), ((dy, bf(4, 8, 56), w), dict(need_dw=False)),
+                     ((dy, bf(4, 7, 64), None), dict(need_dx=False)), ((dy, None, bf(64)), dict(need_dw=False)), ((dy, None, bf(24, 64)), dict(need_dw=False)),
+                     ((dy, None, w), dict(need_dw=False, dx_add=bf(4, 8, 56))), ((dy, None, w), dict(need_dw=False, order="to_sparse", T=2, H=4, W=3, s=2))):
+        with pytest.raises(ValueError):
+            sk.skiparse_linear_bwd(*args, **kw)
+    assert not calls

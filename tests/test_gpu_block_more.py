@@ -95,3 +95,24 @@ def test_more_tokens_than_a_launch_of_positions_has_wavefronts():
     # one rounding of the result; products and their sum in float32
     assert bool(((got - want).abs() <= ref.BF16 * want.abs() + 8 * ref.F32 * x.abs().amax(1, keepdim=True)).all())
     assert torch.equal(got[:, 260:], x[:, 260:])
+
+
+@pytest.mark.parametrize("order", ["same", "to_sparse", "to_original"])
+def test_gradients_without_what_they_do_not_read(order):
+    import paper_2605_28691_amd as sk
+
+    T, H, W, s, K, N = 3, 4, 8, 2, 72, 136
+    n = T * H * W
+    sparse, plain = (4, n // 4), (1, n)
+    lead = sparse if order == "to_sparse" else plain
+    back = sparse if order == "to_original" else plain
+    g = torch.Generator(device="cuda").manual_seed(8)
+    r = lambda *shape: torch.randn(*shape, generator=g, device="cuda").bfloat16()  # noqa: E731
+    dy, pre, x, w = r(*lead, N), r(*lead, N), r(*back, K), r(N, K)
+    kw = dict(pre=pre, act="silu", order=order, T=T, H=H, W=W, s=s)
+    want = sk.skiparse_linear_bwd(dy, x, w, **kw)
+    dx, dw, db = sk.skiparse_linear_bwd(dy, None, w, need_dw=False, **kw)
+    assert dw is None and torch.equal(dx, want[0]) and torch.equal(db, want[2])
+    dx, dw, db = sk.skiparse_linear_bwd(dy, x, None, need_dx=False, **kw)
+    assert dx is None and torch.equal(dw, want[1]) and torch.equal(db, want[2])
+    assert torch.equal(sk.skiparse_linear_bwd(dy, None, None, need_dx=False, need_dw=False, **kw)[2], want[2])
