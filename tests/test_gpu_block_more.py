@@ -116,3 +116,54 @@ def test_gradients_without_what_they_do_not_read(order):
     dx, dw, db = sk.skiparse_linear_bwd(dy, x, None, need_dx=False, **kw)
     assert dx is None and torch.equal(dw, want[1]) and torch.equal(db, want[2])
     assert torch.equal(sk.skiparse_linear_bwd(dy, None, None, need_dx=False, need_dw=False, **kw)[2], want[2])
+
+
+@pytest.mark.parametrize("pattern", ["token", "group"])
+def test_attention_gradients_from_checkpoints(pattern):
+    """The attention's backward on saved tensors that went through 8 bits, against its formulas in float64 on the same values: P = exp(q k^T c - lse), dV = P^T dO,
+    dS = P (dO V^T - rowsum(dO O)), dQ = c dS K, dK = c dS^T Q.  P and dS are rounded to bf16 for the products and the gradients once more: three roundings of 2^-8 at most, below 1e-2 in the
+    2-norm as everywhere in the backward's tests."""
+    import paper_2605_28691_amd as sk
+    import synth_inputs as si
+
+    w = si.make_shape("ckpt_grad", 1, 3, 64, 3, 8, 12, 2, seed=72)
+    q, k, v = (t.cuda() for t in si.make_qkv(w))
+    dout = si.make_dout(w).cuda()
+    grid, H, W = (w.T, w.H, w.W), w.H, w.W
+    if pattern == "group":
+        assert H % (w.s * w.s) == 0 and W % (w.s * w.s) == 0
+    at = (*grid, w.s, pattern)
+    out, lse = sk.skiparse_attn_fwd_lse(q, k, v, *at)
+    restored = [sk.skiparse_checkpoint_load(sk.skiparse_checkpoint_save(t)) for t in (q, k, v, out)]
+    assert not torch.equal(restored[0], q)
+    got = sk.skiparse_attn_bwd(*restored, dout, lse, *at)
+    to = lambda t: ref.moved(t.double(), "to_sparse", (w.B, *grid), w.s, pattern).transpose(1, 2)  # noqa: E731  [sequences][heads][positions][D]
+    q64, k64, v64, o64, d64 = (to(t) for t in (*restored, dout))
+    c = w.D ** -0.5
+    p = torch.exp(q64 @ k64.transpose(-1, -2).contiguous() * c - lse.double()[..., None])
+    ds = p * (d64 @ v64.transpose(-1, -2).contiguous() - (d64 * o64).sum(-1, keepdim=True))
+    want = ds @ k64 * c, ds.transpose(-1, -2).contiguous() @ q64 * c, p.transpose(-1, -2).contiguous() @ d64
+    for a, b, name in zip(got, want, ("dq", "dk", "dv")):
+        a = to(a)
+        assert float((a - b).norm()) <= 1e-2 * float(b.norm()) and float((a - b).abs().max()) <= 3e-2 * float(b.abs().max()), name
+
+
+def test_bias_gradient_of_many_rows():
+    """300,000 rows, in parts of 128 that a second launch adds up."""
+    import paper_2605_28691_amd as sk
+
+    M, N = 300_000, 1000
+    g = torch.Generator(device="cuda").manual_seed(9)
+    dy = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+    pre = (2 * torch.randn(M, N, generator=g, device="cuda")).bfloat16()
+    for act in ("none", "silu"):
+        _, _, db = sk.skiparse_linear_bwd(dy, None, None, pre=None if act == "none" else pre, act=act, need_dx=False, need_dw=False)
+        want, size, off = (torch.zeros(N, dtype=torch.float64, device="cuda") for _ in range(3))
+        for i in range(0, M, 30_000):
+            d = dy[i : i + 30_000].double()
+            t = d if act == "none" else d * ref.slope(act, pre[i : i + 30_000].double())
+            want += t.sum(0)
+            size += t.abs().sum(0)
+            off += d.abs().sum(0)
+        # float32 sums of 16, 8, up to 147 and 16 terms one after the other; the slope's own arithmetic is good to 2^-19
+        assert ((db.double() - want).abs() <= ref.BF16 * want.abs() + (16 + 8 + 147 + 16) * ref.F32 * size + (2.0 ** -19 * off if act != "none" else 0)).all(), act
