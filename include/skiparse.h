@@ -260,7 +260,7 @@ int skiparse_rope(const void* q, const void* k, void* q_out, void* k_out, const 
  * a row (the last one may be shorter): codes[rows][cols] E4M3 and scales[rows][ceil(cols/32)], one byte e + 127 a block, for the smallest 2^e with
  * |x| <= 448 * 2^e; code = rne(x * 2^-e), value = code * 2^e.  A block of zeros has byte 127.  A value that is not finite becomes NaN and does not enter the
  * scale.  cols a multiple of 8; codes 16-byte aligned, scales at any address.  _load gives the values back in bf16 or float32 (exact in both, down to the type's
- * smallest numbers); byte 255 stands for NaN.
+ * smallest numbers, and up to 2^128: |x| beyond 248 * 2^120, 3.30e38, is rounded to that and comes back as infinity); byte 255 stands for NaN.
  */
 int skiparse_checkpoint_save(const void* x, void* codes, void* scales, int rows, int cols, int dtype, void* stream);
 int skiparse_checkpoint_load(const void* codes, const void* scales, void* out, int rows, int cols, int dtype, void* stream);

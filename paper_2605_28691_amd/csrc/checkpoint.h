@@ -1,7 +1,8 @@
 // Format of an 8-bit activation checkpoint: blocks of 32 consecutive channels of a row, one E4M3 code a value and one exponent byte a block.
 //     a = largest finite |x| of the block,  e = smallest integer with a <= 448 * 2^e,  code = rne(x * 2^-e),  byte = e + 127
+// Beyond 248 * 2^120 (3.30e38) a finite x rounds to 2^128, which is infinity in both types: as any rounding to fewer bits next to the largest number.
 // A power of two as scale costs no precision (a float's rounding error is relative), makes the scaling exact in both directions and takes a byte where a
-// float would take four; a block is what two lanes of an accumulator hold of a row (linear.hip), so that a product's epilogue can write one.
+// float would take four; a block is what four lanes of an accumulator hold of a row (linear.hip), so that a product's epilogue can write one.
 // Blocks of nothing but zeros have byte 127.  A value that is not finite gets a NaN code and does not enter the maximum.  The last block of a row whose length is
 // no multiple of 32 is shorter.
 #pragma once

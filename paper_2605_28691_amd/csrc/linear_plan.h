@@ -21,7 +21,7 @@ constexpr uint32_t LINEAR_STEP = 64, LINEAR_STEPS = 2 * LINEAR_STEP;  // k is wa
 constexpr uint32_t LINEAR_MAX_PARTS = 16;
 constexpr uint64_t LINEAR_GRID = 1ull << 24;  // a launch has fewer workgroups of 256: a grid, fewer than 2^32 threads
 // Fitted to products of 28 sizes (1 to 32,760 rows, 256 to 20,480 channels, the three forms), each with every tile and several numbers of parts: over the last 36 of them what the
-// rule takes is 1 % slower than the best in the mean, 9 % at most.  For example, us, 256 / 128 / 64 / 128 x 256, uncut: 8190 x 1536 -> 1536 36 / 43 / 60 / 48, dx of
+// rule takes is 1 % slower than the best in the mean, 9 % at most (profiles/linear_tiles.txt; without an epilogue, which the rule does not see, nor whether operands are transposed).  For example, us, 256 / 128 / 64 / 128 x 256, uncut: 8190 x 1536 -> 1536 36 / 43 / 60 / 48, dx of
 // 6426 x 1000 -> 4008 82 / 71 / 120 / 53 (408 tiles of 128 are 80 % of a round of two a CU, 204 of 128 x 256 of a round of one; 256 x 128 64), 1000 x 2048 -> 2048
 // 40 / 17 / 18 / 25; cut best: 3840 x 5120 -> 5120 155 / 173 / 285 / 184.
 constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {
@@ -92,9 +92,9 @@ inline bool linear_few(uint32_t M, uint32_t K) { return M <= 16u || (M <= 32u &&
 // One row: channels of a wavefront, as many as leave 2048 wavefronts.
 inline uint32_t row_channels(uint32_t N) { return N >= 8192u ? 4u : N >= 4096u ? 2u : 1u; }
 
-// More: blocks of 16 channels of a workgroup.  Two halve what is read of x; one leaves more workgroups, and a CU has two of them, of which one can begin while the other ends.
-// (us, two / one: 5120 -> 5120, 2 rows 12.2 / 13.9, 16 rows 14.4 / 17.0; 5120 -> 13,824, 16 rows 30.4 / 32.9; 1536 -> 8960, 2 rows 9.4 / 8.1, 16 rows 9.7 / 8.4, 17 rows
-// 11.0 / 11.8; 8960 -> 1536, 16 rows 11.9 / 8.7.)
+// More: blocks of 16 channels of a workgroup.  Two halve what is read of x; one leaves more workgroups, and with up to 16 rows a CU has two of them (68 KB of LDS each; 104
+// with up to 32), of which one can begin while the other ends.  (us, two / one: 5120 -> 5120, 2 rows 12.2 / 13.9, 16 rows 14.4 / 17.0; 5120 -> 13,824, 16 rows 30.4 / 32.9;
+// 1536 -> 8960, 2 rows 9.4 / 8.1, 16 rows 9.7 / 8.4, 17 rows 11.0 / 11.8; 8960 -> 1536, 16 rows 11.9 / 8.7.)
 inline uint32_t few_blocks(uint32_t M, uint32_t N, uint32_t K) { return N >= 4096u && (K >= 4096u || M > 16u) ? 2u : 1u; }
 
 // Workgroup -> tile.  Workgroup id % 8 is the XCD; each XCD has a contiguous range of an order in which TILE_GROUP tiles of m are walked together along n, so that the 32
