@@ -216,6 +216,8 @@ def _failed(code: int, name: str) -> None:
 def _general(name: str, *args) -> None:
     """The call by way of ctypes, which takes every integer-like argument and names what it refuses."""
     f = getattr(lib(), name)
+    if len(args) != len(f.argtypes):  # ctypes would pass on what is too many
+        raise TypeError(f"{name} takes {len(f.argtypes)} arguments, not {len(args)}")
     _fit(name, f.argtypes, args)
     args = list(args)
     for i, what in _TENSORS[name]:
@@ -549,13 +551,14 @@ def skiparse_rope(q: torch.Tensor, k: torch.Tensor | None, table: RopeTable, T: 
     if k is not None and (k.shape != q.shape or k.dtype != q.dtype):
         raise ValueError("q and k differ in shape or type")
     data, (lt, lh, lw), (rt, rh, rw) = table
+    t0, h0, w0 = at
     if data.dtype != torch.float32 or data.numel() != 2 * (lt * (rt // 2) + lh * (rh // 2) + lw * (rw // 2)):
         raise ValueError("the table is float32 and as long as its lengths and axes say")
     shape = (s2 * B, n // s2, heads, D) if order == "to_sparse" else (B, n, heads, D) if order == "to_original" else q.shape
     q_out = _into(q_out, shape, q)
     k_out = None if k is None else _into(k_out, shape, q)
     _here(q, k, q_out, k_out, data)
-    _skiparse_rope(q, k, q_out, k_out, data, B, heads, T, H, W, D, rt, rh, rw, lt, lh, lw, *at, s, PATTERNS[pattern], ORDERS[order],
+    _skiparse_rope(q, k, q_out, k_out, data, B, heads, T, H, W, D, rt, rh, rw, lt, lh, lw, t0, h0, w0, s, PATTERNS[pattern], ORDERS[order],
                    ROPE_LAYOUTS[layout], 1 if inverse else 0, _DTYPES[q.dtype], _stream())
     return q_out, k_out
 

@@ -94,3 +94,25 @@ def test_backward_asks_for_what_it_reads_only(monkeypatch):
         with pytest.raises(ValueError):
             sk.skiparse_linear_bwd(*args, **kw)
     assert not calls
+
+
+def test_arguments_of_another_number_are_refused(monkeypatch):
+    """A place with more or fewer than three numbers does not move the arguments behind it; nor does any call by the general way."""
+    monkeypatch.setattr(sk, "_stream", lambda: 0)
+    monkeypatch.setattr(sk, "_here", lambda *t: None)
+    q = torch.zeros(1, 4, 1, 8, dtype=torch.bfloat16)
+    table = sk.RopeTable(torch.zeros(2 * 16 * 4), (1, 1, 16), (0, 0, 8))
+    calls = []
+    with monkeypatch.context() as m:
+        m.setattr(sk, "_skiparse_rope", lambda *a: calls.append(a))
+        sk.skiparse_rope(q, None, table, 1, 1, 4, at=(0, 0, 5))
+        assert len(calls[0]) == len(sk.lib().skiparse_rope.argtypes) and calls.pop()[17:20] == (0, 0, 5)
+        for at in ((0, 0), (0, 0, 0, 0), ()):
+            with pytest.raises(ValueError):
+                sk.skiparse_rope(q, None, table, 1, 1, 4, at=at)
+    assert not calls
+    for name, tensors in sk._TENSORS.items():
+        n = len(getattr(sk.lib(), name).argtypes)
+        for count in (0, n - 1, n + 1):
+            with pytest.raises(TypeError, match="arguments"):
+                sk._general(name, *[1] * count)
