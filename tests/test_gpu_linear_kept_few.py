@@ -109,3 +109,34 @@ def test_rows_that_move(M, order):
     got, kept = sk.skiparse_linear_fwd(x, w, bias, act="silu", keep="checkpoint", order=order, T=T, H=H, W=W, s=2)
     want, ckpt = sk.skiparse_linear_fwd(ref.moved(x, order, (1, T, H, W), 2, "token").contiguous(), w, bias, act="silu", keep="checkpoint")
     assert torch.equal(got, want) and torch.equal(kept.codes, ckpt.codes) and torch.equal(kept.scales, ckpt.scales)
+
+
+@pytest.mark.parametrize("M", [1, 5, 20])
+def test_captured_and_replayed(M):
+    """A few rows forward with a checkpoint, and dx from it without x, in a HIP graph, replayed on new inputs with eager work between."""
+    import paper_2605_28691_amd as sk
+
+    K, N = 520, 1000
+    x, w, bias, dy = _inputs(M, K, N, 40 + M)
+
+    def step():
+        out, pre = sk.skiparse_linear_fwd(x, w, bias, act="silu", keep="checkpoint")
+        dx, _, db = sk.skiparse_linear_bwd(dy, None, w, pre=pre, act="silu", need_dw=False)
+        return out, *pre, dx, db
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for trial in range(3):
+        for t, new in zip((x, w, bias, dy), _inputs(M, K, N, 50 + trial)):
+            t.copy_(new)
+        for t in kept:
+            t.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in kept]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), trial
