@@ -292,6 +292,40 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
                         void* dw, void* db, int B, int T, int H, int W, int in_features, int out_features, int s, int pattern, int order, int act, int dtype,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Root-mean-square norm of rows of `cols` channels (the tokens of a hidden state, or, with heads * rows of head_dim channels, the heads of q and k), bf16 or float32:
+ *   h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h r weight            residual NULL: h = x;  weight NULL: ones
+ * x, residual and sum have their rows on the one side of `order`, out (and out_scales) on the other: a norm in front of a chain of sparse blocks writes the sparse layout, the residual stream
+ *   stays where it is.  rows = B*T*H*W (plain rows: a grid 1 x 1 x rows).
+ *   sum: NULL, or where h, rounded, is kept; only with a residual.  It may be x or residual.  y is made of the sum as it is before that rounding.
+ *   out: y rounded to the type of x, with out_scales NULL; or, with out_scales [rows], the int8 codes and scales of y.  Where rows keep their places out may be x (if it is no codes, and sum is not x).
+ *   Nothing else may overlap.  cols a multiple of 8 up to 32,768; eps > 0.  Sums in float32, and in 64 bits where squares leave its range; one rounding.
+ * Rows in 8-bit integers: m = largest |v| of the row (at least 2^-118), code = rne(v * (127 / m)), scale = m / 127, all decisions in float32, so codes are -127 .. 127 and a value is code * scale.  A row of zeros has scale 1; one
+ *   that holds a value that is not finite has codes 0 and scale NaN, so that what a product makes of it is NaN too.  The norm's codes are those of h weight, which is y up to the row's factor r.
+ * skiparse_quantize_int8: x, rows moved as `order` says, in 8-bit integers: activations in front of a product, or once the weights ([out_features][in_features]: a scale a channel).
+ * skiparse_rmsnorm_bwd: gradients for a loss with dL/dy = dy (rows as out's), h as kept in sum (or x, without a residual; rows as x's):
+ *   g = dy weight, u = h r:  dx = r (g - u mean(g u)) + dx_add,  dweight = sum over the rows of dy u;     dx is x's gradient and the residual's.
+ *   dx_add (what comes along the residual stream; NULL or rows as dx's) may be dx.  dx or dw may be NULL (not wanted).  dw is shaped as weight, in its type.
+ *   workspace: skiparse_rmsnorm_bwd_workspace_bytes() bytes where dw is wanted, else NULL will do.  Deterministic (sums over rows in a fixed order, which may depend on rows and cols and on nothing else).
+ */
+int skiparse_rmsnorm_fwd(const void* x, const void* residual, const void* weight, void* sum, void* out, float* out_scales, int B, int T, int H, int W, int cols,
+                         float eps, int s, int pattern, int order, int dtype, void* stream);
+size_t skiparse_rmsnorm_bwd_workspace_bytes(int rows, int cols);
+int skiparse_rmsnorm_bwd(const void* dy, const void* h, const void* weight, const void* dx_add, void* dx, void* dw, int B, int T, int H, int W, int cols, float eps,
+                         int s, int pattern, int order, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+int skiparse_quantize_int8(const void* x, void* codes, float* scales, int B, int T, int H, int W, int cols, int s, int pattern, int order, int dtype, void* stream);
+
+/*
+ * The linear layer in 8-bit integers: z = x_scales[row] w_scales[channel] sum_k x w + bias,  out = act(z) + residual, with int8 codes x [rows][in_features] and w
+ * [out_features][in_features] (as skiparse_quantize_int8 makes them; any int8 will do), float32 scales, and bias, residual and out in bf16, as skiparse_linear_fwd has them: `order`, act
+ * and which buffers may be the same likewise.  The sums are exact, in 32-bit integers, so a row's bits depend on nothing but the row: what follows is float32, rounded once.
+ * in_features a multiple of 16 up to 131,056 (beyond, a sum could leave 32 bits), out_features a multiple of 8 below 2^23; with rows that move x is less than 4 GiB; a result has
+ * less than 2^24 tiles of 256 x 256.  workspace: skiparse_linear_fwd_int8_workspace_bytes() bytes, NULL where that is 0; it holds nothing between calls, and calls that may overlap need one each.
+ */
+size_t skiparse_linear_fwd_int8_workspace_bytes(int rows, int in_features, int out_features);
+int skiparse_linear_fwd_int8(const void* x, const float* x_scales, const void* w, const float* w_scales, const void* bias, const void* residual, void* out, int B, int T, int H,
+                             int W, int in_features, int out_features, int s, int pattern, int order, int act, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text for an error code; never NULL. */
 const char* skiparse_strerror(int code);
 

@@ -115,6 +115,18 @@ def lib() -> ctypes.CDLL:
         L.skiparse_linear_bwd_workspace_bytes.argtypes = [i] * 6
         L.skiparse_linear_bwd.restype = i
         L.skiparse_linear_bwd.argtypes = [vp] * 10 + [i] * 11 + [vp, sz, vp]
+        L.skiparse_rmsnorm_fwd.restype = i
+        L.skiparse_rmsnorm_fwd.argtypes = [vp] * 6 + [i] * 5 + [f] + [i] * 4 + [vp]
+        L.skiparse_rmsnorm_bwd_workspace_bytes.restype = sz
+        L.skiparse_rmsnorm_bwd_workspace_bytes.argtypes = [i] * 2
+        L.skiparse_rmsnorm_bwd.restype = i
+        L.skiparse_rmsnorm_bwd.argtypes = [vp] * 6 + [i] * 5 + [f] + [i] * 4 + [vp, sz, vp]
+        L.skiparse_quantize_int8.restype = i
+        L.skiparse_quantize_int8.argtypes = [vp] * 3 + [i] * 9 + [vp]
+        L.skiparse_linear_fwd_int8_workspace_bytes.restype = sz
+        L.skiparse_linear_fwd_int8_workspace_bytes.argtypes = [i] * 3
+        L.skiparse_linear_fwd_int8.restype = i
+        L.skiparse_linear_fwd_int8.argtypes = [vp] * 7 + [i] * 10 + [vp, sz, vp]
         _bind(L)
         _lib = L
     return _lib
@@ -177,6 +189,10 @@ _TENSORS = {
     "skiparse_linear_fwd": ((0, "x"), (1, "w"), (2, "bias"), (3, "residual"), (4, "out"), (5, "pre"), (6, "pre_scales"), (18, "workspace")),
     "skiparse_linear_bwd": ((0, "dy"), (1, "x"), (2, "x_scales"), (3, "w"), (4, "pre"), (5, "pre_scales"), (6, "dx_add"), (7, "dx"), (8, "dw"), (9, "db"),
                             (21, "workspace")),
+    "skiparse_rmsnorm_fwd": ((0, "x"), (1, "residual"), (2, "weight"), (3, "total"), (4, "out"), (5, "scales")),
+    "skiparse_rmsnorm_bwd": ((0, "dy"), (1, "h"), (2, "weight"), (3, "dx_add"), (4, "dx"), (5, "dw"), (16, "workspace")),
+    "skiparse_quantize_int8": ((0, "x"), (1, "codes"), (2, "scales")),
+    "skiparse_linear_fwd_int8": ((0, "x"), (1, "x's scales"), (2, "w"), (3, "w's scales"), (4, "bias"), (5, "residual"), (6, "out"), (17, "workspace")),
 }
 # Those that a call can do without.
 _OPTIONAL = {
@@ -184,6 +200,9 @@ _OPTIONAL = {
     "skiparse_rope": {1, 3},
     "skiparse_linear_fwd": {2, 3, 5, 6, 18},
     "skiparse_linear_bwd": {1, 2, 3, 4, 5, 6, 7, 8, 9, 21},
+    "skiparse_rmsnorm_fwd": {1, 2, 3, 5},
+    "skiparse_rmsnorm_bwd": {2, 3, 4, 5, 16},
+    "skiparse_linear_fwd_int8": {4, 5, 17},
 }
 
 
@@ -723,3 +742,127 @@ def skiparse_linear_bwd(dy: torch.Tensor, x, w: torch.Tensor | None, pre=None, a
     workspace, size = _space(workspace, dy, "skiparse_linear_bwd_workspace_bytes", M, K, N, ORDERS[order], ACTS[act], 0 if xs is None else 1)
     _skiparse_linear_bwd(dy, xc, xs, w, codes, scales, dx_add, dx, dw, db, *grid, K, N, s, PATTERNS[pattern], ORDERS[order], ACTS[act], BF16, workspace, size, _stream())
     return dx, dw, db
+
+
+class Quantized(NamedTuple):
+    """Rows in 8-bit integers: codes (int8) of the rows' shape, and one float32 scale a row: a value is code * scale."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _quantized_of(shape, like) -> Quantized:
+    return Quantized(like.new_empty(shape, dtype=torch.int8), like.new_empty(shape[:-1], dtype=torch.float32))
+
+
+def _is_quantized(q, what: str, shape=None) -> Quantized:
+    if not isinstance(q, Quantized):
+        raise ValueError(f"{what} must be Quantized")
+    shape = tuple(q.codes.shape) if shape is None else tuple(shape)
+    if q.codes.dtype != torch.int8 or q.scales.dtype != torch.float32 or tuple(q.codes.shape) != shape or tuple(q.scales.shape) != shape[:-1]:
+        raise ValueError(f"{what}: not int8 codes of shape {shape} with a float32 scale a row")
+    return q
+
+
+def _same_type(like, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != like.dtype:
+            raise ValueError(f"tensors of one type are needed, {like.dtype} here")
+
+
+def _of_channels(weight, cols: int) -> None:
+    if weight is not None and tuple(weight.shape) != (cols,):
+        raise ValueError(f"weight must have shape ({cols},)")
+
+
+def skiparse_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, residual: torch.Tensor | None = None, eps: float = 1e-6, order: str = "same", T: int = 0,
+                         H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", quantize: bool = False, out=None, total: torch.Tensor | None = None):
+    """h / sqrt(mean(h^2) + eps) * weight over the last dimension, h = x + residual: the result, or with a residual (result, h).  bf16 or float32, all of one type; h is rounded to it, the result made
+    of what it is before that.  quantize=True: the result as Quantized, for skiparse_linear_fwd_int8.  order "to_sparse" or "to_original" moves the rows of the grid T x H x W on the way: x, residual and h
+    are [B][T*H*W][channels] or [s*s*B][T*H*W/(s*s)][channels], the result the other; h stays where x is.  `out` and `total` (of h; may be residual or x) are buffers to use; out may be x where rows stay."""
+    cols = x.shape[-1]
+    grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
+    _of_channels(weight, cols)
+    _same_type(x, weight, residual)
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError(f"residual must have the shape of x, {tuple(x.shape)}")
+    if total is not None and residual is None:
+        raise ValueError("without a residual the sum is x")
+    shape, scales = (*lead, cols), None
+    if quantize:
+        codes, scales = out = _quantized_of(shape, x) if out is None else _is_quantized(out, "out", shape)
+    else:
+        codes = out = _into(out, shape, x)
+    if residual is not None:
+        total = _into(total, x.shape, x)
+    _here(x, weight, residual, total, codes, scales)
+    _skiparse_rmsnorm_fwd(x, residual, weight, total, codes, scales, *grid, cols, float(eps), s, PATTERNS[pattern], ORDERS[order], _DTYPES[x.dtype], _stream())
+    return out if residual is None else (out, total)
+
+
+def skiparse_rmsnorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return _size("skiparse_rmsnorm_bwd_workspace_bytes", rows, cols)
+
+
+def skiparse_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None = None, dx_add: torch.Tensor | None = None, eps: float = 1e-6, order: str = "same",
+                         T: int = 0, H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", need_dx: bool = True, need_dw: bool = True, dx: torch.Tensor | None = None,
+                         dw: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Gradients (dx, dweight) of skiparse_rmsnorm_fwd for dL/dresult = dy; None for one that is not needed.  h: what the forward call returned beside its result, or its x where it had no residual.
+    dx is the gradient of x and of the residual, with dx_add, what comes along the residual stream, added to it; dx_add may be dx."""
+    if not (need_dx or need_dw):
+        return None, None
+    cols = h.shape[-1]
+    grid, back = _linear_rows(dy.shape[:-1], _BACK[order], T, H, W, s)
+    if dy.shape[-1] != cols or tuple(h.shape) != (*back, cols) or (dx_add is not None and dx_add.shape != h.shape):
+        raise ValueError("dy, h or dx_add does not have its shape")
+    _of_channels(weight, cols)
+    _same_type(h, dy, weight, dx_add)
+    dx = _into(dx, h.shape, h) if need_dx else None
+    dw = _into(dw, (cols,), h) if need_dw else None
+    _here(dy, h, weight, dx_add, dx, dw, workspace)
+    size = 0
+    if need_dw:
+        workspace, size = _space(workspace, h, "skiparse_rmsnorm_bwd_workspace_bytes", grid[0] * grid[1] * grid[2] * grid[3], cols)
+    else:
+        workspace = None
+    _skiparse_rmsnorm_bwd(dy, h, weight, dx_add, dx, dw, *grid, cols, float(eps), s, PATTERNS[pattern], ORDERS[order], _DTYPES[h.dtype], workspace, size, _stream())
+    return dx, dw
+
+
+def skiparse_quantize_int8(x: torch.Tensor, order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", out: Quantized | None = None) -> Quantized:
+    """[..., channels] in bf16 or float32 -> int8 codes and a float32 scale a row: activations in front of skiparse_linear_fwd_int8, or once its weights [out, in].  order moves rows on the way, as in
+    skiparse_rmsnorm_fwd."""
+    grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
+    shape = (*lead, x.shape[-1])
+    out = _quantized_of(shape, x) if out is None else _is_quantized(out, "out", shape)
+    _here(x, *out)
+    _skiparse_quantize_int8(x, out.codes, out.scales, *grid, x.shape[-1], s, PATTERNS[pattern], ORDERS[order], _DTYPES[x.dtype], _stream())
+    return out
+
+
+def skiparse_linear_fwd_int8_workspace_bytes(rows: int, in_features: int, out_features: int) -> int:
+    return _size("skiparse_linear_fwd_int8_workspace_bytes", rows, in_features, out_features)
+
+
+def skiparse_linear_fwd_int8(x: Quantized, w: Quantized, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None, act: str = "none", order: str = "same", T: int = 0,
+                             H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """act(x w^T + bias) + residual in bf16 from 8-bit integers: x [..., in] and w [out, in] as skiparse_quantize_int8 or skiparse_rmsnorm_fwd leave them, bias [out], residual and result
+    [..., out] bf16.  order as in skiparse_linear_fwd; the scales' rows move with the codes'.  `out` (may be residual) and `workspace` are buffers to use."""
+    _is_quantized(x, "x")
+    _is_quantized(w, "w")
+    if w.codes.dim() != 2:
+        raise ValueError("w is [out, in]")
+    K, (N, Kw) = x.codes.shape[-1], w.codes.shape
+    if K != Kw or (bias is not None and tuple(bias.shape) != (N,)):
+        raise ValueError("x, w and bias do not fit each other")
+    _bf16("bias and residual", bias, residual)
+    grid, lead = _linear_rows(x.codes.shape[:-1], order, T, H, W, s)
+    shape = (*lead, N)
+    out = _into(out, shape, x.codes, torch.bfloat16)
+    if residual is not None and tuple(residual.shape) != shape:
+        raise ValueError(f"residual must have the result's shape {shape}")
+    _here(*x, *w, bias, residual, out, workspace)
+    M = grid[0] * grid[1] * grid[2] * grid[3]
+    workspace, size = _space(workspace, x.codes, "skiparse_linear_fwd_int8_workspace_bytes", M, K, N)
+    _skiparse_linear_fwd_int8(x.codes, x.scales, w.codes, w.scales, bias, residual, out, *grid, K, N, s, PATTERNS[pattern], ORDERS[order], ACTS[act], workspace, size, _stream())
+    return out

@@ -814,6 +814,145 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
     return SKIPARSE_OK;
 }
 
+// ---- root-mean-square norm, rows in 8-bit integers
+
+// Sizes, enums and the row map; `moved`: rows change places.
+static int rows_common(int B, int T, int H, int W, int cols, int s, int pattern, int order, int dtype, bool* moved, size_t* rows) {
+    if (!valid_order(order, false) || elem_size(dtype) == 0) return SKIPARSE_EINVAL;
+    *moved = order != SKIPARSE_ORDER_SAME && s != 1;
+    Shape sh;
+    const int rc = *moved ? check_shape(B, 1, T, H, W, cols, s, pattern, &sh) : check_rows(B, 1, T, H, W, cols, &sh);
+    if (rc != SKIPARSE_OK) return rc;
+    if (dtype == SKIPARSE_FP8_E4M3 || cols % 8 != 0 || (uint32_t)cols > NORM_MAX_COLS) return SKIPARSE_EUNSUPPORTED;
+    *rows = (size_t)B * sh.n_tok;
+    return SKIPARSE_OK;
+}
+// Which row of the source a row of the destination takes, where rows move from the original order to the sparse layout or back.
+static RowArgs row_args(int B, int T, int H, int W, int s, int pattern, bool to_sparse) {
+    const GridMap g = make_gridmap(T, H, W, s, pattern);
+    return to_sparse ? make_row_args<TO_SPARSE>(g, (uint32_t)B) : make_row_args<TO_ORIGINAL>(g, (uint32_t)B);
+}
+// a finite number above zero
+static bool valid_eps(float eps) { return eps >= 1.17549435e-38f && eps <= 3.0e38f; }
+
+int skiparse_rmsnorm_fwd(const void* x, const void* residual, const void* weight, void* sum, void* out, float* out_scales, int B, int T, int H, int W, int cols,
+                         float eps, int s, int pattern, int order, int dtype, void* stream) {
+    if (!x || !out || (sum && !residual) || !valid_eps(eps)) return SKIPARSE_EINVAL;
+    bool moved;
+    size_t rows;
+    const int rc = rows_common(B, T, H, W, cols, s, pattern, order, dtype, &moved, &rows);
+    if (rc != SKIPARSE_OK) return rc;
+    for (const void* p : {x, residual, weight, (const void*)sum, (const void*)out, (const void*)out_scales})
+        if (p && misaligned(p)) return SKIPARSE_EINVAL;
+    const size_t bytes = rows * cols * elem_size(dtype);
+    const Span sx = {x, bytes}, sr = {residual, bytes}, sw = {weight, (size_t)cols * elem_size(dtype)}, ss = {sum, bytes};
+    const Span so = {out, out_scales ? rows * cols : bytes}, sc = {out_scales, rows * sizeof(float)};
+    if (touches(so, {sr, sw, ss, sc}) || touches(sc, {sx, sr, sw, ss}) || touches(ss, {sw})) return SKIPARSE_EINVAL;
+    if (touches(so, {sx}) && (out != x || moved || out_scales)) return SKIPARSE_EINVAL;
+    if ((touches(ss, {sx}) && sum != x) || (touches(ss, {sr}) && sum != residual)) return SKIPARSE_EINVAL;
+    NormArgs a = {};
+    a.x = x; a.residual = residual; a.weight = weight; a.sum = sum; a.out = out; a.scales = out_scales;
+    a.n_rows = (uint32_t)rows; a.cols = (uint32_t)cols;
+    a.eps = eps;
+    a.kind = out_scales ? ROWS_NORM_QUANTIZED : ROWS_NORM;
+    a.f32 = dtype == SKIPARSE_FP32;
+    a.order = moved ? order : SKIPARSE_ORDER_SAME;
+    if (moved) a.rows = row_args(B, T, H, W, s, pattern, order == SKIPARSE_ORDER_TO_SPARSE);
+    return finish(launch_norm_rows(a, (hipStream_t)stream));
+}
+
+int skiparse_quantize_int8(const void* x, void* codes, float* scales, int B, int T, int H, int W, int cols, int s, int pattern, int order, int dtype, void* stream) {
+    if (!x || !codes || !scales) return SKIPARSE_EINVAL;
+    bool moved;
+    size_t rows;
+    const int rc = rows_common(B, T, H, W, cols, s, pattern, order, dtype, &moved, &rows);
+    if (rc != SKIPARSE_OK) return rc;
+    if (misaligned(x) || misaligned(codes) || misaligned(scales)) return SKIPARSE_EINVAL;
+    const Span sx = {x, rows * cols * elem_size(dtype)}, so = {codes, rows * cols}, sc = {scales, rows * sizeof(float)};
+    if (touches(so, {sx, sc}) || touches(sc, {sx})) return SKIPARSE_EINVAL;
+    NormArgs a = {};
+    a.x = x; a.out = codes; a.scales = scales;
+    a.n_rows = (uint32_t)rows; a.cols = (uint32_t)cols;
+    a.kind = ROWS_QUANTIZED;
+    a.f32 = dtype == SKIPARSE_FP32;
+    a.order = moved ? order : SKIPARSE_ORDER_SAME;
+    if (moved) a.rows = row_args(B, T, H, W, s, pattern, order == SKIPARSE_ORDER_TO_SPARSE);
+    return finish(launch_norm_rows(a, (hipStream_t)stream));
+}
+
+size_t skiparse_rmsnorm_bwd_workspace_bytes(int rows, int cols) {
+    if (rows < 1 || cols < 1 || (uint32_t)cols > NORM_MAX_COLS) return 0;
+    return (size_t)norm_bwd_parts((uint32_t)rows, (uint32_t)cols) * (size_t)cols * sizeof(float);
+}
+
+int skiparse_rmsnorm_bwd(const void* dy, const void* h, const void* weight, const void* dx_add, void* dx, void* dw, int B, int T, int H, int W, int cols, float eps,
+                         int s, int pattern, int order, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!dy || !h || (!dx && !dw) || (dx_add && !dx) || !valid_eps(eps)) return SKIPARSE_EINVAL;
+    bool moved;
+    size_t rows;
+    const int rc = rows_common(B, T, H, W, cols, s, pattern, order, dtype, &moved, &rows);
+    if (rc != SKIPARSE_OK) return rc;
+    for (const void* p : {dy, h, weight, dx_add, (const void*)dx, (const void*)dw})
+        if (p && misaligned(p)) return SKIPARSE_EINVAL;
+    const size_t need = dw ? skiparse_rmsnorm_bwd_workspace_bytes((int)rows, cols) : 0;
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
+    const size_t bytes = rows * cols * elem_size(dtype), wbytes = (size_t)cols * elem_size(dtype);
+    const Span sy = {dy, bytes}, sh = {h, bytes}, sw = {weight, wbytes}, sa = {dx_add, bytes}, gx = {dx, bytes}, gw = {dw, wbytes}, ws = {need ? workspace : nullptr, need};
+    if (touches(gx, {sy, sh, sw, gw, ws}) || touches(gw, {sy, sh, sw, sa, ws}) || touches(ws, {sy, sh, sw, sa})) return SKIPARSE_EINVAL;
+    if (touches(gx, {sa}) && dx_add != dx) return SKIPARSE_EINVAL;
+    NormBwdArgs a = {};
+    a.dy = dy; a.h = h; a.weight = weight; a.dx_add = dx_add; a.dx = dx; a.dw = dw;
+    a.parts = (float*)workspace;
+    a.n_rows = (uint32_t)rows; a.cols = (uint32_t)cols;
+    a.eps = eps;
+    a.f32 = dtype == SKIPARSE_FP32;
+    if (moved) {  // row of x -> row of the result that was made of it
+        const bool back = order == SKIPARSE_ORDER_TO_SPARSE;
+        a.order = back ? SKIPARSE_ORDER_TO_ORIGINAL : SKIPARSE_ORDER_TO_SPARSE;
+        a.rows = row_args(B, T, H, W, s, pattern, !back);
+    }
+    return finish(launch_norm_bwd(a, (hipStream_t)stream));
+}
+
+// ---- linear layer in 8-bit integers
+
+constexpr int INT8_MAX_FEATURES = 131056;  // 2^14 a product: 2^31 / 2^14 of them could leave 32 bits
+
+size_t skiparse_linear_fwd_int8_workspace_bytes(int rows, int in_features, int out_features) {
+    if (rows < 1 || in_features < 1 || out_features < 1) return 0;
+    return linear_int8_workspace((uint32_t)rows, (uint32_t)out_features, (uint32_t)in_features);
+}
+
+int skiparse_linear_fwd_int8(const void* x, const float* x_scales, const void* w, const float* w_scales, const void* bias, const void* residual, void* out, int B, int T, int H,
+                             int W, int in_features, int out_features, int s, int pattern, int order, int act, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!x || !x_scales || !w || !w_scales || !out) return SKIPARSE_EINVAL;
+    bool moved;
+    size_t rows;
+    const int rc = linear_common(B, T, H, W, in_features, out_features, s, pattern, order, act, SKIPARSE_BF16, &moved, &rows);
+    if (rc != SKIPARSE_OK) return rc;
+    if (in_features % 16 != 0) return SKIPARSE_EUNSUPPORTED;
+    if (in_features > INT8_MAX_FEATURES) return SKIPARSE_ESHAPE;
+    for (const void* p : {x, (const void*)x_scales, w, (const void*)w_scales, bias, residual, (const void*)out})
+        if (p && misaligned(p)) return SKIPARSE_EINVAL;
+    const size_t K = (size_t)in_features, N = (size_t)out_features;
+    if (!linear_fits(rows, N)) return SKIPARSE_ESHAPE;
+    if (moved && rows * K >= (1ull << 32) - 64) return SKIPARSE_ESHAPE;  // rows that move are addressed with 32-bit byte offsets
+    const Span sx = {x, rows * K}, sxs = {x_scales, rows * sizeof(float)}, sw = {w, N * K}, sws = {w_scales, N * sizeof(float)}, sb = {bias, N * 2}, sr = {residual, rows * N * 2};
+    const Span so = {out, rows * N * 2};
+    if (touches(so, {sx, sxs, sw, sws, sb}) || (residual != out && touches(so, {sr}))) return SKIPARSE_EINVAL;
+    const size_t need = linear_int8_workspace((uint32_t)rows, (uint32_t)N, (uint32_t)K);
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
+    if (touches({need ? workspace : nullptr, need}, {sx, sxs, sw, sws, sb, sr, so})) return SKIPARSE_EINVAL;
+    LinearInt8Args a = {};
+    a.x = x; a.x_scales = x_scales; a.w = w; a.w_scales = w_scales; a.bias = bias; a.residual = residual; a.out = out;
+    a.M = (uint32_t)rows; a.N = (uint32_t)N; a.K = (uint32_t)K;
+    a.act = act;
+    a.order = moved ? order : SKIPARSE_ORDER_SAME;
+    if (moved) a.rows = row_args(B, T, H, W, s, pattern, order == SKIPARSE_ORDER_TO_SPARSE);
+    a.partial = workspace;
+    return finish(launch_linear_int8(a, (hipStream_t)stream));
+}
+
 const char* skiparse_strerror(int code) {
     switch (code) {
         case SKIPARSE_OK: return "ok";

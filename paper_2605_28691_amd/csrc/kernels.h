@@ -230,4 +230,61 @@ struct LinearRowsArgs {
 };
 hipError_t launch_linear_rows(const LinearRowsArgs& a, hipStream_t stream);
 
+// Root-mean-square norm of rows, its result as it is or in 8-bit integers, and rows in 8-bit integers without a norm.
+constexpr uint32_t NORM_MAX_COLS = 32768;
+enum RowsKind : int { ROWS_NORM = 0, ROWS_NORM_QUANTIZED = 1, ROWS_QUANTIZED = 2 };
+struct NormArgs {
+    const void* x;
+    const void* residual;  // or null
+    const void* weight;    // or null: ones
+    void* sum;             // x + residual, rows as x's, or null; may be x or residual
+    void* out;             // as x, or int8 codes
+    float* scales;         // of the codes
+    uint32_t n_rows, cols;
+    float eps;
+    int kind;
+    bool f32;
+    int order;             // ORDER_SAME, or the row map from which a row of the result takes its row of x
+    RowArgs rows;
+    uint32_t first;        // set by the launcher
+    float per_n;
+};
+hipError_t launch_norm_rows(const NormArgs& a, hipStream_t stream);
+
+struct NormBwdArgs {
+    const void* dy;
+    const void* h;
+    const void* weight;    // or null: ones
+    const void* dx_add;    // or null; may be dx
+    void* dx;              // or null
+    void* dw;              // or null
+    float* parts;          // [norm_bwd_parts(n_rows, cols)][cols] where dw is wanted
+    uint32_t n_rows, cols;
+    float eps;
+    bool f32;
+    int order;             // from the result's order back to h's
+    RowArgs rows;
+    float per_n;           // set by the launcher
+};
+uint32_t norm_bwd_parts(uint32_t rows, uint32_t cols);
+hipError_t launch_norm_bwd(const NormBwdArgs& a, hipStream_t stream);
+
+// The linear layer in 8-bit integers.
+struct LinearInt8Args {
+    const void* x;           // int8 [M][K]
+    const float* x_scales;   // [M]
+    const void* w;           // int8 [N][K]
+    const float* w_scales;   // [N]
+    const void* bias;        // bf16 [N] or null
+    const void* residual;    // bf16 [M][N] or null; may be out
+    void* out;               // bf16 [M][N]
+    uint32_t M, N, K;
+    int act;
+    int order;               // ORDER_SAME, or the row map from which row m of out takes its row of x
+    RowArgs rows;
+    void* partial;           // linear_int8_workspace() bytes
+};
+size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K);
+hipError_t launch_linear_int8(const LinearInt8Args& a, hipStream_t stream);
+
 }  // namespace skiparse

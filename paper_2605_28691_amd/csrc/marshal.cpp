@@ -189,7 +189,11 @@ constexpr unsigned at(int i, I... more) { return 1u << i | at(more...); }
     X(skiparse_checkpoint_save, NEVER) \
     X(skiparse_checkpoint_load, NEVER) \
     X(skiparse_linear_fwd, at(2, 3, 5, 6, 18)) \
-    X(skiparse_linear_bwd, at(1, 2, 3, 4, 5, 6, 7, 8, 9, 21))
+    X(skiparse_linear_bwd, at(1, 2, 3, 4, 5, 6, 7, 8, 9, 21)) \
+    X(skiparse_rmsnorm_fwd, at(1, 2, 3, 5)) \
+    X(skiparse_rmsnorm_bwd, at(2, 3, 4, 5, 16)) \
+    X(skiparse_quantize_int8, NEVER) \
+    X(skiparse_linear_fwd_int8, at(4, 5, 17))
 ENTRIES(SLOT)
 ENTRIES(ENTRY)
 
