@@ -943,13 +943,13 @@ int skiparse_linear_fwd_int8(const void* x, const float* x_scales, const void* w
     const size_t need = linear_int8_workspace((uint32_t)rows, (uint32_t)N, (uint32_t)K);
     if (need && (!workspace || workspace_bytes < need || misaligned(workspace))) return SKIPARSE_EWORKSPACE;
     if (touches({need ? workspace : nullptr, need}, {sx, sxs, sw, sws, sb, sr, so})) return SKIPARSE_EINVAL;
-    LinearInt8Args a = {};
-    a.x = x; a.x_scales = x_scales; a.w = w; a.w_scales = w_scales; a.bias = bias; a.residual = residual; a.out = out;
-    a.M = (uint32_t)rows; a.N = (uint32_t)N; a.K = (uint32_t)K;
-    a.act = act;
+    LinearArgs a = {};
+    a.p = x; a.q = w; a.x_scales = x_scales; a.w_scales = w_scales;
+    a.M = (uint32_t)rows; a.N = (uint32_t)N; a.K = (uint32_t)K / 2u;
+    a.e = {bias, residual, out, nullptr, nullptr, act};
+    a.partial = (float*)workspace;
     a.order = moved ? order : SKIPARSE_ORDER_SAME;
     if (moved) a.rows = row_args(B, T, H, W, s, pattern, order == SKIPARSE_ORDER_TO_SPARSE);
-    a.partial = workspace;
     return finish(launch_linear_int8(a, (hipStream_t)stream));
 }
 

@@ -192,7 +192,7 @@ struct RopeScaling {
 hipError_t launch_rope_table(float* table, RopeAxis t, RopeAxis h, RopeAxis w, const RopeScaling& s, hipStream_t stream);
 
 // Products of the linear layer.  C[m][n] = sum_k P(m, k) Q(n, k), P given as [m][k] or, transposed, as [k][m], Q likewise.
-enum LinearForm : int { LINEAR_FWD = 0, LINEAR_DX = 1, LINEAR_DW = 2 };  // neither, Q, both transposed
+enum LinearForm : int { LINEAR_FWD = 0, LINEAR_DX = 1, LINEAR_DW = 2, LINEAR_INT8 = 3 };  // neither, Q, both transposed; neither, in 8-bit integers
 enum LinearAct : int { ACT_NONE = 0, ACT_GELU_TANH = 1, ACT_SILU = 2 };
 // What happens to C on the way out: z = C + bias, kept in pre; out = act(z) + residual.
 struct LinearEpilogue {
@@ -211,6 +211,8 @@ struct LinearArgs {
     int order;     // ORDER_SAME, or the row map from which row m of C takes its row of P (LINEAR_FWD only)
     RowArgs rows;
     float* partial;  // linear_workspace() bytes
+    const float* x_scales;  // LINEAR_INT8: of the rows of p and of q.  K counts pairs of codes then, 16 bits as in the other forms
+    const float* w_scales;
 };
 size_t linear_workspace(int form, uint32_t M, uint32_t N, uint32_t K);
 hipError_t launch_linear(int form, const LinearArgs& a, hipStream_t stream);
@@ -269,22 +271,8 @@ struct NormBwdArgs {
 uint32_t norm_bwd_parts(uint32_t rows, uint32_t cols);
 hipError_t launch_norm_bwd(const NormBwdArgs& a, hipStream_t stream);
 
-// The linear layer in 8-bit integers.
-struct LinearInt8Args {
-    const void* x;           // int8 [M][K]
-    const float* x_scales;   // [M]
-    const void* w;           // int8 [N][K]
-    const float* w_scales;   // [N]
-    const void* bias;        // bf16 [N] or null
-    const void* residual;    // bf16 [M][N] or null; may be out
-    void* out;               // bf16 [M][N]
-    uint32_t M, N, K;
-    int act;
-    int order;               // ORDER_SAME, or the row map from which row m of out takes its row of x
-    RowArgs rows;
-    void* partial;           // linear_int8_workspace() bytes
-};
+// The linear layer in 8-bit integers: M rows, N channels, K codes of a row; a.K in pairs of codes.
 size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K);
-hipError_t launch_linear_int8(const LinearInt8Args& a, hipStream_t stream);
+hipError_t launch_linear_int8(const LinearArgs& a, hipStream_t stream);
 
 }  // namespace skiparse

@@ -1,57 +1,97 @@
 // The linear layer in 8-bit integers: out = act(sx[m] sw[n] sum_k x[m][k] w[n][k] + bias) + residual, x and w int8, sums exact in int32, the rest in float32, rounded once to bf16.
-#include "kernels.h"
-#include "linear_act.h"
+// The products are those of linear_tiles.h with v_mfma_i32_16x16x64_i8: its operands are 16 bytes a lane, as those of the bf16 product are, and k is summed over, so the walk over k, what it
+// loads and how it lies in LDS are the same bytes, two codes in the place of one number.  What is left of the sums on the way out are scales: those of a wavefront's rows and channels are asked for before
+// its walk begins.  Parts of a sum are whole numbers too: however a product is cut, a row's bits are the same.
+#include "linear_tiles.h"
 
 namespace skiparse {
 
-typedef __attribute__((ext_vector_type(4))) int i32x4;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-
-// A wavefront has 16 rows and 64 channels, and reads its fragments from memory: lane l 16 bytes of row l % 16 from k = 16 (l / 16).
-__global__ __launch_bounds__(256) void linear_int8_kernel(LinearInt8Args a, uint32_t blocks_m) {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, li = lane & 15u, g = lane >> 4;
-    const uint32_t m = (blockIdx.x % blocks_m * 4u + wave) * 16u + li, n0 = blockIdx.x / blocks_m * 64u;
-    const uint32_t mc = m < a.M ? m : a.M - 1u;
-    const uint32_t from = a.order == 1 ? source_row<TO_SPARSE>(a.rows, mc, 0u) : a.order == 2 ? source_row<TO_ORIGINAL>(a.rows, mc, 0u) : mc;
-    const char* const x = (const char*)a.x + (size_t)from * a.K;
-    const i32x4 zero = {0, 0, 0, 0};
-    i32x4 acc[4] = {zero, zero, zero, zero};
-    for (uint32_t k = 0; k < a.K; k += 64u) {
-        const uint32_t at = k + 16u * g;
-        const i32x4 p = at < a.K ? *(const i32x4*)(x + at) : zero;
+// One row: a wavefront has CH channels and reads 2048 codes of each at once; four products an instruction (v_dot4_i32_i8).
+template <int CH>
+__global__ __launch_bounds__(256) void linear_int8_row_kernel(LinearArgs a) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    constexpr int AT_ONCE = 2;  // times 1024 codes
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n0 = (blockIdx.x * 4u + wave) * CH;
+    if (n0 >= a.N) return;
+    const uint32_t ld = a.K * 2u;  // bytes
+    int acc[CH];
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const uint32_t n = n0 + 16u * j + li;
-            const i32x4 q = at < a.K && n < a.N ? *(const i32x4*)((const char*)a.w + (size_t)n * a.K + at) : zero;
-            acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q, p, acc[j], 0, 0, 0);
+    for (int c = 0; c < CH; c++) acc[c] = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+    // N is a multiple of 8, so a wavefront's channels are all there
+    const auto wb = __builtin_amdgcn_make_buffer_rsrc((char*)a.q + (size_t)n0 * ld, 0, LIN_RECORDS, 0x27000);
+    const auto xb = __builtin_amdgcn_make_buffer_rsrc((char*)a.p, 0, LIN_RECORDS, 0x27000);
+    for (uint32_t k = 0; k < ld; k += 1024u * AT_ONCE) {
+        u32x4 w[AT_ONCE][CH], x[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) {
+            const uint32_t at = k + 1024u * u + lane * 16u;  // behind the end: zeros
+#pragma unroll
+            for (int c = 0; c < CH; c++) w[u][c] = __builtin_amdgcn_raw_buffer_load_b128(wb, at < ld ? at + c * ld : LIN_OUTSIDE, 0, 0);
+            x[u] = __builtin_amdgcn_raw_buffer_load_b128(xb, at < ld ? at : LIN_OUTSIDE, 0, 0);
         }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+#pragma unroll
+                for (int c = 0; c < CH; c++) acc[c] = __builtin_amdgcn_sdot4((int)w[u][c][e], (int)x[u][e], acc[c], false);
     }
-    if (m >= a.M) return;
-    const float sx = a.x_scales[from];
+#endif
+    int sum = 0;  // lane c takes that of channel c
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        const uint32_t n = n0 + 16u * j + 4u * g;
-        if (n >= a.N) continue;
-        bf16x4 y;
+    for (int c = 0; c < CH; c++) {
+        int s = acc[c];
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            float z = fmaf((float)acc[j][e] * sx, a.w_scales[n + e], a.bias != nullptr ? (float)((const __bf16*)a.bias)[n + e] : 0.f);
-            z = act_value(a.act, z);
-            if (a.residual != nullptr) z += (float)((const __bf16*)a.residual)[(size_t)m * a.N + n + e];
-            y[e] = (__bf16)z;
-        }
-        *(bf16x4*)((__bf16*)a.out + (size_t)m * a.N + n) = y;
+        for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
+        if (lane == (uint32_t)c) sum = s;
+    }
+    if (lane >= CH) return;
+    const uint32_t n = n0 + lane;
+    const LinearEpilogue& e = a.e;
+    float z = act_value(e.act, int8_value(sum, a.x_scales[0], a.w_scales[n], e.bias != nullptr ? (float)((const __bf16*)e.bias)[n] : 0.f));
+    if (e.residual != nullptr) z = int8_plus(z, (float)((const __bf16*)e.residual)[n]);
+    ((__bf16*)e.out)[n] = (__bf16)z;
+}
+
+template <int CH>
+static hipError_t launch_row8(const LinearArgs& a, hipStream_t stream) {
+    constexpr uint32_t per = CH * 4u;
+    linear_int8_row_kernel<CH><<<(a.N + per - 1u) / per, 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+template <int FM, int FN>
+static hipError_t launch_few8(const LinearArgs& a, hipStream_t stream) {
+    constexpr uint32_t per = 16u * FN;
+    linear_few_kernel<FM, FN, false, LINEAR_INT8><<<(a.N + per - 1u) / per, 64 * FEW_WAVES, 0, stream>>>(a);
+    return hipGetLastError();
+}
+static hipError_t launch_few8(const LinearArgs& a, hipStream_t stream) {
+    if (a.M == 1u) {  // moved or not, row 0
+        const uint32_t channels = row_channels(a.N);
+        return channels == 1u ? launch_row8<1>(a, stream) : channels == 2u ? launch_row8<2>(a, stream) : launch_row8<4>(a, stream);
+    }
+    if (few_blocks(a.M, a.N, a.K) == 2u) return a.M <= 16u ? launch_few8<1, 2>(a, stream) : launch_few8<2, 2>(a, stream);
+    return a.M <= 16u ? launch_few8<1, 1>(a, stream) : launch_few8<2, 1>(a, stream);
+}
+
+template <bool EXTRAS>
+static hipError_t launch_int8(const LinearArgs& a, hipStream_t stream) {
+    const LinearPlan p = plan_linear(a.M, a.N, a.K);
+    switch (p.shape) {
+        case T256: return launch_tiles<T256, LINEAR_INT8, EXTRAS>(a, p, stream);
+        case T128: return launch_tiles<T128, LINEAR_INT8, EXTRAS>(a, p, stream);
+        case T128X256: return launch_tiles<T128X256, LINEAR_INT8, EXTRAS>(a, p, stream);
+        default: return launch_tiles<T64, LINEAR_INT8, EXTRAS>(a, p, stream);
     }
 }
 
-size_t linear_int8_workspace(uint32_t, uint32_t, uint32_t) { return 0; }
+size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K) { return linear_few(M, K / 2u) ? 0u : plan_linear(M, N, K / 2u).workspace(); }
 
-hipError_t launch_linear_int8(const LinearInt8Args& a, hipStream_t stream) {
-    const uint64_t bm = ((uint64_t)a.M + 63u) / 64u, bn = ((uint64_t)a.N + 63u) / 64u;
-    if (!fits_grid(bm * bn, 256u)) return hipErrorInvalidConfiguration;
-    linear_int8_kernel<<<(uint32_t)(bm * bn), 256, 0, stream>>>(a, (uint32_t)bm);
-    return hipGetLastError();
+hipError_t launch_linear_int8(const LinearArgs& a, hipStream_t stream) {
+    if (linear_few(a.M, a.K)) return launch_few8(a, stream);
+    return a.e.act != ACT_NONE || a.e.residual ? launch_int8<true>(a, stream) : launch_int8<false>(a, stream);
 }
 
 }  // namespace skiparse
