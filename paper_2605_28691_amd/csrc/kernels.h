@@ -249,6 +249,7 @@ struct NormArgs {
     int order;             // ORDER_SAME, or the row map from which a row of the result takes its row of x
     RowArgs rows;
     uint32_t first;        // set by the launcher
+    uint32_t chunks;       // of 512 channels
     float per_n;
 };
 hipError_t launch_norm_rows(const NormArgs& a, hipStream_t stream);
@@ -266,7 +267,8 @@ struct NormBwdArgs {
     bool f32;
     int order;             // from the result's order back to h's
     RowArgs rows;
-    float per_n;           // set by the launcher
+    uint32_t chunks;       // set by the launcher: of 512 channels
+    float per_n;
 };
 uint32_t norm_bwd_parts(uint32_t rows, uint32_t cols);
 hipError_t launch_norm_bwd(const NormBwdArgs& a, hipStream_t stream);

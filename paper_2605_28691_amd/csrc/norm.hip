@@ -2,303 +2,484 @@
 // norm's gradients.  All sums in float32.
 //     h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h r w          int8: codes and scale of h w (int8_rows.h), the scale times r: r is the same for a row and changes no code
 //     g = dy w,  u = h r,  dx = r (g - u mean(g u)) + dx_add,  dw = sum over the rows of dy u
-// Bound by HBM bandwidth: every tensor is moved once, a row stays in its workgroup's registers between its sum and its result.
+// Bound by HBM bandwidth: every tensor is moved once, a row stays in registers between its sum and its result.
 #include "int8_rows.h"
 #include "kernels.h"
+#include "norm_shape.h"
 #include "row_pieces.h"
 
 namespace skiparse {
 
-constexpr uint32_t NORM_WAVES = 16;  // of a workgroup, at most
-constexpr int NORM_CH = 4;           // pieces of 8 channels of a lane
-static_assert(NORM_WAVES * 64 * NORM_CH * 8 == NORM_MAX_COLS, "a row is in registers");
-
-// Sums over a workgroup, the same in every lane, in an order that depends on nothing.
-template <int N>
-struct Together {
-    float v[NORM_WAVES][N];
-    double d[NORM_WAVES][N];
+// What a lane knows of its row.  SPAN_LANES: several rows a wavefront, `lanes` lanes each; SPAN_WAVE: a row a wavefront; SPAN_GROUP: a row a workgroup.
+template <int SPAN>
+struct Place {
+    uint32_t piece, step;  // the lane's first piece of the row, and from one to the next
+    __device__ __attribute__((always_inline)) inline explicit Place(uint32_t lanes) {
+        const uint32_t lane = threadIdx.x & 63u;
+        piece = SPAN == SPAN_LANES ? lane & (lanes - 1u) : SPAN == SPAN_WAVE ? lane : threadIdx.x;
+        step = SPAN == SPAN_GROUP ? blockDim.x : 64u;
+    }
+    // rows that a workgroup has at once, and which of them is the lane's
+    static __host__ __device__ inline uint32_t rows(uint32_t lanes, uint32_t threads) { return SPAN == SPAN_LANES ? threads / lanes : SPAN == SPAN_WAVE ? threads / 64u : 1u; }
+    static __device__ inline uint32_t row(uint32_t lanes) {
+        if (SPAN == SPAN_LANES) return threadIdx.x / lanes;
+        return SPAN == SPAN_WAVE ? (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0u;
+    }
 };
-template <typename S>
-__device__ inline S wave_sum(S v) {
+
+struct Plus {
+    template <typename S>
+    __device__ static inline S of(S a, S b) { return a + b; }
+};
+struct Largest {
+    __device__ static inline uint32_t of(uint32_t a, uint32_t b) { return a > b ? a : b; }
+};
+
+// The lanes of a row, of `lanes` neighbours, as one value in each of them, a + b for the pairs 1, 2, 4 .. apart.  Within rows of 16 lanes as DPP operands: where quads agree, the lanes of a mirrored half
+// row are as good as those 4 apart, and so on.
+template <int CONTROL>
+__device__ __attribute__((always_inline)) inline uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, 0xf, 0xf, true); }
+template <typename OP, typename S, int N>
+__device__ __attribute__((always_inline)) inline void across(S (&v)[N], uint32_t lanes) {
+    static_assert(sizeof(S) == 4, "a register");
+    auto bits = [](S x) __attribute__((always_inline)) -> uint32_t { return __builtin_bit_cast(uint32_t, x); };
+    auto value = [](uint32_t x) __attribute__((always_inline)) -> S { return __builtin_bit_cast(S, x); };
+#define EACH for (int i = 0; i < N; i++)
+    if (lanes >= 2u)
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-    return v;
+        EACH v[i] = OP::of(v[i], value(dpp<0xb1>(bits(v[i]))));  // quad_perm 1 0 3 2
+    if (lanes >= 4u)
+#pragma unroll
+        EACH v[i] = OP::of(v[i], value(dpp<0x4e>(bits(v[i]))));  // quad_perm 2 3 0 1
+    if (lanes >= 8u)
+#pragma unroll
+        EACH v[i] = OP::of(v[i], value(dpp<0x141>(bits(v[i]))));  // row_half_mirror
+    if (lanes >= 16u)
+#pragma unroll
+        EACH v[i] = OP::of(v[i], value(dpp<0x140>(bits(v[i]))));  // row_mirror
+    if (lanes >= 32u)
+#pragma unroll
+        EACH {
+            const auto r = __builtin_amdgcn_permlane16_swap(bits(v[i]), bits(v[i]), false, false);
+            v[i] = OP::of(value(r[0]), value(r[1]));
+        }
+    if (lanes >= 64u)
+#pragma unroll
+        EACH {
+            const auto r = __builtin_amdgcn_permlane32_swap(bits(v[i]), bits(v[i]), false, false);
+            v[i] = OP::of(value(r[0]), value(r[1]));
+        }
+#undef EACH
 }
-template <typename S, int N>
-__device__ inline void group_sum(S (&v)[N], S (*all)[N]) {
+
+// Sums of a row: of each 512 channels over their lanes, then these one after the other.  So they are the same whichever shape has the row, and a row's bits depend on nothing but the row.
+// v[k][i]: of the lane's channels in its piece i.  all: a place for the 512s of a workgroup's row (SPAN_GROUP); each call until a barrier takes another.
+template <int SPAN, int CH, int N>
+__device__ __attribute__((always_inline)) inline void row_sums(float (&v)[N][CH], float (&sum)[N], uint32_t lanes, uint32_t chunks, float (*all)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = wave_sum(v[i]);
-    const uint32_t waves = blockDim.x >> 6;
-    if (waves == 1u) return;
-    __syncthreads();  // what was there has been read
+    for (int k = 0; k < N; k++) across<Plus>(v[k], SPAN == SPAN_LANES ? lanes : 64u);
+    if (SPAN != SPAN_GROUP) {
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            sum[k] = v[k][0];
+#pragma unroll
+            for (int i = 1; i < CH; i++) sum[k] += v[k][i];
+        }
+        return;
+    }
+    const uint32_t waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63u) == 0u) {
 #pragma unroll
-        for (int i = 0; i < N; i++) all[threadIdx.x >> 6][i] = v[i];
+        for (int i = 0; i < CH; i++)
+#pragma unroll
+            for (int k = 0; k < N; k++) all[i * waves + wave][k] = v[k][i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-        v[i] = all[0][i];
-        for (uint32_t w = 1; w < waves; w++) v[i] += all[w][i];
-    }
+    for (int k = 0; k < N; k++) sum[k] = all[0][k];
+    for (uint32_t c = 1; c < chunks; c++)
+#pragma unroll
+        for (int k = 0; k < N; k++) sum[k] += all[c][k];
 }
-__device__ inline uint32_t group_max(uint32_t v, float (*all)[1]) {
-#pragma unroll
+template <int SPAN, int N>
+__device__ __attribute__((always_inline)) inline void row_sums64(double (&v)[N], uint32_t lanes, double (*all)[N]) {
     for (int off = 32; off >= 1; off >>= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)v, off);
-        v = o > v ? o : v;
+        if (SPAN == SPAN_LANES && (uint32_t)off >= lanes) continue;
+#pragma unroll
+        for (int k = 0; k < N; k++) v[k] += __shfl_xor(v[k], off);
     }
-    const uint32_t waves = blockDim.x >> 6;
-    if (waves == 1u) return v;
-    __syncthreads();
-    if ((threadIdx.x & 63u) == 0u) all[threadIdx.x >> 6][0] = __uint_as_float(v);
-    __syncthreads();
-    for (uint32_t w = 0; w < waves; w++) {
-        const uint32_t o = __float_as_uint(all[w][0]);
-        v = o > v ? o : v;
+    if (SPAN != SPAN_GROUP) return;
+    if ((threadIdx.x & 63u) == 0u) {
+#pragma unroll
+        for (int k = 0; k < N; k++) all[threadIdx.x >> 6][k] = v[k];
     }
-    return v;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; k++) v[k] = all[0][k];
+    for (uint32_t w = 1; w < blockDim.x >> 6; w++)
+#pragma unroll
+        for (int k = 0; k < N; k++) v[k] += all[w][k];
+}
+template <int SPAN>
+__device__ __attribute__((always_inline)) inline uint32_t row_largest(uint32_t v, uint32_t lanes, uint32_t* all) {
+    uint32_t top[1] = {v};
+    across<Largest>(top, SPAN == SPAN_LANES ? lanes : 64u);
+    if (SPAN != SPAN_GROUP) return top[0];
+    if ((threadIdx.x & 63u) == 0u) all[threadIdx.x >> 6] = top[0];
+    __syncthreads();
+    for (uint32_t w = 0; w < blockDim.x >> 6; w++) top[0] = Largest::of(top[0], all[w]);
+    return top[0];
 }
 
 // Squares of values beyond 2^63 or so are infinite in float32, and those below 2^-63 lose digits: a row whose sum says so is summed again in 64 bits.
 __device__ inline bool out_of_range(float squares, float per_n, float eps) { return !(squares <= 1e38f) || squares * per_n + eps < 1e-30f; }
 __device__ inline float inverse_size(float squares, float per_n, float eps) { return 1.f / sqrtf(squares * per_n + eps); }
 
-template <typename T, int KIND>
-__global__ __launch_bounds__(64 * NORM_WAVES) void norm_rows_kernel(NormArgs a) {
-    __shared__ Together<1> all;
-    const uint32_t row = a.first + blockIdx.x;
-    const uint32_t from = a.order == 1 ? source_row<TO_SPARSE>(a.rows, row, 0u) : a.order == 2 ? source_row<TO_ORIGINAL>(a.rows, row, 0u) : row;
-    const size_t at = (size_t)from * a.cols, to = (size_t)row * a.cols;
-    float h[NORM_CH][8];
-    float sum[1] = {0.f};
+__device__ inline uint32_t source_of(int order, const RowArgs& rows, uint32_t row) {
+    return order == 1 ? source_row<TO_SPARSE>(rows, row, 0u) : order == 2 ? source_row<TO_ORIGINAL>(rows, row, 0u) : row;
+}
+
+template <typename T, int KIND, int SPAN, int CH>
+__global__ __launch_bounds__(SPAN == SPAN_GROUP ? norm_group_threads(CH) : 256) void norm_rows_kernel(NormArgs a, uint32_t lanes) {
+    constexpr int PLACES = SPAN == SPAN_GROUP ? NORM_WAVES : 1, CHUNKS = SPAN == SPAN_GROUP ? norm_group_threads(CH) / 64 * CH : 1;
+    __shared__ float sums[CHUNKS][1];
+    __shared__ double sums64[PLACES][1];
+    __shared__ uint32_t tops[PLACES];
+    const Place<SPAN> at(lanes);
+    const uint32_t row = a.first + blockIdx.x * Place<SPAN>::rows(lanes, blockDim.x) + Place<SPAN>::row(lanes);
+    const bool on = row < a.n_rows;
+    if (SPAN == SPAN_WAVE && !on) return;
+    const uint32_t from = on ? source_of(a.order, a.rows, row) : 0u;
+    const size_t in = (size_t)from * a.cols, to = (size_t)row * a.cols;
+    auto there = [&](int i, uint32_t& c) __attribute__((always_inline)) -> bool {
+        c = (at.piece + i * at.step) * 8u;
+        return on && c < a.cols;
+    };
+    float h[CH][8];
+    Piece<T> x[CH], res[CH];
+    uint32_t c;
 #pragma unroll
-    for (int i = 0; i < NORM_CH; i++) {
-        const uint32_t c = (threadIdx.x + i * blockDim.x) * 8u;
+    for (int i = 0; i < CH; i++)
+        if (there(i, c)) x[i] = load_piece<T>(a.x, in + c);
+    if (KIND != ROWS_QUANTIZED && a.residual != nullptr) {
+#pragma unroll
+        for (int i = 0; i < CH; i++)
+            if (there(i, c)) res[i] = load_piece<T>(a.residual, in + c);
+    }
+    float squares[1][CH];
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+        squares[0][i] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; e++) h[i][e] = 0.f;
-        if (c >= a.cols) continue;
-        const Piece<T> x = load_piece<T>(a.x, at + c);
+        if (!there(i, c)) continue;
 #pragma unroll
-        for (int e = 0; e < 8; e++) h[i][e] = x.get(e);
+        for (int e = 0; e < 8; e++) h[i][e] = x[i].get(e);
+        if (KIND == ROWS_QUANTIZED) continue;
         if (a.residual != nullptr) {
-            const Piece<T> r = load_piece<T>(a.residual, at + c);
 #pragma unroll
-            for (int e = 0; e < 8; e++) h[i][e] += r.get(e);
+            for (int e = 0; e < 8; e++) h[i][e] += res[i].get(e);
         }
         if (a.sum != nullptr) {
             Piece<T> s;
             s.set(h[i]);
-            store_piece<T>(a.sum, at + c, s);
+            store_piece<T>(a.sum, in + c, s);
         }
 #pragma unroll
-        for (int e = 0; e < 8; e++) sum[0] += h[i][e] * h[i][e];
+        for (int e = 0; e < 8; e++) squares[0][i] = fmaf(h[i][e], h[i][e], squares[0][i]);
     }
     float r = 1.f;
     if (KIND != ROWS_QUANTIZED) {
-        group_sum(sum, all.v);
+        float sum[1];
+        row_sums<SPAN, CH, 1>(squares, sum, lanes, a.chunks, sums);
         r = inverse_size(sum[0], a.per_n, a.eps);
-        if (out_of_range(sum[0], a.per_n, a.eps)) {
+        const bool bad = on && out_of_range(sum[0], a.per_n, a.eps);
+        if (__builtin_expect(SPAN == SPAN_GROUP ? bad : __builtin_amdgcn_ballot_w64(bad) != 0, 0)) {  // all lanes of a wavefront go
             double d[1] = {0.};
 #pragma unroll
-            for (int i = 0; i < NORM_CH; i++)
+            for (int i = 0; i < CH; i++)
 #pragma unroll
                 for (int e = 0; e < 8; e++) d[0] += (double)h[i][e] * h[i][e];
-            group_sum(d, all.d);
-            r = (float)(1. / sqrt(d[0] / a.cols + a.eps));
+            row_sums64<SPAN>(d, lanes, sums64);
+            if (bad) r = (float)(1. / sqrt(d[0] / a.cols + a.eps));
         }
     }
     uint32_t top = 0u;
 #pragma unroll
-    for (int i = 0; i < NORM_CH; i++) {
-        const uint32_t c = (threadIdx.x + i * blockDim.x) * 8u;
+    for (int i = 0; i < CH; i++) {
         if (KIND == ROWS_NORM) {
 #pragma unroll
             for (int e = 0; e < 8; e++) h[i][e] *= r;
         }
-        if (c < a.cols && KIND != ROWS_QUANTIZED && a.weight != nullptr) {
+        const bool here = there(i, c);
+        if (KIND != ROWS_QUANTIZED && here && a.weight != nullptr) {
             const Piece<T> w = load_piece<T>(a.weight, c);
 #pragma unroll
             for (int e = 0; e < 8; e++) h[i][e] *= w.get(e);
         }
-        if (KIND == ROWS_NORM && c < a.cols) {
-            Piece<T> y;
-            y.set(h[i]);
-            store_piece<T>(a.out, to + c, y);
-        }
+        if (KIND == ROWS_NORM) {
+            if (here) {
+                Piece<T> y;
+                y.set(h[i]);
+                store_piece<T>(a.out, to + c, y);
+            }
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) top = int8_size(h[i][e]) > top ? int8_size(h[i][e]) : top;
+            for (int e = 0; e < 8; e++) top = Largest::of(top, int8_size(h[i][e]));
+        }
     }
     if (KIND == ROWS_NORM) return;
-    const Int8Row q(group_max(top, all.v), r);
+    const Int8Row q(row_largest<SPAN>(top, lanes, tops), r);
 #pragma unroll
-    for (int i = 0; i < NORM_CH; i++) {
-        const uint32_t c = (threadIdx.x + i * blockDim.x) * 8u;
-        if (c < a.cols)
-            *(piece_u32x2*)((char*)a.out + to + c) = piece_u32x2{q.codes(h[i][0], h[i][1], h[i][2], h[i][3]), q.codes(h[i][4], h[i][5], h[i][6], h[i][7])};
-    }
-    if (threadIdx.x == 0u) a.scales[row] = q.scale;
+    for (int i = 0; i < CH; i++)
+        if (there(i, c)) *(piece_u32x2*)((char*)a.out + to + c) = piece_u32x2{q.codes(h[i][0], h[i][1], h[i][2], h[i][3]), q.codes(h[i][4], h[i][5], h[i][6], h[i][7])};
+    if (on && at.piece == 0u) a.scales[row] = q.scale;
 }
 
-template <typename T>
-static void launch_rows_t(const NormArgs& a, uint32_t blocks, uint32_t threads, hipStream_t stream) {
-    switch (a.kind) {
-        case ROWS_NORM: norm_rows_kernel<T, ROWS_NORM><<<blocks, threads, 0, stream>>>(a); break;
-        case ROWS_NORM_QUANTIZED: norm_rows_kernel<T, ROWS_NORM_QUANTIZED><<<blocks, threads, 0, stream>>>(a); break;
-        default: norm_rows_kernel<T, ROWS_QUANTIZED><<<blocks, threads, 0, stream>>>(a); break;
-    }
-}
-
-static uint32_t threads_of(uint32_t cols) {
-    const uint32_t waves = (cols / 8u + 63u) / 64u;
-    return 64u * (waves < NORM_WAVES ? waves : NORM_WAVES);
-}
-
-hipError_t launch_norm_rows(const NormArgs& all, hipStream_t stream) {
-    const uint32_t threads = threads_of(all.cols);
-    NormArgs a = all;
-    a.per_n = 1.f / (float)a.cols;
-    constexpr uint32_t AT_ONCE = 1u << 21;  // a grid has less than 2^32 threads
-    for (a.first = 0; a.first < a.n_rows; a.first += AT_ONCE) {
-        const uint32_t n = a.n_rows - a.first < AT_ONCE ? a.n_rows - a.first : AT_ONCE;
-        if (a.f32) launch_rows_t<float>(a, n, threads, stream);
-        else launch_rows_t<__bf16>(a, n, threads, stream);
+template <typename T, int KIND>
+static hipError_t launch_rows_t(NormArgs a, hipStream_t stream) {
+    const NormShape s = norm_shape(a.n_rows, a.cols);
+    const uint32_t per = s.span == SPAN_LANES ? s.threads / s.lanes : s.span == SPAN_WAVE ? s.threads / 64u : 1u;
+    const uint32_t at_once = (uint32_t)((1ull << 31) / s.threads) * per;  // rows of a launch: a grid has less than 2^32 threads
+    for (uint64_t first = 0; first < a.n_rows; first += at_once) {
+        a.first = (uint32_t)first;
+        const uint32_t n = a.n_rows - a.first < at_once ? a.n_rows - a.first : at_once, blocks = (n + per - 1u) / per;
+        if (s.span == SPAN_LANES) norm_rows_kernel<T, KIND, SPAN_LANES, 1><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
+#define ROWS(SPAN, CH) \
+    else if (s.span == SPAN && s.ch == CH) norm_rows_kernel<T, KIND, SPAN, CH><<<blocks, s.threads, 0, stream>>>(a, 64u);
+        ROWS(SPAN_WAVE, 1)
+        ROWS(SPAN_WAVE, 2)
+        ROWS(SPAN_WAVE, 3)
+        ROWS(SPAN_WAVE, 4)
+        ROWS(SPAN_WAVE, 6)
+        ROWS(SPAN_WAVE, 8)
+        ROWS(SPAN_WAVE, 10)
+        ROWS(SPAN_GROUP, 1)
+        ROWS(SPAN_GROUP, 2)
+        ROWS(SPAN_GROUP, 4)
+        ROWS(SPAN_GROUP, 8)
+#undef ROWS
+        else return hipErrorInvalidValue;
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
-// ---- gradients
-
-uint32_t norm_bwd_parts(uint32_t rows, uint32_t) { return rows < 512u ? rows : 512u; }
-
-// A workgroup takes a contiguous part of the rows, and has the sums of its part for the weights' gradient.
 template <typename T>
-__global__ __launch_bounds__(64 * NORM_WAVES) void norm_bwd_kernel(NormBwdArgs a) {
-    __shared__ Together<2> all;
-    const uint32_t first = (uint32_t)((uint64_t)blockIdx.x * a.n_rows / gridDim.x), end = (uint32_t)((uint64_t)(blockIdx.x + 1u) * a.n_rows / gridDim.x);
-    float dw[NORM_CH][8] = {};
-    for (uint32_t row = first; row < end; row++) {
-        const uint32_t from = a.order == 1 ? source_row<TO_SPARSE>(a.rows, row, 0u) : a.order == 2 ? source_row<TO_ORIGINAL>(a.rows, row, 0u) : row;
-        const size_t at = (size_t)row * a.cols, in = (size_t)from * a.cols;
-        float h[NORM_CH][8], g[NORM_CH][8], sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < NORM_CH; i++) {
-            const uint32_t c = (threadIdx.x + i * blockDim.x) * 8u;
-#pragma unroll
-            for (int e = 0; e < 8; e++) h[i][e] = g[i][e] = 0.f;
-            if (c >= a.cols) continue;
-            const Piece<T> x = load_piece<T>(a.h, at + c), y = load_piece<T>(a.dy, in + c);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                h[i][e] = x.get(e);
-                g[i][e] = y.get(e);
-            }
-        }
-        auto weight = [&](int i, float (&w)[8]) __attribute__((always_inline)) {
-            const uint32_t c = (threadIdx.x + i * blockDim.x) * 8u;
-#pragma unroll
-            for (int e = 0; e < 8; e++) w[e] = 1.f;
-            if (a.weight == nullptr || c >= a.cols) return;
-            const Piece<T> p = load_piece<T>(a.weight, c);
-#pragma unroll
-            for (int e = 0; e < 8; e++) w[e] = p.get(e);
-        };
-#pragma unroll
-        for (int i = 0; i < NORM_CH; i++) {
-            float w[8];
-            weight(i, w);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                sum[0] += h[i][e] * h[i][e];
-                sum[1] += g[i][e] * w[e] * h[i][e];
-            }
-        }
-        group_sum(sum, all.v);
-        float r = inverse_size(sum[0], a.per_n, a.eps), mean = sum[1] * a.per_n * r;
-        if (out_of_range(sum[0], a.per_n, a.eps) || !(fabsf(sum[1]) <= 1e38f)) {
-            double d[2] = {0., 0.};
-#pragma unroll
-            for (int i = 0; i < NORM_CH; i++) {
-                float w[8];
-                weight(i, w);
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    d[0] += (double)h[i][e] * h[i][e];
-                    d[1] += (double)g[i][e] * w[e] * h[i][e];
-                }
-            }
-            group_sum(d, all.d);
-            const double s = 1. / sqrt(d[0] / a.cols + a.eps);
-            r = (float)s;
-            mean = (float)(d[1] / a.cols * s);
-        }
-#pragma unroll
-        for (int i = 0; i < NORM_CH; i++) {
-            const uint32_t c = (threadIdx.x + i * blockDim.x) * 8u;
-            float w[8];
-            weight(i, w);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float u = h[i][e] * r;
-                dw[i][e] += g[i][e] * u;
-                g[i][e] = r * (g[i][e] * w[e] - u * mean);
-            }
-            if (c >= a.cols || a.dx == nullptr) continue;
-            if (a.dx_add != nullptr) {
-                const Piece<T> p = load_piece<T>(a.dx_add, at + c);
-#pragma unroll
-                for (int e = 0; e < 8; e++) g[i][e] += p.get(e);
-            }
-            Piece<T> y;
-            y.set(g[i]);
-            store_piece<T>(a.dx, at + c, y);
-        }
-    }
-    if (a.dw == nullptr) return;
-#pragma unroll
-    for (int i = 0; i < NORM_CH; i++) {
-        const uint32_t c = (threadIdx.x + i * blockDim.x) * 8u;
-        if (c >= a.cols) continue;
-        Piece<float> p;
-        p.set(dw[i]);
-        store_piece<float>(a.parts, (size_t)blockIdx.x * a.cols + c, p);
+static hipError_t launch_rows_of(const NormArgs& a, hipStream_t stream) {
+    switch (a.kind) {
+        case ROWS_NORM: return launch_rows_t<T, ROWS_NORM>(a, stream);
+        case ROWS_NORM_QUANTIZED: return launch_rows_t<T, ROWS_NORM_QUANTIZED>(a, stream);
+        default: return launch_rows_t<T, ROWS_QUANTIZED>(a, stream);
     }
 }
 
-// The parts' sums, 64 channels a workgroup, 16 parts at a time, in an order that depends on nothing.
+hipError_t launch_norm_rows(const NormArgs& all, hipStream_t stream) {
+    NormArgs a = all;
+    a.per_n = 1.f / (float)a.cols;
+    a.chunks = (a.cols + 511u) / 512u;
+    return a.f32 ? launch_rows_of<float>(a, stream) : launch_rows_of<__bf16>(a, stream);
+}
+
+// ---- gradients
+
+// A workgroup takes a contiguous part of the rows, and has the sums of its part for the weights' gradient in registers: each lane those of its channels.  The next row is on its way while one is
+// worked on.
+template <typename T, int SPAN, int CH>
+__global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : NORM_BWD_THREADS) void norm_bwd_kernel(NormBwdArgs a, uint32_t lanes) {
+    constexpr int PLACES = SPAN == SPAN_GROUP ? NORM_WAVES : 1;
+    __shared__ float sums[2][SPAN == SPAN_GROUP ? NORM_WAVES * CH : 1][2];  // of rows by turns: one barrier a row is enough
+    __shared__ double sums64[PLACES][2];
+    __shared__ __attribute__((aligned(16))) float dws[SPAN == SPAN_GROUP ? 4 : NORM_BWD_THREADS / 64 * CH * 512];
+    const Place<SPAN> at(lanes);
+    const uint32_t first = (uint32_t)((uint64_t)blockIdx.x * a.n_rows / gridDim.x), end = (uint32_t)((uint64_t)(blockIdx.x + 1u) * a.n_rows / gridDim.x);
+    const uint32_t stride = Place<SPAN>::rows(lanes, blockDim.x);
+    auto there = [&](int i, uint32_t& c) __attribute__((always_inline)) -> bool {
+        c = (at.piece + i * at.step) * 8u;
+        return c < a.cols;
+    };
+    uint32_t c;
+    Piece<T> w[CH];
+    if (a.weight != nullptr) {
+#pragma unroll
+        for (int i = 0; i < CH; i++)
+            if (there(i, c)) w[i] = load_piece<T>(a.weight, c);
+    } else {
+        const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+        for (int i = 0; i < CH; i++) w[i].set(ones);
+    }
+    float dw[CH][8] = {};
+    Piece<T> hn[CH], yn[CH], an[CH];
+    const bool adds = a.dx != nullptr && a.dx_add != nullptr;
+    auto load = [&](uint32_t row) __attribute__((always_inline)) {
+        if (row >= end) return;
+        const size_t in = (size_t)source_of(a.order, a.rows, row) * a.cols, to = (size_t)row * a.cols;
+#pragma unroll
+        for (int i = 0; i < CH; i++)
+            if (there(i, c)) {
+                hn[i] = load_piece<T>(a.h, to + c);
+                yn[i] = load_piece<T>(a.dy, in + c);
+                if (adds) an[i] = load_piece<T>(a.dx_add, to + c);
+            }
+    };
+    const uint32_t row0 = first + Place<SPAN>::row(lanes);
+    load(row0);
+    uint32_t turn = 0u;
+    // every lane goes through every round: rows are exchanged within wavefronts
+    for (uint32_t base = first; base < end; base += stride) {
+        const uint32_t row = base + (row0 - first);
+        const bool on = row < end;
+        if (SPAN == SPAN_WAVE && !on) break;
+        Piece<T> hc[CH], yc[CH], ac[CH];
+#pragma unroll
+        for (int i = 0; i < CH; i++) {
+            hc[i] = hn[i];
+            yc[i] = yn[i];
+            ac[i] = an[i];
+        }
+        load(row + stride);
+        float parts[2][CH], sum[2];
+#pragma unroll
+        for (int i = 0; i < CH; i++) {
+            parts[0][i] = parts[1][i] = 0.f;
+            if (!(on && there(i, c))) continue;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float h = hc[i].get(e);
+                parts[0][i] = fmaf(h, h, parts[0][i]);
+                parts[1][i] = fmaf(yc[i].get(e) * w[i].get(e), h, parts[1][i]);
+            }
+        }
+        row_sums<SPAN, CH, 2>(parts, sum, lanes, a.chunks, sums[turn & 1u]);
+        turn++;
+        float r = inverse_size(sum[0], a.per_n, a.eps), mean = sum[1] * a.per_n * r;
+        const bool bad = on && (out_of_range(sum[0], a.per_n, a.eps) || !(fabsf(sum[1]) <= 1e38f));
+        if (__builtin_expect(SPAN == SPAN_GROUP ? bad : __builtin_amdgcn_ballot_w64(bad) != 0, 0)) {
+            double d[2] = {0., 0.};
+#pragma unroll
+            for (int i = 0; i < CH; i++) {
+                if (!(on && there(i, c))) continue;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const double h = hc[i].get(e);
+                    d[0] += h * h;
+                    d[1] += (double)yc[i].get(e) * w[i].get(e) * h;
+                }
+            }
+            if (SPAN == SPAN_GROUP) __syncthreads();  // the last such row's have been read
+            row_sums64<SPAN>(d, lanes, sums64);
+            if (bad) {
+                const double s = 1. / sqrt(d[0] / a.cols + a.eps);
+                r = (float)s;
+                mean = (float)(d[1] / a.cols * s);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < CH; i++) {
+            if (!(on && there(i, c))) continue;
+            float g[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float u = hc[i].get(e) * r, y = yc[i].get(e);
+                dw[i][e] = fmaf(y, u, dw[i][e]);
+                g[e] = r * (y * w[i].get(e) - u * mean);
+                if (adds) g[e] += ac[i].get(e);
+            }
+            if (a.dx == nullptr) continue;
+            Piece<T> p;
+            p.set(g);
+            store_piece<T>(a.dx, (size_t)row * a.cols + c, p);
+        }
+    }
+    if (a.dw == nullptr) return;
+    auto out = [&](const float (&s)[8]) __attribute__((always_inline)) {
+        Piece<float> p;
+        p.set(s);
+        store_piece<float>(a.parts, (size_t)blockIdx.x * a.cols + c, p);
+    };
+    if (SPAN == SPAN_GROUP) {
+#pragma unroll
+        for (int i = 0; i < CH; i++)
+            if (there(i, c)) out(dw[i]);
+        return;
+    }
+    // the wavefronts' sums, and those of the rows that a wavefront has at once, in order
+    const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+        if (SPAN == SPAN_LANES) {
+            for (uint32_t off = 32u; off >= lanes; off >>= 1)
+#pragma unroll
+                for (int e = 0; e < 8; e++) dw[i][e] += __shfl_xor(dw[i][e], (int)off);
+        }
+        Piece<float> p;
+        p.set(dw[i]);
+        store_piece<float>(dws, ((wave * CH + i) * 64u + (threadIdx.x & 63u)) * 8u, p);
+    }
+    __syncthreads();
+    if (wave != 0u || (SPAN == SPAN_LANES && threadIdx.x >= lanes)) return;
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+        if (!there(i, c)) continue;
+        for (uint32_t v = 1; v < waves; v++) {
+            const Piece<float> p = load_piece<float>(dws, ((v * CH + i) * 64u + threadIdx.x) * 8u);
+#pragma unroll
+            for (int e = 0; e < 8; e++) dw[i][e] += p.get(e);
+        }
+        out(dw[i]);
+    }
+}
+
+// The parts' sums, 32 channels a workgroup, 32 parts at a time, in an order that depends on nothing.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__ part, T* __restrict__ dw, uint32_t parts, uint32_t cols) {
-    __shared__ float sums[16][64];
-    const uint32_t lane = threadIdx.x & 63u, ty = threadIdx.x >> 6, n = blockIdx.x * 64u + lane;
+    __shared__ float sums[32][33];
+    const uint32_t lane = threadIdx.x & 31u, ty = threadIdx.x >> 5, n = blockIdx.x * 32u + lane;
     float s = 0.f;
     if (n < cols) {
 #pragma unroll 8
-        for (uint32_t p = ty; p < parts; p += 16u) s += part[(size_t)p * cols + n];
+        for (uint32_t p = ty; p < parts; p += 32u) s += part[(size_t)p * cols + n];
     }
     sums[ty][lane] = s;
     __syncthreads();
-    if (ty != 0u || n >= cols) return;
-    s = 0.f;
+    // channel `ty`, over the lanes
+    s = sums[lane][ty];
 #pragma unroll
-    for (uint32_t i = 0; i < 16u; i++) s += sums[i][lane];
-    dw[n] = (T)s;
+    for (int off = 16; off >= 1; off >>= 1) s += __shfl_xor(s, off);
+    if (lane == 0u && blockIdx.x * 32u + ty < cols) dw[blockIdx.x * 32u + ty] = (T)s;
+}
+
+uint32_t norm_bwd_parts(uint32_t rows, uint32_t cols) { return norm_bwd_shape(rows, cols).parts; }
+
+template <typename T>
+static hipError_t launch_bwd_t(const NormBwdArgs& a, hipStream_t stream) {
+    const NormBwdShape s = norm_bwd_shape(a.n_rows, a.cols);
+    if (s.span == SPAN_LANES) norm_bwd_kernel<T, SPAN_LANES, 1><<<s.parts, s.threads, 0, stream>>>(a, s.lanes);
+#define ROWS(SPAN, CH) \
+    else if (s.span == SPAN && s.ch == CH) norm_bwd_kernel<T, SPAN, CH><<<s.parts, s.threads, 0, stream>>>(a, 64u);
+    ROWS(SPAN_WAVE, 1)
+    ROWS(SPAN_WAVE, 2)
+    ROWS(SPAN_WAVE, 3)
+    ROWS(SPAN_WAVE, 4)
+    ROWS(SPAN_GROUP, 1)
+    ROWS(SPAN_GROUP, 2)
+    ROWS(SPAN_GROUP, 3)
+    ROWS(SPAN_GROUP, 4)
+#undef ROWS
+    else return hipErrorInvalidValue;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.dw == nullptr) return e;
+    norm_dw_kernel<T><<<(a.cols + 31u) / 32u, 1024, 0, stream>>>(a.parts, (T*)a.dw, s.parts, a.cols);
+    return hipGetLastError();
 }
 
 hipError_t launch_norm_bwd(const NormBwdArgs& all, hipStream_t stream) {
     NormBwdArgs a = all;
     a.per_n = 1.f / (float)a.cols;
-    const uint32_t parts = norm_bwd_parts(a.n_rows, a.cols), threads = threads_of(a.cols);
-    if (a.f32) norm_bwd_kernel<float><<<parts, threads, 0, stream>>>(a);
-    else norm_bwd_kernel<__bf16><<<parts, threads, 0, stream>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.dw == nullptr) return e;
-    const uint32_t blocks = (a.cols + 63u) / 64u;
-    if (a.f32) norm_dw_kernel<float><<<blocks, 1024, 0, stream>>>(a.parts, (float*)a.dw, parts, a.cols);
-    else norm_dw_kernel<__bf16><<<blocks, 1024, 0, stream>>>(a.parts, (__bf16*)a.dw, parts, a.cols);
-    return hipGetLastError();
+    a.chunks = (a.cols + 511u) / 512u;
+    return a.f32 ? launch_bwd_t<float>(a, stream) : launch_bwd_t<__bf16>(a, stream);
 }
 
 }  // namespace skiparse
