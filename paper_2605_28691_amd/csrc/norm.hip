@@ -10,20 +10,55 @@
 
 namespace skiparse {
 
-// What a lane knows of its row.  SPAN_LANES: several rows a wavefront, `lanes` lanes each; SPAN_WAVE: a row a wavefront; SPAN_GROUP: a row a workgroup.
-template <int SPAN>
+// Which row, and which channels of it, a lane has: pieces of 8, CH of them.  SPAN_LANES: several rows a wavefront, `lanes` lanes each; SPAN_WAVE: a row a wavefront; SPAN_GROUP: a row a workgroup.
+template <typename T, int SPAN, int CH>
 struct Place {
-    uint32_t piece, step;  // the lane's first piece of the row, and from one to the next
-    __device__ __attribute__((always_inline)) inline explicit Place(uint32_t lanes) {
-        const uint32_t lane = threadIdx.x & 63u;
-        piece = SPAN == SPAN_LANES ? lane & (lanes - 1u) : SPAN == SPAN_WAVE ? lane : threadIdx.x;
-        step = SPAN == SPAN_GROUP ? blockDim.x : 64u;
+    uint32_t first, step, cols;  // the lane's first channel, from a piece to the next, the row's channels
+    uint32_t half;               // from a unit of a piece to the next
+    __device__ __attribute__((always_inline)) inline Place(uint32_t lanes, uint32_t n) {
+        const uint32_t lane = threadIdx.x & 63u, in_row = SPAN == SPAN_LANES ? lane & (lanes - 1u) : lane;
+        first = in_row * Piece<T>::EACH + (SPAN == SPAN_GROUP ? (threadIdx.x >> 6) * 512u : 0u);
+        step = SPAN == SPAN_GROUP ? blockDim.x * 8u : 512u;
+        half = SPAN == SPAN_LANES ? lanes * 4u : 256u;
+        cols = n;
     }
     // rows that a workgroup has at once, and which of them is the lane's
-    static __host__ __device__ inline uint32_t rows(uint32_t lanes, uint32_t threads) { return SPAN == SPAN_LANES ? threads / lanes : SPAN == SPAN_WAVE ? threads / 64u : 1u; }
+    static __device__ inline uint32_t rows(uint32_t lanes) { return SPAN == SPAN_LANES ? blockDim.x / lanes : SPAN == SPAN_WAVE ? blockDim.x / 64u : 1u; }
     static __device__ inline uint32_t row(uint32_t lanes) {
         if (SPAN == SPAN_LANES) return threadIdx.x / lanes;
         return SPAN == SPAN_WAVE ? (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0u;
+    }
+    // first channel of unit u of piece i; false: behind the row's end
+    __device__ __attribute__((always_inline)) inline bool at(int i, int u, uint32_t& c) const {
+        c = first + i * step + u * half;
+        return c < cols;
+    }
+    // piece i of the row that begins with element `row`; zeros behind its end, and for lanes without a row
+    template <bool NT>
+    __device__ __attribute__((always_inline)) inline Piece<T> load_one(const void* from, size_t row, bool on, int i) const {
+        Piece<T> p;
+#pragma unroll
+        for (int u = 0; u < Piece<T>::UNITS; u++) {
+            uint32_t c;
+            p.raw[u] = piece_u32x4{0u, 0u, 0u, 0u};
+            if (at(i, u, c) && on) p.raw[u] = load16<NT>((const T*)from + row + c);
+        }
+        return p;
+    }
+    template <bool NT>
+    __device__ __attribute__((always_inline)) inline void load(const void* from, size_t row, bool on, Piece<T> (&p)[CH]) const {
+#pragma unroll
+        for (int i = 0; i < CH; i++) p[i] = load_one<NT>(from, row, on, i);
+    }
+    template <bool NT>
+    __device__ __attribute__((always_inline)) inline void store(void* to, size_t row, bool on, int i, const float (&v)[8]) const {
+        Piece<T> p;
+        p.set(v);
+#pragma unroll
+        for (int u = 0; u < Piece<T>::UNITS; u++) {
+            uint32_t c;
+            if (at(i, u, c) && on) store16<NT>((T*)to + row + c, p.raw[u]);
+        }
     }
 };
 
@@ -101,25 +136,6 @@ __device__ __attribute__((always_inline)) inline void row_sums(float (&v)[N][CH]
 #pragma unroll
         for (int k = 0; k < N; k++) sum[k] += all[c][k];
 }
-template <int SPAN, int N>
-__device__ __attribute__((always_inline)) inline void row_sums64(double (&v)[N], uint32_t lanes, double (*all)[N]) {
-    for (int off = 32; off >= 1; off >>= 1) {
-        if (SPAN == SPAN_LANES && (uint32_t)off >= lanes) continue;
-#pragma unroll
-        for (int k = 0; k < N; k++) v[k] += __shfl_xor(v[k], off);
-    }
-    if (SPAN != SPAN_GROUP) return;
-    if ((threadIdx.x & 63u) == 0u) {
-#pragma unroll
-        for (int k = 0; k < N; k++) all[threadIdx.x >> 6][k] = v[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; k++) v[k] = all[0][k];
-    for (uint32_t w = 1; w < blockDim.x >> 6; w++)
-#pragma unroll
-        for (int k = 0; k < N; k++) v[k] += all[w][k];
-}
 template <int SPAN>
 __device__ __attribute__((always_inline)) inline uint32_t row_largest(uint32_t v, uint32_t lanes, uint32_t* all) {
     uint32_t top[1] = {v};
@@ -131,63 +147,51 @@ __device__ __attribute__((always_inline)) inline uint32_t row_largest(uint32_t v
     return top[0];
 }
 
-// Squares of values beyond 2^63 or so are infinite in float32, and those below 2^-63 lose digits: a row whose sum says so is summed again in 64 bits.
+// Squares of values beyond 2^63 or so are infinite in float32, and those below 2^-63 lose digits: a row whose sum says so is summed once more, with its values times a power of two that keeps
+// every square that counts in range (values below 2^128 times 2^-80; values below 2^-42, of which squares below 2^-126 do not count beside eps, times 2^70).
 __device__ inline bool out_of_range(float squares, float per_n, float eps) { return !(squares <= 1e38f) || squares * per_n + eps < 1e-30f; }
-__device__ inline float inverse_size(float squares, float per_n, float eps) { return 1.f / sqrtf(squares * per_n + eps); }
+__device__ inline float into_range(float squares) { return squares <= 1.f ? 0x1p70f : 0x1p-80f; }
+// 1 / sqrt(mean + eps), of values times `by` if that is not 1
+__device__ inline float inverse_size(float squares, float per_n, float eps, float by = 1.f) { return 1.f / sqrtf(squares * per_n + eps * by * by); }
 
 __device__ inline uint32_t source_of(int order, const RowArgs& rows, uint32_t row) {
     return order == 1 ? source_row<TO_SPARSE>(rows, row, 0u) : order == 2 ? source_row<TO_ORIGINAL>(rows, row, 0u) : row;
 }
 
-template <typename T, int KIND, int SPAN, int CH>
-__global__ __launch_bounds__(SPAN == SPAN_GROUP ? norm_group_threads(CH) : 256) void norm_rows_kernel(NormArgs a, uint32_t lanes) {
-    constexpr int PLACES = SPAN == SPAN_GROUP ? NORM_WAVES : 1, CHUNKS = SPAN == SPAN_GROUP ? norm_group_threads(CH) / 64 * CH : 1;
+template <typename T, int KIND, int SPAN, int CH, bool NT>
+__global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : 256) void norm_rows_kernel(NormArgs a, uint32_t lanes) {
+    constexpr int PLACES = SPAN == SPAN_GROUP ? NORM_WAVES : 1, CHUNKS = SPAN == SPAN_GROUP ? NORM_WAVES * CH : 1;
     __shared__ float sums[CHUNKS][1];
-    __shared__ double sums64[PLACES][1];
+    __shared__ float again[CHUNKS][1];
     __shared__ uint32_t tops[PLACES];
-    const Place<SPAN> at(lanes);
-    const uint32_t row = a.first + blockIdx.x * Place<SPAN>::rows(lanes, blockDim.x) + Place<SPAN>::row(lanes);
+    const Place<T, SPAN, CH> at(lanes, a.cols);
+    const uint32_t row = a.first + blockIdx.x * at.rows(lanes) + at.row(lanes);
     const bool on = row < a.n_rows;
     if (SPAN == SPAN_WAVE && !on) return;
     const uint32_t from = on ? source_of(a.order, a.rows, row) : 0u;
     const size_t in = (size_t)from * a.cols, to = (size_t)row * a.cols;
-    auto there = [&](int i, uint32_t& c) __attribute__((always_inline)) -> bool {
-        c = (at.piece + i * at.step) * 8u;
-        return on && c < a.cols;
-    };
     float h[CH][8];
-    Piece<T> x[CH], res[CH];
-    uint32_t c;
-#pragma unroll
-    for (int i = 0; i < CH; i++)
-        if (there(i, c)) x[i] = load_piece<T>(a.x, in + c);
-    if (KIND != ROWS_QUANTIZED && a.residual != nullptr) {
-#pragma unroll
-        for (int i = 0; i < CH; i++)
-            if (there(i, c)) res[i] = load_piece<T>(a.residual, in + c);
-    }
+    Piece<T> x[CH], other[CH];
+    at.template load<NT>(a.x, in, on, x);
+    const bool adds = KIND != ROWS_QUANTIZED && a.residual != nullptr;
+    if (adds) at.template load<NT>(a.residual, in, on, other);
     float squares[1][CH];
 #pragma unroll
     for (int i = 0; i < CH; i++) {
-        squares[0][i] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; e++) h[i][e] = 0.f;
-        if (!there(i, c)) continue;
 #pragma unroll
         for (int e = 0; e < 8; e++) h[i][e] = x[i].get(e);
         if (KIND == ROWS_QUANTIZED) continue;
-        if (a.residual != nullptr) {
+        if (adds) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) h[i][e] += res[i].get(e);
+            for (int e = 0; e < 8; e++) h[i][e] += other[i].get(e);
+            if (a.sum != nullptr) at.template store<NT>(a.sum, in, on, i, h[i]);
         }
-        if (a.sum != nullptr) {
-            Piece<T> s;
-            s.set(h[i]);
-            store_piece<T>(a.sum, in + c, s);
-        }
+        squares[0][i] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; e++) squares[0][i] = fmaf(h[i][e], h[i][e], squares[0][i]);
     }
+    const bool weighs = KIND != ROWS_QUANTIZED && a.weight != nullptr;
+    if (weighs) at.template load<false>(a.weight, 0, true, other);
     float r = 1.f;
     if (KIND != ROWS_QUANTIZED) {
         float sum[1];
@@ -195,13 +199,15 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? norm_group_threads(CH) : 256) 
         r = inverse_size(sum[0], a.per_n, a.eps);
         const bool bad = on && out_of_range(sum[0], a.per_n, a.eps);
         if (__builtin_expect(SPAN == SPAN_GROUP ? bad : __builtin_amdgcn_ballot_w64(bad) != 0, 0)) {  // all lanes of a wavefront go
-            double d[1] = {0.};
+            const float by = into_range(sum[0]);
 #pragma unroll
-            for (int i = 0; i < CH; i++)
+            for (int i = 0; i < CH; i++) {
+                squares[0][i] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; e++) d[0] += (double)h[i][e] * h[i][e];
-            row_sums64<SPAN>(d, lanes, sums64);
-            if (bad) r = (float)(1. / sqrt(d[0] / a.cols + a.eps));
+                for (int e = 0; e < 8; e++) squares[0][i] = fmaf(h[i][e] * by, h[i][e] * by, squares[0][i]);
+            }
+            row_sums<SPAN, CH, 1>(squares, sum, lanes, a.chunks, again);
+            if (bad) r = by * inverse_size(sum[0], a.per_n, a.eps, by);
         }
     }
     uint32_t top = 0u;
@@ -211,18 +217,12 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? norm_group_threads(CH) : 256) 
 #pragma unroll
             for (int e = 0; e < 8; e++) h[i][e] *= r;
         }
-        const bool here = there(i, c);
-        if (KIND != ROWS_QUANTIZED && here && a.weight != nullptr) {
-            const Piece<T> w = load_piece<T>(a.weight, c);
+        if (weighs) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) h[i][e] *= w.get(e);
+            for (int e = 0; e < 8; e++) h[i][e] *= other[i].get(e);
         }
         if (KIND == ROWS_NORM) {
-            if (here) {
-                Piece<T> y;
-                y.set(h[i]);
-                store_piece<T>(a.out, to + c, y);
-            }
+            at.template store<NT>(a.out, to, on, i, h[i]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; e++) top = Largest::of(top, int8_size(h[i][e]));
@@ -231,33 +231,39 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? norm_group_threads(CH) : 256) 
     if (KIND == ROWS_NORM) return;
     const Int8Row q(row_largest<SPAN>(top, lanes, tops), r);
 #pragma unroll
-    for (int i = 0; i < CH; i++)
-        if (there(i, c)) *(piece_u32x2*)((char*)a.out + to + c) = piece_u32x2{q.codes(h[i][0], h[i][1], h[i][2], h[i][3]), q.codes(h[i][4], h[i][5], h[i][6], h[i][7])};
-    if (on && at.piece == 0u) a.scales[row] = q.scale;
+    for (int i = 0; i < CH; i++) {
+        uint32_t codes[2], c;
+        codes[0] = q.codes(h[i][0], h[i][1], h[i][2], h[i][3]);
+        codes[1] = q.codes(h[i][4], h[i][5], h[i][6], h[i][7]);
+        char* const out = (char*)a.out + to;
+        if (Piece<T>::UNITS == 1) {
+            if (at.at(i, 0, c) && on) *(piece_u32x2*)(out + c) = piece_u32x2{codes[0], codes[1]};
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+                if (at.at(i, u, c) && on) *(uint32_t*)(out + c) = codes[u];
+        }
+    }
+    if (on && at.first == 0u) a.scales[row] = q.scale;
 }
 
-template <typename T, int KIND>
+template <typename T, int KIND, bool NT>
 static hipError_t launch_rows_t(NormArgs a, hipStream_t stream) {
-    const NormShape s = norm_shape(a.n_rows, a.cols);
+    const NormShape s = norm_shape(a.n_rows, a.cols, sizeof(T) * (a.residual ? 2u : 1u));
     const uint32_t per = s.span == SPAN_LANES ? s.threads / s.lanes : s.span == SPAN_WAVE ? s.threads / 64u : 1u;
-    const uint32_t at_once = (uint32_t)((1ull << 31) / s.threads) * per;  // rows of a launch: a grid has less than 2^32 threads
+    const uint64_t at_once = ((1ull << 31) / s.threads) * per;  // rows of a launch: a grid has less than 2^32 threads
     for (uint64_t first = 0; first < a.n_rows; first += at_once) {
         a.first = (uint32_t)first;
-        const uint32_t n = a.n_rows - a.first < at_once ? a.n_rows - a.first : at_once, blocks = (n + per - 1u) / per;
-        if (s.span == SPAN_LANES) norm_rows_kernel<T, KIND, SPAN_LANES, 1><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
+        const uint32_t n = (uint32_t)(a.n_rows - first < at_once ? a.n_rows - first : at_once), blocks = (n + per - 1u) / per;
+        if (s.span == SPAN_LANES) norm_rows_kernel<T, KIND, SPAN_LANES, 1, NT><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
 #define ROWS(SPAN, CH) \
-    else if (s.span == SPAN && s.ch == CH) norm_rows_kernel<T, KIND, SPAN, CH><<<blocks, s.threads, 0, stream>>>(a, 64u);
+    else if (s.span == SPAN && s.ch == CH) norm_rows_kernel<T, KIND, SPAN, CH, NT><<<blocks, s.threads, 0, stream>>>(a, 64u);
         ROWS(SPAN_WAVE, 1)
         ROWS(SPAN_WAVE, 2)
         ROWS(SPAN_WAVE, 3)
-        ROWS(SPAN_WAVE, 4)
-        ROWS(SPAN_WAVE, 6)
-        ROWS(SPAN_WAVE, 8)
-        ROWS(SPAN_WAVE, 10)
         ROWS(SPAN_GROUP, 1)
         ROWS(SPAN_GROUP, 2)
         ROWS(SPAN_GROUP, 4)
-        ROWS(SPAN_GROUP, 8)
 #undef ROWS
         else return hipErrorInvalidValue;
         const hipError_t e = hipGetLastError();
@@ -266,12 +272,19 @@ static hipError_t launch_rows_t(NormArgs a, hipStream_t stream) {
     return hipSuccess;
 }
 
-template <typename T>
+template <typename T, int KIND>
 static hipError_t launch_rows_of(const NormArgs& a, hipStream_t stream) {
+    const uint64_t n = (uint64_t)a.n_rows * a.cols, e = sizeof(T);
+    const uint64_t moved = n * (e + (a.residual ? e : 0u) + (a.sum ? e : 0u) + (KIND == ROWS_NORM ? e : 1u));
+    return moved >= NORM_PAST_CACHES ? launch_rows_t<T, KIND, true>(a, stream) : launch_rows_t<T, KIND, false>(a, stream);
+}
+
+template <typename T>
+static hipError_t launch_rows_as(const NormArgs& a, hipStream_t stream) {
     switch (a.kind) {
-        case ROWS_NORM: return launch_rows_t<T, ROWS_NORM>(a, stream);
-        case ROWS_NORM_QUANTIZED: return launch_rows_t<T, ROWS_NORM_QUANTIZED>(a, stream);
-        default: return launch_rows_t<T, ROWS_QUANTIZED>(a, stream);
+        case ROWS_NORM: return launch_rows_of<T, ROWS_NORM>(a, stream);
+        case ROWS_NORM_QUANTIZED: return launch_rows_of<T, ROWS_NORM_QUANTIZED>(a, stream);
+        default: return launch_rows_of<T, ROWS_QUANTIZED>(a, stream);
     }
 }
 
@@ -279,72 +292,72 @@ hipError_t launch_norm_rows(const NormArgs& all, hipStream_t stream) {
     NormArgs a = all;
     a.per_n = 1.f / (float)a.cols;
     a.chunks = (a.cols + 511u) / 512u;
-    return a.f32 ? launch_rows_of<float>(a, stream) : launch_rows_of<__bf16>(a, stream);
+    return a.f32 ? launch_rows_as<float>(a, stream) : launch_rows_as<__bf16>(a, stream);
 }
 
 // ---- gradients
 
 // A workgroup takes a contiguous part of the rows, and has the sums of its part for the weights' gradient in registers: each lane those of its channels.  The next row is on its way while one is
-// worked on.
-template <typename T, int SPAN, int CH>
+// worked on.  LEAN, for rows so long that the registers do not hold all that: no next row, weights and dx_add are read where they are used.
+template <typename T, int SPAN, int CH, bool NT>
 __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : NORM_BWD_THREADS) void norm_bwd_kernel(NormBwdArgs a, uint32_t lanes) {
-    constexpr int PLACES = SPAN == SPAN_GROUP ? NORM_WAVES : 1;
-    __shared__ float sums[2][SPAN == SPAN_GROUP ? NORM_WAVES * CH : 1][2];  // of rows by turns: one barrier a row is enough
-    __shared__ double sums64[PLACES][2];
-    __shared__ __attribute__((aligned(16))) float dws[SPAN == SPAN_GROUP ? 4 : NORM_BWD_THREADS / 64 * CH * 512];
-    const Place<SPAN> at(lanes);
+    constexpr bool LEAN = SPAN == SPAN_GROUP && CH * (int)sizeof(T) >= 8;
+    constexpr int CHUNKS = SPAN == SPAN_GROUP ? NORM_WAVES * CH : 1;
+    __shared__ float sums[2][CHUNKS][2];  // of rows by turns: one barrier a row is enough
+    __shared__ float again[CHUNKS][2];
+    constexpr bool STAGED = SPAN == SPAN_GROUP && CH == 4;  // the sums for the weights' gradient in LDS: 8 floats a piece are too much as well
+    __shared__ __attribute__((aligned(16))) float dws[STAGED ? 64 * NORM_WAVES * CH * 8 : SPAN == SPAN_GROUP ? 4 : NORM_BWD_THREADS / 64 * CH * 512];
+    const Place<T, SPAN, CH> at(lanes, a.cols);
     const uint32_t first = (uint32_t)((uint64_t)blockIdx.x * a.n_rows / gridDim.x), end = (uint32_t)((uint64_t)(blockIdx.x + 1u) * a.n_rows / gridDim.x);
-    const uint32_t stride = Place<SPAN>::rows(lanes, blockDim.x);
-    auto there = [&](int i, uint32_t& c) __attribute__((always_inline)) -> bool {
-        c = (at.piece + i * at.step) * 8u;
-        return c < a.cols;
-    };
-    uint32_t c;
+    const uint32_t stride = at.rows(lanes), own = at.row(lanes);
     Piece<T> w[CH];
-    if (a.weight != nullptr) {
-#pragma unroll
-        for (int i = 0; i < CH; i++)
-            if (there(i, c)) w[i] = load_piece<T>(a.weight, c);
-    } else {
+    auto weight = [&](int i) __attribute__((always_inline)) {
         const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-#pragma unroll
-        for (int i = 0; i < CH; i++) w[i].set(ones);
-    }
-    float dw[CH][8] = {};
-    Piece<T> hn[CH], yn[CH], an[CH];
-    const bool adds = a.dx != nullptr && a.dx_add != nullptr;
-    auto load = [&](uint32_t row) __attribute__((always_inline)) {
-        if (row >= end) return;
-        const size_t in = (size_t)source_of(a.order, a.rows, row) * a.cols, to = (size_t)row * a.cols;
-#pragma unroll
-        for (int i = 0; i < CH; i++)
-            if (there(i, c)) {
-                hn[i] = load_piece<T>(a.h, to + c);
-                yn[i] = load_piece<T>(a.dy, in + c);
-                if (adds) an[i] = load_piece<T>(a.dx_add, to + c);
-            }
+        if (a.weight != nullptr) w[i] = at.template load_one<false>(a.weight, 0, true, i);
+        else w[i].set(ones);
     };
-    const uint32_t row0 = first + Place<SPAN>::row(lanes);
-    load(row0);
+    if (!LEAN) {
+#pragma unroll
+        for (int i = 0; i < CH; i++) weight(i);
+    }
+    float dw[STAGED ? 1 : CH][8] = {};
+    piece_u32x4* const staged = (piece_u32x4*)dws + threadIdx.x;  // a lane's own
+    if (STAGED) {
+#pragma unroll
+        for (int i = 0; i < 2 * CH; i++) staged[i * (64 * NORM_WAVES)] = piece_u32x4{0u, 0u, 0u, 0u};
+    }
+    Piece<T> hc[CH], yc[CH], ac[CH], hn[CH], yn[CH], an[CH];
+    const bool adds = a.dx != nullptr && a.dx_add != nullptr;
+    auto load = [&](uint32_t row, Piece<T> (&h)[CH], Piece<T> (&y)[CH], Piece<T> (&add)[CH]) __attribute__((always_inline)) {
+        const bool on = row < end;
+        const size_t in = on ? (size_t)source_of(a.order, a.rows, row) * a.cols : 0, to = (size_t)row * a.cols;
+        at.template load<NT>(a.h, to, on, h);
+        at.template load<NT>(a.dy, in, on, y);
+        if (adds && !LEAN) at.template load<NT>(a.dx_add, to, on, add);
+    };
+    if (!LEAN) load(first + own, hn, yn, an);
     uint32_t turn = 0u;
     // every lane goes through every round: rows are exchanged within wavefronts
     for (uint32_t base = first; base < end; base += stride) {
-        const uint32_t row = base + (row0 - first);
+        const uint32_t row = base + own;
         const bool on = row < end;
         if (SPAN == SPAN_WAVE && !on) break;
-        Piece<T> hc[CH], yc[CH], ac[CH];
+        if (LEAN) {
+            load(row, hc, yc, ac);
+        } else {
 #pragma unroll
-        for (int i = 0; i < CH; i++) {
-            hc[i] = hn[i];
-            yc[i] = yn[i];
-            ac[i] = an[i];
+            for (int i = 0; i < CH; i++) {
+                hc[i] = hn[i];
+                yc[i] = yn[i];
+                ac[i] = an[i];
+            }
+            load(row + stride, hn, yn, an);
         }
-        load(row + stride);
         float parts[2][CH], sum[2];
 #pragma unroll
         for (int i = 0; i < CH; i++) {
             parts[0][i] = parts[1][i] = 0.f;
-            if (!(on && there(i, c))) continue;
+            if (LEAN) weight(i);
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 const float h = hc[i].get(e);
@@ -355,80 +368,118 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : NORM_BWD_THR
         row_sums<SPAN, CH, 2>(parts, sum, lanes, a.chunks, sums[turn & 1u]);
         turn++;
         float r = inverse_size(sum[0], a.per_n, a.eps), mean = sum[1] * a.per_n * r;
-        const bool bad = on && (out_of_range(sum[0], a.per_n, a.eps) || !(fabsf(sum[1]) <= 1e38f));
+        const bool bad = on && out_of_range(sum[0], a.per_n, a.eps);
         if (__builtin_expect(SPAN == SPAN_GROUP ? bad : __builtin_amdgcn_ballot_w64(bad) != 0, 0)) {
-            double d[2] = {0., 0.};
+            const float by = into_range(sum[0]);
 #pragma unroll
             for (int i = 0; i < CH; i++) {
-                if (!(on && there(i, c))) continue;
+                parts[0][i] = parts[1][i] = 0.f;
+                if (LEAN) weight(i);
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    const double h = hc[i].get(e);
-                    d[0] += h * h;
-                    d[1] += (double)yc[i].get(e) * w[i].get(e) * h;
+                    const float h = hc[i].get(e) * by;
+                    parts[0][i] = fmaf(h, h, parts[0][i]);
+                    parts[1][i] = fmaf(yc[i].get(e) * w[i].get(e), h, parts[1][i]);
                 }
             }
             if (SPAN == SPAN_GROUP) __syncthreads();  // the last such row's have been read
-            row_sums64<SPAN>(d, lanes, sums64);
+            row_sums<SPAN, CH, 2>(parts, sum, lanes, a.chunks, again);
             if (bad) {
-                const double s = 1. / sqrt(d[0] / a.cols + a.eps);
-                r = (float)s;
-                mean = (float)(d[1] / a.cols * s);
+                const float s = inverse_size(sum[0], a.per_n, a.eps, by);
+                r = by * s;
+                mean = sum[1] * a.per_n * s;
             }
+        }
+        if (LEAN) {
+            // taken from the registers as they came once more, not kept as floats from above
+#pragma unroll
+            for (int i = 0; i < CH; i++)
+#pragma unroll
+                for (int u = 0; u < Piece<T>::UNITS; u++) asm volatile("" : "+v"(hc[i].raw[u]), "+v"(yc[i].raw[u]));
         }
 #pragma unroll
         for (int i = 0; i < CH; i++) {
-            if (!(on && there(i, c))) continue;
+            if (LEAN) {
+                __builtin_amdgcn_sched_barrier(0);  // a piece after the other
+                weight(i);
+                if (adds) ac[i] = at.template load_one<NT>(a.dx_add, (size_t)row * a.cols, on, i);
+            }
             float g[8];
+            Piece<float> d;
+            if (STAGED) {
+#pragma unroll
+                for (int q = 0; q < 2; q++) d.raw[q] = staged[(2 * i + q) * (64 * NORM_WAVES)];
+            } else d.set(dw[i]);
+            float(&sum_dw)[8] = dw[STAGED ? 0 : i];
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 const float u = hc[i].get(e) * r, y = yc[i].get(e);
-                dw[i][e] = fmaf(y, u, dw[i][e]);
+                sum_dw[e] = on ? fmaf(y, u, d.get(e)) : d.get(e);
                 g[e] = r * (y * w[i].get(e) - u * mean);
                 if (adds) g[e] += ac[i].get(e);
             }
-            if (a.dx == nullptr) continue;
-            Piece<T> p;
-            p.set(g);
-            store_piece<T>(a.dx, (size_t)row * a.cols + c, p);
+            if (STAGED) {
+                d.set(sum_dw);
+#pragma unroll
+                for (int q = 0; q < 2; q++) staged[(2 * i + q) * (64 * NORM_WAVES)] = d.raw[q];
+            }
+            if (a.dx != nullptr) at.template store<NT>(a.dx, (size_t)row * a.cols, on, i, g);
         }
     }
     if (a.dw == nullptr) return;
-    auto out = [&](const float (&s)[8]) __attribute__((always_inline)) {
+    auto out = [&](int i, const float (&s)[8]) __attribute__((always_inline)) {
         Piece<float> p;
         p.set(s);
-        store_piece<float>(a.parts, (size_t)blockIdx.x * a.cols + c, p);
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            uint32_t c;
+            if (!at.at(i, Piece<T>::UNITS == 2 ? q : 0, c)) continue;
+            store16<false>(a.parts + (size_t)blockIdx.x * a.cols + c + (Piece<T>::UNITS == 2 ? 0u : 4u * q), p.raw[q]);
+        }
     };
     if (SPAN == SPAN_GROUP) {
 #pragma unroll
-        for (int i = 0; i < CH; i++)
-            if (there(i, c)) out(dw[i]);
+        for (int i = 0; i < CH; i++) {
+            if (STAGED) {
+                Piece<float> d;
+#pragma unroll
+                for (int q = 0; q < 2; q++) d.raw[q] = staged[(2 * i + q) * (64 * NORM_WAVES)];
+#pragma unroll
+                for (int e = 0; e < 8; e++) dw[0][e] = d.get(e);
+            }
+            out(i, dw[STAGED ? 0 : i]);
+        }
         return;
     }
     // the wavefronts' sums, and those of the rows that a wavefront has at once, in order
-    const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if constexpr (SPAN != SPAN_GROUP) {
+        const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+        piece_u32x4* const mine = (piece_u32x4*)dws + (threadIdx.x & 63u);
 #pragma unroll
-    for (int i = 0; i < CH; i++) {
-        if (SPAN == SPAN_LANES) {
-            for (uint32_t off = 32u; off >= lanes; off >>= 1)
+        for (int i = 0; i < CH; i++) {
+            if (SPAN == SPAN_LANES) {
+                for (uint32_t off = 32u; off >= lanes; off >>= 1)
 #pragma unroll
-                for (int e = 0; e < 8; e++) dw[i][e] += __shfl_xor(dw[i][e], (int)off);
+                    for (int e = 0; e < 8; e++) dw[i][e] += __shfl_xor(dw[i][e], (int)off);
+            }
+            Piece<float> p;
+            p.set(dw[i]);
+#pragma unroll
+            for (int q = 0; q < 2; q++) mine[((wave * CH + i) * 2u + q) * 64u] = p.raw[q];
         }
-        Piece<float> p;
-        p.set(dw[i]);
-        store_piece<float>(dws, ((wave * CH + i) * 64u + (threadIdx.x & 63u)) * 8u, p);
-    }
-    __syncthreads();
-    if (wave != 0u || (SPAN == SPAN_LANES && threadIdx.x >= lanes)) return;
+        __syncthreads();
+        if (wave != 0u || (SPAN == SPAN_LANES && threadIdx.x >= lanes)) return;
 #pragma unroll
-    for (int i = 0; i < CH; i++) {
-        if (!there(i, c)) continue;
-        for (uint32_t v = 1; v < waves; v++) {
-            const Piece<float> p = load_piece<float>(dws, ((v * CH + i) * 64u + threadIdx.x) * 8u);
+        for (int i = 0; i < CH; i++) {
+            for (uint32_t v = 1; v < waves; v++) {
+                Piece<float> p;
 #pragma unroll
-            for (int e = 0; e < 8; e++) dw[i][e] += p.get(e);
+                for (int q = 0; q < 2; q++) p.raw[q] = mine[((v * CH + i) * 2u + q) * 64u];
+#pragma unroll
+                for (int e = 0; e < 8; e++) dw[i][e] += p.get(e);
+            }
+            out(i, dw[i]);
         }
-        out(dw[i]);
     }
 }
 
@@ -453,19 +504,16 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
 
 uint32_t norm_bwd_parts(uint32_t rows, uint32_t cols) { return norm_bwd_shape(rows, cols).parts; }
 
-template <typename T>
+template <typename T, bool NT>
 static hipError_t launch_bwd_t(const NormBwdArgs& a, hipStream_t stream) {
     const NormBwdShape s = norm_bwd_shape(a.n_rows, a.cols);
-    if (s.span == SPAN_LANES) norm_bwd_kernel<T, SPAN_LANES, 1><<<s.parts, s.threads, 0, stream>>>(a, s.lanes);
+    if (s.span == SPAN_LANES) norm_bwd_kernel<T, SPAN_LANES, 1, NT><<<s.parts, s.threads, 0, stream>>>(a, s.lanes);
 #define ROWS(SPAN, CH) \
-    else if (s.span == SPAN && s.ch == CH) norm_bwd_kernel<T, SPAN, CH><<<s.parts, s.threads, 0, stream>>>(a, 64u);
+    else if (s.span == SPAN && s.ch == CH) norm_bwd_kernel<T, SPAN, CH, NT><<<s.parts, s.threads, 0, stream>>>(a, 64u);
     ROWS(SPAN_WAVE, 1)
     ROWS(SPAN_WAVE, 2)
-    ROWS(SPAN_WAVE, 3)
-    ROWS(SPAN_WAVE, 4)
     ROWS(SPAN_GROUP, 1)
     ROWS(SPAN_GROUP, 2)
-    ROWS(SPAN_GROUP, 3)
     ROWS(SPAN_GROUP, 4)
 #undef ROWS
     else return hipErrorInvalidValue;
@@ -479,7 +527,9 @@ hipError_t launch_norm_bwd(const NormBwdArgs& all, hipStream_t stream) {
     NormBwdArgs a = all;
     a.per_n = 1.f / (float)a.cols;
     a.chunks = (a.cols + 511u) / 512u;
-    return a.f32 ? launch_bwd_t<float>(a, stream) : launch_bwd_t<__bf16>(a, stream);
+    const uint64_t moved = (uint64_t)a.n_rows * a.cols * (a.f32 ? 4u : 2u) * (2u + (a.dx ? 1u : 0u) + (a.dx && a.dx_add ? 1u : 0u));
+    if (moved >= NORM_PAST_CACHES) return a.f32 ? launch_bwd_t<float, true>(a, stream) : launch_bwd_t<__bf16, true>(a, stream);
+    return a.f32 ? launch_bwd_t<float, false>(a, stream) : launch_bwd_t<__bf16, false>(a, stream);
 }
 
 }  // namespace skiparse

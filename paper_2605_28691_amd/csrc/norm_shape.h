@@ -7,8 +7,7 @@ namespace skiparse {
 constexpr uint32_t NORM_WAVES = 16;          // of a workgroup that has a row, at most
 constexpr uint32_t NORM_BWD_THREADS = 256;   // of one whose wavefronts have a row each
 
-// threads of a workgroup that has a row, at most, with `ch` pieces a lane
-constexpr uint32_t norm_group_threads(int ch) { return ch >= 8 ? 32u * NORM_WAVES : 64u * NORM_WAVES; }
+constexpr uint64_t NORM_PAST_CACHES = 256ull << 20;  // bytes that a call moves, from which on nothing of them is worth a place in the caches
 
 enum NormSpan : int { SPAN_LANES = 0, SPAN_WAVE = 1, SPAN_GROUP = 2 };  // a row: of a part of a wavefront, of one, of a workgroup
 struct NormShape {
@@ -22,20 +21,19 @@ inline uint32_t norm_lanes(uint32_t pieces) {
     return lanes;
 }
 
-inline NormShape norm_shape(uint32_t rows, uint32_t cols) {
-    const uint32_t pieces = (cols + 7u) / 8u;
+// `read`: bytes that are read for a channel.  What counts is that enough of them are on their way: 16 workgroups of few wavefronts a CU, or fewer of more; with rows of more than 3 pieces a lane the wavefronts of
+// a workgroup share one, two pieces a lane where a channel has 2 bytes, one otherwise.  (us, rows of a wavefront / of a workgroup with 1, 2, 4 pieces a lane: 80,640 x 5120 with residual 579 / 535 / 562 / 564,
+// quantised 225 / 308 / 217 / 225; 32,760 x 1536 with residual, quantised 57.3 / 59.8 / 58.6 / 58.3; 6426 x 4008 float32 with residual - / 75.8 / 78.8 / 82.7; one row of 5120 4.9 / 2.6 / 2.9 / 3.6,
+// 256 rows 8.7 / 5.3 / 5.6 / 6.2.)
+inline NormShape norm_shape(uint32_t rows, uint32_t cols, uint32_t read) {
+    const uint32_t pieces = (cols + 7u) / 8u, per_lane = (pieces + 63u) / 64u;
     if (pieces <= 32u) return {SPAN_LANES, 1, norm_lanes(pieces), 256u};
-    const uint32_t per_lane = (pieces + 63u) / 64u;
-    if (rows >= 2048u && per_lane <= 10u) {
-        for (int ch : {1, 2, 3, 4, 6, 8, 10})
-            if ((uint32_t)ch >= per_lane) return {SPAN_WAVE, ch, 64u, 256u};
-    }
-    const uint32_t most = rows >= 2048u ? 8u : 1u;
-    for (int ch : {1, 2, 4, 8}) {
+    if (per_lane == 1u || (rows >= 1024u && per_lane <= 3u)) return {SPAN_WAVE, (int)per_lane, 64u, 256u};
+    for (int ch : {rows >= 1024u && read <= 2u ? 2 : 1, 2}) {
         const uint32_t waves = (per_lane + (uint32_t)ch - 1u) / (uint32_t)ch;
-        if (waves <= NORM_WAVES && (uint32_t)ch >= most) return {SPAN_GROUP, ch, 64u, 64u * waves};
+        if (waves <= NORM_WAVES) return {SPAN_GROUP, ch, 64u, 64u * waves};
     }
-    return {SPAN_GROUP, 4, 64u, 64u * NORM_WAVES};
+    return {SPAN_GROUP, 4, 64u, 64u * ((per_lane + 3u) / 4u)};
 }
 
 struct NormBwdShape {
@@ -49,15 +47,17 @@ inline NormBwdShape norm_bwd_shape(uint32_t rows, uint32_t cols) {
     if (pieces <= 32u) {
         s = {SPAN_LANES, 1, norm_lanes(pieces), NORM_BWD_THREADS, 0u};
         at_once = NORM_BWD_THREADS / s.lanes;
-    } else if (per_lane <= 4u) {
+    } else if (per_lane <= 2u) {
         s = {SPAN_WAVE, (int)per_lane, 64u, NORM_BWD_THREADS, 0u};
         at_once = NORM_BWD_THREADS / 64u;
     } else {
-        const uint32_t ch = per_lane <= 48u ? 3u : 4u;
+        const uint32_t ch = per_lane <= 16u ? 1u : per_lane <= 32u ? 2u : 4u;
         s = {SPAN_GROUP, (int)ch, 64u, 64u * ((per_lane + ch - 1u) / ch), 0u};
     }
-    const uint32_t rounds = (rows + at_once - 1u) / at_once;
-    s.parts = rounds < 1024u ? rounds : 1024u;
+    const uint32_t rounds = (rows + at_once - 1u) / at_once, waves = s.threads / 64u;
+    const uint32_t most = 256u * ((7u + waves) / waves), few = rounds / 8u > 256u ? rounds / 8u : 256u;
+    s.parts = most < few ? most : few;
+    if (s.parts > rounds) s.parts = rounds;
     return s;
 }
 

@@ -1,4 +1,5 @@
-// Eight channels of a row as they lie in memory, bf16 or float32: what a lane moves at once in the passes over rows.
+// Eight channels of a row as a lane of the passes over rows has them: 16 bytes of bf16, or twice 16 bytes of float32.  An instruction moves 16 bytes a lane, neighbours' next to each other, so that lines are moved
+// as a whole: a lane's two halves in float32 lie apart by all the lanes' first halves.  (32 bytes a lane in one place: 6426 x 4008 normalised in 79.5 us, now PIECE_US.)
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -12,6 +13,7 @@ template <typename T>
 struct Piece;
 template <>
 struct Piece<__bf16> {
+    static constexpr int UNITS = 1, EACH = 8;  // instructions that move it, channels of one
     piece_u32x4 raw[1];
     __device__ inline float get(int e) const { return __uint_as_float(e & 1 ? raw[0][e >> 1] & 0xffff0000u : raw[0][e >> 1] << 16); }
     __device__ inline void set(const float (&v)[8]) {
@@ -24,6 +26,7 @@ struct Piece<__bf16> {
 };
 template <>
 struct Piece<float> {
+    static constexpr int UNITS = 2, EACH = 4;
     piece_u32x4 raw[2];
     __device__ inline float get(int e) const { return __uint_as_float(raw[e >> 2][e & 3]); }
     __device__ inline void set(const float (&v)[8]) {
@@ -32,20 +35,15 @@ struct Piece<float> {
     }
 };
 
-// `at`: in elements
-template <typename T>
-__device__ inline Piece<T> load_piece(const void* from, size_t at) {
-    Piece<T> p;
-    const piece_u32x4* const q = (const piece_u32x4*)((const T*)from + at);
-#pragma unroll
-    for (unsigned i = 0; i < sizeof(p.raw) / 16; i++) p.raw[i] = q[i];
-    return p;
+// NT: past the caches, for tensors that they do not hold until the next pass
+template <bool NT>
+__device__ __attribute__((always_inline)) inline piece_u32x4 load16(const void* p) {
+    return NT ? __builtin_nontemporal_load((const piece_u32x4*)p) : *(const piece_u32x4*)p;
 }
-template <typename T>
-__device__ inline void store_piece(void* to, size_t at, const Piece<T>& p) {
-    piece_u32x4* const q = (piece_u32x4*)((T*)to + at);
-#pragma unroll
-    for (unsigned i = 0; i < sizeof(p.raw) / 16; i++) q[i] = p.raw[i];
+template <bool NT>
+__device__ __attribute__((always_inline)) inline void store16(void* p, piece_u32x4 v) {
+    if (NT) __builtin_nontemporal_store(v, (piece_u32x4*)p);
+    else *(piece_u32x4*)p = v;
 }
 
 }  // namespace skiparse
