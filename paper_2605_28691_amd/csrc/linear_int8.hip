@@ -6,11 +6,12 @@
 
 namespace skiparse {
 
-// One row: a wavefront has CH channels and reads 2048 codes of each at once; four products an instruction (v_dot4_i32_i8).
-template <int CH>
+// One row: a wavefront has two channels and reads 2048 codes of each at once; four products an instruction (v_dot4_i32_i8).  Bound by reading w, and by what a launch takes.  (us, 1 / 2 / 4 channels: 5120 -> 5120
+// 7.4 / 7.2 / 8.0, 1536 -> 8960 6.2 / 5.0 / 5.3, 8960 -> 1536 7.6 / 6.0 / 6.6, 5120 -> 30,720, 157 MB, 32.1 / 29.5 / 29.5.)
+constexpr int ROW8_CHANNELS = 2;
 __global__ __launch_bounds__(256) void linear_int8_row_kernel(LinearArgs a) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-    constexpr int AT_ONCE = 2;  // times 1024 codes
+    constexpr int CH = ROW8_CHANNELS, AT_ONCE = 2;  // times 1024 codes
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t n0 = (blockIdx.x * 4u + wave) * CH;
     if (n0 >= a.N) return;
@@ -55,10 +56,9 @@ __global__ __launch_bounds__(256) void linear_int8_row_kernel(LinearArgs a) {
     ((__bf16*)e.out)[n] = (__bf16)z;
 }
 
-template <int CH>
 static hipError_t launch_row8(const LinearArgs& a, hipStream_t stream) {
-    constexpr uint32_t per = CH * 4u;
-    linear_int8_row_kernel<CH><<<(a.N + per - 1u) / per, 256, 0, stream>>>(a);
+    constexpr uint32_t per = ROW8_CHANNELS * 4u;
+    linear_int8_row_kernel<<<(a.N + per - 1u) / per, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 template <int FM, int FN>
@@ -68,17 +68,14 @@ static hipError_t launch_few8(const LinearArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 static hipError_t launch_few8(const LinearArgs& a, hipStream_t stream) {
-    if (a.M == 1u) {  // moved or not, row 0
-        const uint32_t channels = row_channels(a.N);
-        return channels == 1u ? launch_row8<1>(a, stream) : channels == 2u ? launch_row8<2>(a, stream) : launch_row8<4>(a, stream);
-    }
-    if (few_blocks(a.M, a.N, a.K) == 2u) return a.M <= 16u ? launch_few8<1, 2>(a, stream) : launch_few8<2, 2>(a, stream);
+    if (a.M == 1u) return launch_row8(a, stream);  // moved or not, row 0
+    if (few_blocks8(a.M, a.N, a.K * 2u) == 2u) return a.M <= 16u ? launch_few8<1, 2>(a, stream) : launch_few8<2, 2>(a, stream);
     return a.M <= 16u ? launch_few8<1, 1>(a, stream) : launch_few8<2, 1>(a, stream);
 }
 
 template <bool EXTRAS>
 static hipError_t launch_int8(const LinearArgs& a, hipStream_t stream) {
-    const LinearPlan p = plan_linear(a.M, a.N, a.K);
+    const LinearPlan p = plan_linear(a.M, a.N, a.K, LINEAR_TILE8);
     switch (p.shape) {
         case T256: return launch_tiles<T256, LINEAR_INT8, EXTRAS>(a, p, stream);
         case T128: return launch_tiles<T128, LINEAR_INT8, EXTRAS>(a, p, stream);
@@ -87,10 +84,10 @@ static hipError_t launch_int8(const LinearArgs& a, hipStream_t stream) {
     }
 }
 
-size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K) { return linear_few(M, K / 2u) ? 0u : plan_linear(M, N, K / 2u).workspace(); }
+size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K) { return linear_few8(M, N, K) ? 0u : plan_linear(M, N, K / 2u, LINEAR_TILE8).workspace(); }
 
 hipError_t launch_linear_int8(const LinearArgs& a, hipStream_t stream) {
-    if (linear_few(a.M, a.K)) return launch_few8(a, stream);
+    if (linear_few8(a.M, a.N, a.K * 2u)) return launch_few8(a, stream);
     return a.e.act != ACT_NONE || a.e.residual ? launch_int8<true>(a, stream) : launch_int8<false>(a, stream);
 }
 
