@@ -25,7 +25,7 @@ def _weight(g, cols, dtype):
 
 
 SIZES = [(1, 8), (1, 5120), (3, 16), (2, 24), (5, 40), (7, 64), (130, 72), (1000, 128), (33, 136), (9, 256), (70, 264), (20, 504), (65, 512), (66, 520), (17, 1000), (12, 1024), (40, 1032), (31, 1536),
-         (8, 2048), (5, 2056), (3, 4008), (300, 5120), (6, 8192), (4, 13824), (2, 20480), (3, 32760), (2, 32768), (70001, 64), (2049, 1536)]
+         (8, 2048), (5, 2056), (3, 4008), (300, 5120), (6, 8192), (4, 13824), (2, 20480), (3, 32760), (2, 32768), (70001, 64), (2049, 1536), (1500, 1000), (1100, 5120), (1030, 264), (1024, 10008)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -119,6 +119,38 @@ def test_gradients_against_differences():
         e[c] = 2.0 ** -7
         num = (loss(h, w + e) - loss(h, w - e)).sum() / ((w + e).double() - (w - e).double())[c]
         assert (num - dw[c].double()).abs() <= 2.0 ** -10 * (dy.double() * y).abs().sum(), c
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows, cols", [(700_000, 64), (300_001, 264), (70_003, 1000), (45_001, 1536), (13_002, 5120), (5_003, 13824), (2_100, 32768)])
+def test_a_row_depends_on_nothing_but_itself(rows, cols, dtype):
+    """Whichever lanes have it, and whether the tensors go past the caches (256 MB moved and more) or not: its bits are those of a call of few rows."""
+    import paper_2605_28691_amd as sk
+
+    g = _gen(cols)
+    x, res, dy = (torch.randn(rows, cols, generator=g, device="cuda").to(dtype) for _ in range(3))
+    w = _weight(g, cols, dtype)
+    out, total = sk.skiparse_rmsnorm_fwd(x, w, res)
+    q, _ = sk.skiparse_rmsnorm_fwd(x, w, res, quantize=True)
+    z = sk.skiparse_quantize_int8(x)
+    dx, dw = sk.skiparse_rmsnorm_bwd(dy, total, w, dx_add=res)
+    for first, n in ((0, 1), (rows - 1, 1), (rows // 3, 5), (rows // 2, 300), (rows - 1025, 1025)):
+        part = slice(first, first + n)
+        xs, rs, ds = x[part].clone(), res[part].clone(), dy[part].clone()
+        o, t = sk.skiparse_rmsnorm_fwd(xs, w, rs)
+        assert torch.equal(o, out[part]) and torch.equal(t, total[part]), n
+        p, _ = sk.skiparse_rmsnorm_fwd(xs, w, rs, quantize=True)
+        assert torch.equal(p.codes, q.codes[part]) and torch.equal(p.scales, q.scales[part]), n
+        p = sk.skiparse_quantize_int8(xs)
+        assert torch.equal(p.codes, z.codes[part]) and torch.equal(p.scales, z.scales[part]), n
+        assert torch.equal(sk.skiparse_rmsnorm_bwd(ds, t, w, dx_add=rs)[0], dx[part]), n
+    # and in place
+    t = res.clone()
+    assert torch.equal(sk.skiparse_rmsnorm_fwd(x, w, t, total=t)[0], out) and torch.equal(t, total)
+    t = res.clone()
+    assert torch.equal(sk.skiparse_rmsnorm_bwd(dy, total, w, dx_add=t, dx=t)[0], dx)
+    _, ew, _, bw = nr.norm_grads(dy, total, w, None, EPS)
+    nr.close(dw, ew, nr.ROUND[dtype] * ew.abs() + bw, "dw")
 
 
 GRIDS = [(1, (2, 4, 8), 2, "token"), (2, (1, 8, 4), 2, "group"), (3, (1, 9, 18), 3, "token"), (2, (2, 9, 9), 3, "group"), (1, (3, 16, 16), 4, "group"), (1, (21, 30, 52), 2, "token")]
@@ -271,6 +303,55 @@ def test_what_lies_round_the_results():
         sk.skiparse_rmsnorm_bwd(out, total, w, dx=dx, dw=dw, workspace=space[1])
         for buf, _, pad in rooms + [space]:
             assert untouched(buf, pad), (rows, cols)
+
+
+@pytest.mark.parametrize("rows, cols", [(1, 5120), (390, 1536), (2049, 264), (30, 20480), (513, 64)])
+def test_two_graphs_and_two_streams(rows, cols):
+    """A training step's calls in two captured graphs that run at once, each with a workspace of its own; replays with other inputs in the same places."""
+    import paper_2605_28691_amd as sk
+
+    g = _gen(rows)
+    sets = []
+    for _ in range(2):
+        x, res, dy = (torch.randn(rows, cols, generator=g, device="cuda").bfloat16() for _ in range(3))
+        w = _weight(g, cols, torch.bfloat16)
+        out, total = sk.skiparse_rmsnorm_fwd(x, w, res)
+        q = sk.skiparse_quantize_int8(out)
+        dx, dw = sk.skiparse_rmsnorm_bwd(dy, total, w, dx_add=dy)
+        sets.append((x, res, dy, w, out, total, q, dx, dw, torch.empty(sk.skiparse_rmsnorm_bwd_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")))
+
+    def step(x, res, dy, w, out, total, q, dx, dw, ws):
+        sk.skiparse_rmsnorm_fwd(x, w, res, out=out, total=total)
+        sk.skiparse_quantize_int8(out, out=q)
+        sk.skiparse_rmsnorm_bwd(dy, total, w, dx_add=dy, dx=dx, dw=dw, workspace=ws)
+
+    graphs = []
+    for s in sets:
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            step(*s)
+        graphs.append(gr)
+    streams = [torch.cuda.Stream() for _ in sets]
+    for turn in range(4):
+        for s in sets:
+            for t in s[:3]:
+                t.copy_(t.roll(1, -1) if turn % 2 else -t.flip(-1))
+        want = []
+        for s in sets:
+            fresh = [*s[:4], *(torch.empty_like(t) for t in s[4:6]), sk.Quantized(*(torch.empty_like(t) for t in s[6])), *(torch.empty_like(t) for t in s[7:])]
+            step(*fresh)
+            want.append(fresh)
+            for t in (*s[4:6], *s[6], *s[7:]):
+                t.zero_()
+        torch.cuda.synchronize()
+        for gr, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                gr.replay()
+        torch.cuda.synchronize()
+        for s, f in zip(sets, want):
+            for a, b in zip((*s[4:6], *s[6], *s[7:9]), (*f[4:6], *f[6], *f[7:9])):
+                assert torch.equal(a, b), turn
 
 
 def test_tensors_that_are_refused():
