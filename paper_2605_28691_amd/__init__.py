@@ -758,20 +758,22 @@ def _quantized_of(shape, like) -> Quantized:
 def _is_quantized(q, what: str, shape=None) -> Quantized:
     if not isinstance(q, Quantized):
         raise ValueError(f"{what} must be Quantized")
-    shape = tuple(q.codes.shape) if shape is None else tuple(shape)
-    if q.codes.dtype != torch.int8 or q.scales.dtype != torch.float32 or tuple(q.codes.shape) != shape or tuple(q.scales.shape) != shape[:-1]:
-        raise ValueError(f"{what}: not int8 codes of shape {shape} with a float32 scale a row")
+    codes, scales = q
+    at = codes.shape
+    if codes.dtype != torch.int8 or scales.dtype != torch.float32 or scales.shape != at[:-1] or (shape is not None and at != shape):
+        raise ValueError(f"{what}: not int8 codes{'' if shape is None else f' of shape {tuple(shape)}'} with a float32 scale a row")
     return q
 
 
 def _same_type(like, *tensors) -> None:
+    dtype = like.dtype
     for t in tensors:
-        if t is not None and t.dtype != like.dtype:
+        if t is not None and t.dtype != dtype:
             raise ValueError(f"tensors of one type are needed, {like.dtype} here")
 
 
 def _of_channels(weight, cols: int) -> None:
-    if weight is not None and tuple(weight.shape) != (cols,):
+    if weight is not None and weight.shape != (cols,):
         raise ValueError(f"weight must have shape ({cols},)")
 
 
@@ -853,13 +855,13 @@ def skiparse_linear_fwd_int8(x: Quantized, w: Quantized, bias: torch.Tensor | No
     if w.codes.dim() != 2:
         raise ValueError("w is [out, in]")
     K, (N, Kw) = x.codes.shape[-1], w.codes.shape
-    if K != Kw or (bias is not None and tuple(bias.shape) != (N,)):
+    if K != Kw or (bias is not None and bias.shape != (N,)):
         raise ValueError("x, w and bias do not fit each other")
     _bf16("bias and residual", bias, residual)
     grid, lead = _linear_rows(x.codes.shape[:-1], order, T, H, W, s)
     shape = (*lead, N)
     out = _into(out, shape, x.codes, torch.bfloat16)
-    if residual is not None and tuple(residual.shape) != shape:
+    if residual is not None and residual.shape != shape:
         raise ValueError(f"residual must have the result's shape {shape}")
     _here(*x, *w, bias, residual, out, workspace)
     M = grid[0] * grid[1] * grid[2] * grid[3]
