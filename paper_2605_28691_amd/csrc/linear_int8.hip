@@ -75,7 +75,7 @@ static hipError_t launch_few8(const LinearArgs& a, hipStream_t stream) {
 
 template <bool EXTRAS>
 static hipError_t launch_int8(const LinearArgs& a, hipStream_t stream) {
-    const LinearPlan p = plan_linear(a.M, a.N, a.K, LINEAR_TILE8);
+    const LinearPlan p = plan_linear(a.M, a.N, a.K, a.e.act != ACT_NONE ? LINEAR_TILE8_ACT : LINEAR_TILE8);
     switch (p.shape) {
         case T256: return launch_tiles<T256, LINEAR_INT8, EXTRAS>(a, p, stream);
         case T128: return launch_tiles<T128, LINEAR_INT8, EXTRAS>(a, p, stream);
@@ -84,7 +84,12 @@ static hipError_t launch_int8(const LinearArgs& a, hipStream_t stream) {
     }
 }
 
-size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K) { return linear_few8(M, N, K) ? 0u : plan_linear(M, N, K / 2u, LINEAR_TILE8).workspace(); }
+// for either, with an activation and without
+size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K) {
+    if (linear_few8(M, N, K)) return 0u;
+    const size_t without = plan_linear(M, N, K / 2u, LINEAR_TILE8).workspace(), with = plan_linear(M, N, K / 2u, LINEAR_TILE8_ACT).workspace();
+    return without > with ? without : with;
+}
 
 hipError_t launch_linear_int8(const LinearArgs& a, hipStream_t stream) {
     if (linear_few8(a.M, a.N, a.K * 2u)) return launch_few8(a, stream);

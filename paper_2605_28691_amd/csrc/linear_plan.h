@@ -27,10 +27,14 @@ constexpr uint64_t LINEAR_GRID = 1ull << 24;  // a launch has fewer workgroups o
 constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {
     {256, 256, 1, 7.6f, 0.945f, {1.3f}}, {128, 128, 2, 2.58f, 0.308f, {0.57f, 0.88f}}, {64, 64, 4, 1.45f, 0.241f, {0.302f, 0.39f, 0.61f, 0.883f}}, {128, 256, 1, 4.29f, 0.587f, {0.809f}}};
 // In 8-bit integers, a step of 128 codes: the same bytes, twice the products.  Fitted to products of 58 sizes (33 to 80,640 rows, 104 to 20,480 channels), each with every tile and several numbers of parts: what the
-// rule takes is 0.8 % slower than the best in the mean, 12 % at most (with the numbers above 4.7 % and 52 %).  For example, us, 256 / 128 / 64 / 128 x 256, uncut: 6426 x 1008 -> 4008 45 / 51 / 66 / 57,
+// rule takes is 1.2 % slower than the best in the mean, 15 % at most (with the numbers above 4.7 % and 52 %).  For example, us, 256 / 128 / 64 / 128 x 256, uncut: 6426 x 1008 -> 4008 45 / 51 / 66 / 57,
 // 16,000 x 640 -> 640 19 / 23 / 25 / 24, 390 x 1536 -> 8960 23 / 16 / 14 / 21; 1560 x 5120 -> 13,824 129 / 131 / 186 / 148, 256 cut in two 121.
 constexpr LinearTile LINEAR_TILE8[LINEAR_SHAPES] = {
     {256, 256, 1, 8.44f, 1.098f, {1.461f}}, {128, 128, 2, 4.21f, 0.486f, {0.872f, 1.099f}}, {64, 64, 4, 2.22f, 0.389f, {0.49f, 0.632f, 0.813f, 1.009f}}, {128, 256, 1, 4.92f, 0.961f, {1.099f}}};
+// With an activation, which a CU's one large workgroup has all to itself: 36 of these products with GELU, 1.1 % in the mean and 12 % at most, without a table of their own 3.5 % and 23 %.  For example
+// 14,771 x 144 -> 8064 123 / 100 / - / 141 us, without GELU 83 / 85 / - / 102; 33,735 x 880 -> 944 82 / 74 / 83 / 87, without 65 / 69 / 83 / 72.
+constexpr LinearTile LINEAR_TILE8_ACT[LINEAR_SHAPES] = {
+    {256, 256, 1, 12.94f, 1.098f, {1.461f}}, {128, 128, 2, 4.21f, 0.486f, {0.872f, 1.099f}}, {64, 64, 4, 2.82f, 0.389f, {0.49f, 0.632f, 0.813f, 1.009f}}, {128, 256, 1, 6.42f, 0.961f, {1.099f}}};
 constexpr float LINEAR_JOIN = 3.2f, LINEAR_JOIN_BYTE = 2.3e-7f;  // us of the launch that joins parts, and of a byte that goes through memory
 
 // us a step with `units` workgroups running, at most a full round
