@@ -295,18 +295,20 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
 /*
  * Root-mean-square norm of rows of `cols` channels (the tokens of a hidden state, or, with heads * rows of head_dim channels, the heads of q and k), bf16 or float32:
  *   h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h r weight            residual NULL: h = x;  weight NULL: ones
- * x, residual and sum have their rows on the one side of `order`, out (and out_scales) on the other: a norm in front of a chain of sparse blocks writes the sparse layout, the residual stream
- *   stays where it is.  rows = B*T*H*W (plain rows: a grid 1 x 1 x rows).
+ * x, residual and sum have their rows on the one side of `order`, out and out_scales on the other: a norm in front of a chain of sparse blocks writes the sparse layout, the residual stream
+ *   stays where it is.  rows = B*T*H*W (plain rows: a grid 1 x 1 x rows).  All tensors are of one type.
  *   sum: NULL, or where h, rounded, is kept; only with a residual.  It may be x or residual.  y is made of the sum as it is before that rounding.
  *   out: y rounded to the type of x, with out_scales NULL; or, with out_scales [rows], the int8 codes and scales of y.  Where rows keep their places out may be x (if it is no codes, and sum is not x).
- *   Nothing else may overlap.  cols a multiple of 8 up to 32,768; eps > 0.  Sums in float32, and in 64 bits where squares leave its range; one rounding.
- * Rows in 8-bit integers: m = largest |v| of the row (at least 2^-118), code = rne(v * (127 / m)), scale = m / 127, all decisions in float32, so codes are -127 .. 127 and a value is code * scale.  A row of zeros has scale 1; one
- *   that holds a value that is not finite has codes 0 and scale NaN, so that what a product makes of it is NaN too.  The norm's codes are those of h weight, which is y up to the row's factor r.
+ *   Nothing else may overlap.  cols a multiple of 8 up to 32,768; eps from 2^-126 to 2^100.  Sums in float32, of values times a power of two where their squares would leave its range; one rounding.
+ * Rows in 8-bit integers: m = largest |v| of the row (at least 2^-118), code = rne(v * (127 / m)), scale = m / 127, all decisions in float32: codes are -127 .. 127, a value is code * scale.  A row of
+ *   zeros has scale 1; one that holds a value that is not finite has codes 0 and scale NaN, so that what a product makes of it is NaN too.  The norm's codes are those of v = h weight, which is y up to
+ *   the row's factor r (h weight beyond float32's range is not finite).
  * skiparse_quantize_int8: x, rows moved as `order` says, in 8-bit integers: activations in front of a product, or once the weights ([out_features][in_features]: a scale a channel).
  * skiparse_rmsnorm_bwd: gradients for a loss with dL/dy = dy (rows as out's), h as kept in sum (or x, without a residual; rows as x's):
  *   g = dy weight, u = h r:  dx = r (g - u mean(g u)) + dx_add,  dweight = sum over the rows of dy u;     dx is x's gradient and the residual's.
- *   dx_add (what comes along the residual stream; NULL or rows as dx's) may be dx.  dx or dw may be NULL (not wanted).  dw is shaped as weight, in its type.
- *   workspace: skiparse_rmsnorm_bwd_workspace_bytes() bytes where dw is wanted, else NULL will do.  Deterministic (sums over rows in a fixed order, which may depend on rows and cols and on nothing else).
+ *   dx_add (what comes along the residual stream; NULL or rows as dx's) may be dx, nothing else may overlap.  dx or dw may be NULL (not wanted).  dw is shaped as weight, in the tensors' type.
+ *   workspace: skiparse_rmsnorm_bwd_workspace_bytes() bytes where dw is wanted, else NULL will do; it holds nothing between calls, and calls that may overlap need one each.
+ * A row's bits depend on nothing but the row, whatever shares the call; dw's on the rows in their order.
  */
 int skiparse_rmsnorm_fwd(const void* x, const void* residual, const void* weight, void* sum, void* out, float* out_scales, int B, int T, int H, int W, int cols,
                          float eps, int s, int pattern, int order, int dtype, void* stream);

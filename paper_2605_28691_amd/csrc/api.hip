@@ -832,8 +832,8 @@ static RowArgs row_args(int B, int T, int H, int W, int s, int pattern, bool to_
     const GridMap g = make_gridmap(T, H, W, s, pattern);
     return to_sparse ? make_row_args<TO_SPARSE>(g, (uint32_t)B) : make_row_args<TO_ORIGINAL>(g, (uint32_t)B);
 }
-// a finite number above zero
-static bool valid_eps(float eps) { return eps >= 1.17549435e-38f && eps <= 3.0e38f; }
+// no denormal number, and so far from the largest that it can be added to a mean of squares
+static bool valid_eps(float eps) { return eps >= 0x1p-126f && eps <= 0x1p100f; }
 
 int skiparse_rmsnorm_fwd(const void* x, const void* residual, const void* weight, void* sum, void* out, float* out_scales, int B, int T, int H, int W, int cols,
                          float eps, int s, int pattern, int order, int dtype, void* stream) {

@@ -2,7 +2,9 @@
 // norm's gradients.  All sums in float32.
 //     h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h r w          int8: codes and scale of h w (int8_rows.h), the scale times r: r is the same for a row and changes no code
 //     g = dy w,  u = h r,  dx = r (g - u mean(g u)) + dx_add,  dw = sum over the rows of dy u
-// Bound by HBM bandwidth: every tensor is moved once, a row stays in registers between its sum and its result.
+// Bound by HBM bandwidth: every tensor is moved once, a row stays in registers between its sum and its result (norm_shape.h: which lanes have it).  Of the norm's codes the largest value and the sum of squares
+// come from one pass over these registers: codes do not need r.  80,640 x 5120 in bf16: with residual and sum, into the sparse layout, 560 us (3.3 GB, 5.9 TB/s; a copy of 2 GiB reaches 4.96), in 8-bit
+// integers 199 us (1.24 GB, 6.2); 32,760 x 1536 with residual in codes 57 us (5.3).
 #include "int8_rows.h"
 #include "kernels.h"
 #include "norm_shape.h"
@@ -297,6 +299,8 @@ hipError_t launch_norm_rows(const NormArgs& all, hipStream_t stream) {
 
 // ---- gradients
 
+// dx and the weights' gradient in one pass over dy and h: 32,760 x 1536 with dx_add 75 us, and 4.4 for the parts' sums (403 MB: 5.1 TB/s), 80,640 x 5120 637 (5.2 TB/s), 6426 x 1000 float32 18 + 3.9 (77 MB: what
+// is in flight with 1024 wavefronts; with twice as many the parts cost what is won).
 // A workgroup takes a contiguous part of the rows, and has the sums of its part for the weights' gradient in registers: each lane those of its channels.  The next row is on its way while one is
 // worked on.  LEAN, for rows so long that the registers do not hold all that: no next row, weights and dx_add are read where they are used.
 template <typename T, int SPAN, int CH, bool NT>

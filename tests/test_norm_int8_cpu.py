@@ -28,7 +28,7 @@ def test_norm_refusals(lib):
         return lib.skiparse_rmsnorm_fwd(x, residual, weight, total, out, scales, B, T, H, W, cols, ctypes.c_float(eps), s, pattern, order, dtype, None)
 
     q = dict(scales=P[5])
-    for bad in (dict(x=None), dict(out=None), dict(residual=None), dict(eps=0), dict(eps=-1e-6), dict(eps=NAN), dict(eps=INF), dict(eps=1e-40), dict(order=3), dict(order=-1), dict(dtype=7), dict(B=0), dict(T=-1),
+    for bad in (dict(x=None), dict(out=None), dict(residual=None), dict(eps=0), dict(eps=-1e-6), dict(eps=NAN), dict(eps=INF), dict(eps=1e-40), dict(eps=2e30), dict(order=3), dict(order=-1), dict(dtype=7), dict(B=0), dict(T=-1),
                 dict(cols=0), dict(pattern=2), dict(s=0), dict(x=ODD), dict(residual=ODD), dict(weight=ODD), dict(total=ODD), dict(out=ODD), dict(scales=ODD),
                 # buffers that overlap: rows move here, so not even whole ones may
                 dict(out=P[0]), dict(out=_near(P[0])), dict(out=P[1]), dict(out=P[2]), dict(out=P[3]), dict(total=_near(P[0])), dict(total=_near(P[1])), dict(total=P[2]),
