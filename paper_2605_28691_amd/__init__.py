@@ -514,7 +514,7 @@ def _here(*tensors) -> None:
     """Calls go to the current device's stream: a tensor of another device is refused.  (One on the CPU is refused where its address is asked for.)"""
     device = torch.cuda.current_device() if _get_device is None else _get_device()
     for t in tensors:
-        if t is not None and t.get_device() not in (device, -1):
+        if t is not None and (at := t.get_device()) != device and at != -1:
             raise ValueError(f"tensor on {t.device}, but the current device is {device}")
 
 
@@ -782,21 +782,26 @@ def skiparse_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, re
     """h / sqrt(mean(h^2) + eps) * weight over the last dimension, h = x + residual: the result, or with a residual (result, h).  bf16 or float32, all of one type; h is rounded to it, the result made
     of what it is before that.  quantize=True: the result as Quantized, for skiparse_linear_fwd_int8.  order "to_sparse" or "to_original" moves the rows of the grid T x H x W on the way: x, residual and h
     are [B][T*H*W][channels] or [s*s*B][T*H*W/(s*s)][channels], the result the other; h stays where x is.  `out` and `total` (of h; may be residual or x) are buffers to use; out may be x where rows stay."""
-    cols = x.shape[-1]
-    grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
+    at = x.shape
+    cols = at[-1]
+    if order == "same":
+        grid, shape = (1, 1, 1, x.numel() // max(cols, 1)), at
+    else:
+        grid, lead = _linear_rows(at[:-1], order, T, H, W, s)
+        shape = (*lead, cols)
     _of_channels(weight, cols)
     _same_type(x, weight, residual)
-    if residual is not None and residual.shape != x.shape:
-        raise ValueError(f"residual must have the shape of x, {tuple(x.shape)}")
-    if total is not None and residual is None:
-        raise ValueError("without a residual the sum is x")
-    shape, scales = (*lead, cols), None
+    scales = None
     if quantize:
         codes, scales = out = _quantized_of(shape, x) if out is None else _is_quantized(out, "out", shape)
     else:
         codes = out = _into(out, shape, x)
     if residual is not None:
-        total = _into(total, x.shape, x)
+        if residual.shape != at:
+            raise ValueError(f"residual must have the shape of x, {tuple(at)}")
+        total = _into(total, at, x)
+    elif total is not None:
+        raise ValueError("without a residual the sum is x")
     _here(x, weight, residual, total, codes, scales)
     _skiparse_rmsnorm_fwd(x, residual, weight, total, codes, scales, *grid, cols, float(eps), s, PATTERNS[pattern], ORDERS[order], _DTYPES[x.dtype], _stream())
     return out if residual is None else (out, total)
@@ -834,11 +839,16 @@ def skiparse_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor
 def skiparse_quantize_int8(x: torch.Tensor, order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", out: Quantized | None = None) -> Quantized:
     """[..., channels] in bf16 or float32 -> int8 codes and a float32 scale a row: activations in front of skiparse_linear_fwd_int8, or once its weights [out, in].  order moves rows on the way, as in
     skiparse_rmsnorm_fwd."""
-    grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
-    shape = (*lead, x.shape[-1])
-    out = _quantized_of(shape, x) if out is None else _is_quantized(out, "out", shape)
-    _here(x, *out)
-    _skiparse_quantize_int8(x, out.codes, out.scales, *grid, x.shape[-1], s, PATTERNS[pattern], ORDERS[order], _DTYPES[x.dtype], _stream())
+    shape = x.shape
+    cols = shape[-1]
+    if order == "same":
+        grid = (1, 1, 1, x.numel() // max(cols, 1))
+    else:
+        grid, lead = _linear_rows(shape[:-1], order, T, H, W, s)
+        shape = (*lead, cols)
+    codes, scales = out = _quantized_of(shape, x) if out is None else _is_quantized(out, "out", shape)
+    _here(x, codes, scales)
+    _skiparse_quantize_int8(x, codes, scales, *grid, cols, s, PATTERNS[pattern], ORDERS[order], _DTYPES[x.dtype], _stream())
     return out
 
 
@@ -852,19 +862,20 @@ def skiparse_linear_fwd_int8(x: Quantized, w: Quantized, bias: torch.Tensor | No
     [..., out] bf16.  order as in skiparse_linear_fwd; the scales' rows move with the codes'.  `out` (may be residual) and `workspace` are buffers to use."""
     _is_quantized(x, "x")
     _is_quantized(w, "w")
-    if w.codes.dim() != 2:
+    xc, xs = x
+    wc, ws = w
+    if wc.dim() != 2:
         raise ValueError("w is [out, in]")
-    K, (N, Kw) = x.codes.shape[-1], w.codes.shape
-    if K != Kw or (bias is not None and bias.shape != (N,)):
+    at, (N, K) = xc.shape, wc.shape
+    if at[-1] != K or (bias is not None and bias.shape != (N,)):
         raise ValueError("x, w and bias do not fit each other")
     _bf16("bias and residual", bias, residual)
-    grid, lead = _linear_rows(x.codes.shape[:-1], order, T, H, W, s)
+    grid, lead = _linear_rows(at[:-1], order, T, H, W, s)
     shape = (*lead, N)
-    out = _into(out, shape, x.codes, torch.bfloat16)
+    out = _into(out, shape, xc, torch.bfloat16)
     if residual is not None and residual.shape != shape:
         raise ValueError(f"residual must have the result's shape {shape}")
-    _here(*x, *w, bias, residual, out, workspace)
-    M = grid[0] * grid[1] * grid[2] * grid[3]
-    workspace, size = _space(workspace, x.codes, "skiparse_linear_fwd_int8_workspace_bytes", M, K, N)
-    _skiparse_linear_fwd_int8(x.codes, x.scales, w.codes, w.scales, bias, residual, out, *grid, K, N, s, PATTERNS[pattern], ORDERS[order], ACTS[act], workspace, size, _stream())
+    _here(xc, xs, wc, ws, bias, residual, out, workspace)
+    workspace, size = _space(workspace, xc, "skiparse_linear_fwd_int8_workspace_bytes", grid[0] * grid[1] * grid[2] * grid[3], K, N)
+    _skiparse_linear_fwd_int8(xc, xs, wc, ws, bias, residual, out, *grid, K, N, s, PATTERNS[pattern], ORDERS[order], ACTS[act], workspace, size, _stream())
     return out
