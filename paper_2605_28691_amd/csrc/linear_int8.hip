@@ -2,10 +2,10 @@
 // The products are those of linear_tiles.h with v_mfma_i32_16x16x64_i8: its operands are 16 bytes a lane, as those of the bf16 product are, and k is summed over, so the walk over k, what it
 // loads and how it lies in LDS are the same bytes, two codes in the place of one number.  What is left of the sums on the way out are scales: those of a wavefront's rows and channels are asked for before
 // its walk begins.  Parts of a sum are whole numbers too: however a product is cut, a row's bits are the same.
-// Large products are bound by the matrix cores at the board's power limit: 16,384^3 2915 TOP/s (a library's product without an epilogue 2434), 80,640 x 5120 -> 20,480 2.69 without an epilogue and
-// 2.5 with GELU (6.2 and 6.7 ms).  Small ones by what stands outside the walk: 32,760 x 1536 -> 1536, three rounds of 256 tiles, 87 us, of which a tile has 1.5 until its loads leave, 2.5 until they land, 20 to 23 for
-// twelve steps (14 with codes of zero) and 5 for its results, 12 with a residual, which all CUs move at once (without any results 71).  Loads sent off earlier in a step and waited for later, in a second barrier, were
-// 3 % slower, results past the caches as well, and first tiles that begin at four different times no faster.
+// Large products are bound by the matrix cores at the board's power limit: 16,384^3 2915 TOP/s (a library's product without an epilogue 2434), 80,640 x 5120 -> 20,480 2.74 without an epilogue and
+// 2.62 with GELU (6.2 and 6.4 ms).  Small ones by what stands outside the walk: 32,760 x 1536 -> 1536, three rounds of 256 tiles, 84 us.  A tile of it has 1.5 until its loads leave, 2.5 until they land, 5 for its
+// results, 12 with a residual, which all CUs move at once, and the rest for twelve steps (20 to 23 with two buffers, 14 on codes of zero; without any results the product took 71 of then 87).  Loads sent off
+// earlier in a step and waited for later, in a second barrier, were 3 % slower, results past the caches as well, and first tiles that begin at four different times no faster.
 #include "linear_tiles.h"
 
 namespace skiparse {
@@ -79,11 +79,10 @@ static hipError_t launch_few8(const LinearArgs& a, hipStream_t stream) {
 
 template <bool EXTRAS>
 static hipError_t launch_int8(const LinearArgs& a, hipStream_t stream) {
-    const LinearPlan p = plan_linear(a.M, a.N, a.K, a.e.act != ACT_NONE ? LINEAR_TILE8_ACT : LINEAR_TILE8);
+    const LinearPlan p = plan_linear8(a.M, a.N, a.K, a.e.act != ACT_NONE);
     switch (p.shape) {
         case T256: return launch_tiles<T256, LINEAR_INT8, EXTRAS>(a, p, stream);
         case T128: return launch_tiles<T128, LINEAR_INT8, EXTRAS>(a, p, stream);
-        case T128X256: return launch_tiles<T128X256, LINEAR_INT8, EXTRAS>(a, p, stream);
         default: return launch_tiles<T64, LINEAR_INT8, EXTRAS>(a, p, stream);
     }
 }
@@ -91,7 +90,7 @@ static hipError_t launch_int8(const LinearArgs& a, hipStream_t stream) {
 // for either, with an activation and without
 size_t linear_int8_workspace(uint32_t M, uint32_t N, uint32_t K) {
     if (linear_few8(M, N, K)) return 0u;
-    const size_t without = plan_linear(M, N, K / 2u, LINEAR_TILE8).workspace(), with = plan_linear(M, N, K / 2u, LINEAR_TILE8_ACT).workspace();
+    const size_t without = plan_linear8(M, N, K / 2u, false).workspace(), with = plan_linear8(M, N, K / 2u, true).workspace();
     return without > with ? without : with;
 }
 

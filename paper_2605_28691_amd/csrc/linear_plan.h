@@ -26,15 +26,16 @@ constexpr uint64_t LINEAR_GRID = 1ull << 24;  // a launch has fewer workgroups o
 // 40 / 17 / 18 / 25; cut best: 3840 x 5120 -> 5120 155 / 173 / 285 / 184.
 constexpr LinearTile LINEAR_TILE[LINEAR_SHAPES] = {
     {256, 256, 1, 7.6f, 0.945f, {1.3f}}, {128, 128, 2, 2.58f, 0.308f, {0.57f, 0.88f}}, {64, 64, 4, 1.45f, 0.241f, {0.302f, 0.39f, 0.61f, 0.883f}}, {128, 256, 1, 4.29f, 0.587f, {0.809f}}};
-// In 8-bit integers, a step of 128 codes: the same bytes, twice the products.  Fitted to products of 58 sizes (33 to 80,640 rows, 104 to 20,480 channels), each with every tile and several numbers of parts: what the
-// rule takes is 1.2 % slower than the best in the mean, 15 % at most (with the numbers above 4.7 % and 52 %).  For example, us, 256 / 128 / 64 / 128 x 256, uncut: 6426 x 1008 -> 4008 45 / 51 / 66 / 57,
-// 16,000 x 640 -> 640 19 / 23 / 25 / 24, 390 x 1536 -> 8960 23 / 16 / 14 / 21; 1560 x 5120 -> 13,824 129 / 131 / 186 / 148, 256 cut in two 121.
-constexpr LinearTile LINEAR_TILE8[LINEAR_SHAPES] = {
-    {256, 256, 1, 8.44f, 1.098f, {1.461f}}, {128, 128, 2, 4.21f, 0.486f, {0.872f, 1.099f}}, {64, 64, 4, 2.22f, 0.389f, {0.49f, 0.632f, 0.813f, 1.009f}}, {128, 256, 1, 4.92f, 0.961f, {1.099f}}};
-// With an activation, which a CU's one large workgroup has all to itself: 36 of these products with GELU, 1.1 % in the mean and 12 % at most, without a table of their own 3.5 % and 23 %.  For example
-// 14,771 x 144 -> 8064 123 / 100 / - / 141 us, without GELU 83 / 85 / - / 102; 33,735 x 880 -> 944 82 / 74 / 83 / 87, without 65 / 69 / 83 / 72.
-constexpr LinearTile LINEAR_TILE8_ACT[LINEAR_SHAPES] = {
-    {256, 256, 1, 12.94f, 1.098f, {1.461f}}, {128, 128, 2, 4.21f, 0.486f, {0.872f, 1.099f}}, {64, 64, 4, 2.82f, 0.389f, {0.49f, 0.632f, 0.813f, 1.009f}}, {128, 256, 1, 6.42f, 0.961f, {1.099f}}};
+// In 8-bit integers, a step of 128 codes: the same bytes, twice the products, another walk, and no tiles of 128 x 256 (two of 128 x 128 on a CU are as good).  Fitted to products of 58 sizes (33 to 80,640 rows, 104 to
+// 20,480 channels), each with every tile and several numbers of parts: what the rule takes is 1.1 % slower than the best in the mean, 12 % at most (with the numbers above 3.4 % and 47 %).  For example, us,
+// 256 / 128 / 64, uncut: 6426 x 1008 -> 4008 44 / 47 / 65, 16,000 x 640 -> 640 20 / 21 / 23, 390 x 1536 -> 8960 23 / 16 / 15; 1560 x 5120 -> 13,824 120 / 126 / 190, 256 cut in two 117.
+constexpr int LINEAR_SHAPES8 = T64 + 1;
+constexpr LinearTile LINEAR_TILE8[LINEAR_SHAPES8] = {
+    {256, 256, 1, 10.34f, 0.971f, {1.267f}}, {128, 128, 2, 4.44f, 0.338f, {0.641f, 0.925f}}, {64, 64, 4, 2.33f, 0.322f, {0.411f, 0.515f, 0.83f, 0.933f}}};
+// With an activation, which a CU's one large workgroup has all to itself: 36 of these products with GELU, 1.3 % in the mean and 10 % at most, without a table of their own 2.5 % and 18 %.  (14,771 x 144 -> 8064
+// 125 / 99 us, without GELU 85 / 82.)
+constexpr LinearTile LINEAR_TILE8_ACT[LINEAR_SHAPES8] = {
+    {256, 256, 1, 12.34f, 0.971f, {1.267f}}, {128, 128, 2, 4.44f, 0.338f, {0.641f, 0.925f}}, {64, 64, 4, 2.33f, 0.322f, {0.411f, 0.515f, 0.83f, 0.933f}}};
 constexpr float LINEAR_JOIN = 3.2f, LINEAR_JOIN_BYTE = 2.3e-7f;  // us of the launch that joins parts, and of a byte that goes through memory
 
 // us a step with `units` workgroups running, at most a full round
@@ -66,10 +67,10 @@ inline uint32_t linear_rows_parts(uint32_t M, uint32_t N) {
 }
 
 // The last round of workgroups over the CUs is seldom full: its tiles are cut along k, into as many parts as make it shortest.
-inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K, const LinearTile (&costs)[LINEAR_SHAPES] = LINEAR_TILE) {
+inline LinearPlan plan_linear(uint32_t M, uint32_t N, uint32_t K, const LinearTile* costs = LINEAR_TILE, int shapes = LINEAR_SHAPES) {
     LinearPlan best = {};
     float best_cost = 0.f;
-    for (int shape = 0; shape < LINEAR_SHAPES; shape++) {
+    for (int shape = 0; shape < shapes; shape++) {
         const LinearTile& t = costs[shape];
         const uint64_t tiles_m = ((uint64_t)M + t.m - 1u) / t.m, tiles_n = ((uint64_t)N + t.n - 1u) / t.n, tiles = tiles_m * tiles_n;
         const uint64_t slots = (uint64_t)LINEAR_CUS * t.per_cu, rounds = tiles / slots, rest = tiles - rounds * slots;
@@ -111,6 +112,9 @@ inline uint32_t few_blocks(uint32_t M, uint32_t N, uint32_t K) { return N >= 409
 inline bool linear_few8(uint32_t M, uint32_t N, uint32_t K) { return M == 1u || (K >= 512u && (M <= 16u || (M <= 32u && N < 16384u))); }
 // (us, one / two blocks of 16 channels: 5120 -> 5120, 2 rows 9.9 / 8.8, 16 rows 11.1 / 9.9, 17 rows 13.8 / 10.6; 1536 -> 8960, 16 rows 8.6 / 9.3, 17 rows 11.6 / 10.4; 8960 -> 1536, 16 rows 8.8 / 11.9.)
 inline uint32_t few_blocks8(uint32_t M, uint32_t N, uint32_t K) { return N >= 4096u && (K >= 4096u || M > 16u) ? 2u : 1u; }
+
+// K in pairs of codes
+inline LinearPlan plan_linear8(uint32_t M, uint32_t N, uint32_t K, bool act) { return plan_linear(M, N, K, act ? LINEAR_TILE8_ACT : LINEAR_TILE8, LINEAR_SHAPES8); }
 
 // Workgroup -> tile.  Workgroup id % 8 is the XCD; each XCD has a contiguous range of an order in which TILE_GROUP tiles of m are walked together along n, so that the 32
 // tiles that it works on at once share operands in its L2.

@@ -98,17 +98,15 @@ __device__ __attribute__((always_inline)) inline float int8_plus(float z, float 
     return z + residual;
 }
 
-// Scales of a wavefront's share of a product in 8-bit integers: lane l holds those of its rows l and 64 + l, and of its channels.
+// Scales and bias of a wavefront's share of a product in 8-bit integers: lane l holds those of its rows l and 64 + l, and of its channels.
 template <int FM, int FN, bool INT8>
 struct Scales {
     __device__ __attribute__((always_inline)) inline Scales(const LinearArgs&, uint32_t, uint32_t, uint32_t) {}
 };
 template <int FM, int FN>
 struct Scales<FM, FN, true> {
-    static constexpr int ROWS = (FM + 3) / 4;
-    float x[ROWS];
-    f32x4 w[FN];
-    bf16x4 bias[FN];
+    static constexpr int ROWS = (FM + 3) / 4, COLS = (FN + 3) / 4;
+    float x[ROWS], w[COLS], bias[COLS];
     __device__ __attribute__((always_inline)) inline Scales(const LinearArgs& a, uint32_t m0, uint32_t n0, uint32_t lane) {
 #pragma unroll
         for (int r = 0; r < ROWS; r++) {
@@ -118,23 +116,36 @@ struct Scales<FM, FN, true> {
             x[r] = a.x_scales[m];
         }
 #pragma unroll
-        for (int j = 0; j < FN; j++) {
-            const uint32_t n = n0 + 16u * j + 4u * (lane >> 4);
-            w[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            bias[j] = bf16x4{};
-            if (n < a.N) {
-                w[j] = *(const f32x4*)(a.w_scales + n);
-                if (a.e.bias != nullptr) bias[j] = *(const bf16x4*)((const __bf16*)a.e.bias + n);
-            }
+        for (int r = 0; r < COLS; r++) {
+            uint32_t n = n0 + 64u * r + lane;
+            n = n < a.N ? n : a.N - 1u;  // channels behind the last are not stored
+            w[r] = a.w_scales[n];
+            bias[r] = a.e.bias != nullptr ? (float)((const __bf16*)a.e.bias)[n] : 0.f;
         }
     }
     // of row 16 i + lane % 16
     __device__ __attribute__((always_inline)) inline float row(int i, uint32_t lane) const { return __shfl(x[i / 4], (i % 4) * 16 + (int)(lane & 15u)); }
-    __device__ __attribute__((always_inline)) inline f32x4 values(const f32x4& sums, float x_scale, int j) const {
+    // of the lane's channels of block j, as they lie in the accumulators
+    struct Channels {
+        f32x4 w[FN], bias[FN];
+    };
+    __device__ __attribute__((always_inline)) inline Channels channels(uint32_t lane) const {
+        Channels c;
+#pragma unroll
+        for (int j = 0; j < FN; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int from = (j % 4) * 16 + 4 * (int)(lane >> 4) + e;
+                c.w[j][e] = __shfl(w[j / 4], from);
+                c.bias[j][e] = __shfl(bias[j / 4], from);
+            }
+        return c;
+    }
+    __device__ __attribute__((always_inline)) inline static f32x4 values(const f32x4& sums, float x_scale, const Channels& c, int j) {
         const i32x4 s = __builtin_bit_cast(i32x4, sums);
         f32x4 z;
 #pragma unroll
-        for (int e = 0; e < 4; e++) z[e] = int8_value(s[e], x_scale, w[j][e], (float)bias[j][e]);
+        for (int e = 0; e < 4; e++) z[e] = int8_value(s[e], x_scale, c.w[j][e], c.bias[j][e]);
         return z;
     }
 };
@@ -306,6 +317,36 @@ __device__ __attribute__((always_inline)) inline f32x4 take(const f32x4& acc) {
     return f32x4{w, x, y, z};
 }
 
+// Accumulators by their registers' names, four for block R / 4: of the products in 8-bit integers, whose walk over three buffers has several ways out, where the compiler would move them about.  It knows no
+// more of them than that begin() overwrites them; with fewer than 256 other values at once it has no use for accumulation registers of its own (tests/test_norm_shape.py looks at what it makes).
+#define ACC10(t) "a" #t "0", "a" #t "1", "a" #t "2", "a" #t "3", "a" #t "4", "a" #t "5", "a" #t "6", "a" #t "7", "a" #t "8", "a" #t "9"
+#define ACC16 ACC10(), "a10", "a11", "a12", "a13", "a14", "a15"
+#define ACC64 ACC10(), ACC10(1), ACC10(2), ACC10(3), ACC10(4), ACC10(5), "a60", "a61", "a62", "a63"
+#define ACC256 ACC10(), ACC10(1), ACC10(2), ACC10(3), ACC10(4), ACC10(5), ACC10(6), ACC10(7), ACC10(8), ACC10(9), ACC10(10), ACC10(11), ACC10(12), ACC10(13), ACC10(14), ACC10(15), ACC10(16), ACC10(17), \
+    ACC10(18), ACC10(19), ACC10(20), ACC10(21), ACC10(22), ACC10(23), ACC10(24), "a250", "a251", "a252", "a253", "a254", "a255"
+template <int REGISTERS>
+__device__ __attribute__((always_inline)) inline void acc_begin() {
+    static_assert(REGISTERS == 16 || REGISTERS == 64 || REGISTERS == 256, "a tile's");
+    if constexpr (REGISTERS == 16) asm volatile("" ::: ACC16);
+    else if constexpr (REGISTERS == 64) asm volatile("" ::: ACC64);
+    else asm volatile("" ::: ACC256);
+}
+template <int R>
+__device__ __attribute__((always_inline)) inline void acc_clear() {
+    asm volatile("v_accvgpr_write_b32 a[%0], 0\n\tv_accvgpr_write_b32 a[%1], 0\n\tv_accvgpr_write_b32 a[%2], 0\n\tv_accvgpr_write_b32 a[%3], 0" ::"n"(R), "n"(R + 1), "n"(R + 2), "n"(R + 3));
+}
+template <int R>
+__device__ __attribute__((always_inline)) inline void acc_product(const bf16x8& q, const bf16x8& p) {
+    asm volatile("v_mfma_i32_16x16x64_i8 a[%0:%1], %2, %3, a[%0:%1]" ::"n"(R), "n"(R + 3), "v"(q), "v"(p));
+}
+template <int R>
+__device__ __attribute__((always_inline)) inline f32x4 acc_take() {
+    float w, x, y, z;
+    asm volatile("v_accvgpr_read_b32 %0, a[%4]\n\tv_accvgpr_read_b32 %1, a[%5]\n\tv_accvgpr_read_b32 %2, a[%6]\n\tv_accvgpr_read_b32 %3, a[%7]"
+                 : "=&v"(w), "=&v"(x), "=&v"(y), "=&v"(z) : "n"(R), "n"(R + 1), "n"(R + 2), "n"(R + 3));
+    return f32x4{w, x, y, z};
+}
+
 template <int N>
 using Int = std::integral_constant<int, N>;
 // f(Int<0>) ... f(Int<N - 1>), written out (the loop of 64 products with what stands between them is too much for the unroller)
@@ -327,6 +368,7 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
     // separate arrays: the compiler must be able to tell that what is being filled is not what is being read.  [buffer][half]; what is in one piece has the first only
     __shared__ __attribute__((aligned(1024))) char p00[SP::BYTES], p01[PT ? SP::BYTES : 16], p10[SP::BYTES], p11[PT ? SP::BYTES : 16];
     __shared__ __attribute__((aligned(1024))) char q00[SQ::BYTES], q01[QT ? SQ::BYTES : 16], q10[SQ::BYTES], q11[QT ? SQ::BYTES : 16];
+    __shared__ __attribute__((aligned(1024))) char p20[INT8 ? SP::BYTES : 16];  // a third one, below
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave & 1u, wn = wave >> 1;
     uint32_t tm, tn, k0, k1, slot;
@@ -363,7 +405,11 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
         return {p0 + (PT ? (size_t)k * ldp : (size_t)k * 2u), q0 + (QT ? (size_t)k * ldq : (size_t)k * 2u), records(PT, k, ldp, m0), records(QT, k, ldq, n0), k < k1 ? k1 - k : 0u};
     };
     const Scales<FM, FN, INT8> scales(a, m0 + wm * (FM * 16u), n0 + wn * (FN * 16u), lane);  // on their way before the walk begins
-    f32x4 acc[FM][FN];  // sums begin with the bias; those of a part, and whole numbers, with 0
+    f32x4 acc[INT8 ? 1 : FM][INT8 ? 1 : FN];  // sums begin with the bias; those of a part, and whole numbers, with 0
+    if constexpr (INT8) {
+        acc_begin<FM * FN * 4>();
+        each<FM * FN>([&](auto G) __attribute__((always_inline)) { acc_clear<4 * decltype(G)::value>(); });
+    } else
 #pragma unroll
     for (int j = 0; j < FN; j++) {
         const f32x4 b = slot == ~0u ? Out<FN, FORM, EXTRAS>::bias(a, n0 + wn * (FN * 16u), j, lane) : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -400,7 +446,7 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
         constexpr int LOADS = decltype(LOADC)::value;
         each<MF>([&](auto G) __attribute__((always_inline)) {
             constexpr int g = decltype(G)::value;
-            if constexpr (INT8) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc[g / FN][g % FN]) : "v"(f.q[g % FN]), "v"(f.p[g / FN]));
+            if constexpr (INT8) acc_product<4 * g>(f.q[g % FN], f.p[g / FN]);
             else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[g / FN][g % FN]) : "v"(f.q[g % FN]), "v"(f.p[g / FN]));
             // number i of n stands behind product i * MF / n
             constexpr int first = (g * RD + MF - 1) / MF, last = ((g + 1) * RD + MF - 1) / MF;
@@ -426,35 +472,86 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
         part(Int<LOADS_B>{}, f1, f0, n0, [&](int i) __attribute__((always_inline)) { load_b(s0, c0, s1, c1, i); });
         if (LOADS_A) meet(Int<LOADS_A + LOADS_B>{});
     };
-    const Half h00 = {p00, q00, 0}, h01 = {PT ? p01 : p00, QT ? q01 : q00, 1}, h10 = {p10, q10, 0}, h11 = {PT ? p11 : p10, QT ? q11 : q10, 1};
-    auto fill = [&](uint32_t k, const Half& first, const Half& second) __attribute__((always_inline)) {
-        const Step s0 = step_at(k), s1 = step_at(k + LIN_KT / 2u);
+    if constexpr (INT8) {
+        // A step takes half the time that it takes in the other forms, less than memory needs to answer.  P, the activations, which come from memory (the weights are in the caches), has three buffers: step t asks for
+        // P of t + 2 in its first half, while P of t is still read, and for Q of t + 2 in its second, into the buffer just read; between the halves all but the loads just sent have landed, the next step's, P's of
+        // which had a step and Q's half of one.  32,760 x 1536 -> 1536 90.6 us with two buffers of both, 84.3 with the third.  P asked for yet half a step sooner, no wait for it until the step after the next:
+        // 80,640 x 5120 -> 20,480 6165 -> 6614 us, since workgroups that share rows drift apart and read them again.
+        auto step8 = [&](uint32_t k, char* cp, char* cq, char* np, char* nq, char* fp) __attribute__((always_inline)) {
+            const Step s2 = step_at(k + 2u * LIN_KT);
+            part(Int<SP::INSTR>{}, f0, f1, Half{cp, cq, 1}, [&](int i) __attribute__((always_inline)) { sp.issue(i, s2.p, s2.rp, s2.left, fp, wave); });
+            meet(Int<SP::INSTR>{});
+            part(Int<SQ::INSTR>{}, f1, f0, Half{np, nq, 0}, [&](int i) __attribute__((always_inline)) { sq.issue(i, s2.q, s2.rq, s2.left, cq, wave); });
+        };
+        auto fill_p = [&](uint32_t k, char* to) __attribute__((always_inline)) {
+            const Step at = step_at(k);
 #pragma unroll
-        for (int i = 0; i < LOADS_A; i++) load_a(s0, first, i);
+            for (int i = 0; i < SP::INSTR; i++) sp.issue(i, at.p, at.rp, at.left, to, wave);
+        };
+        auto fill_q = [&](uint32_t k, char* to) __attribute__((always_inline)) {
+            const Step at = step_at(k);
 #pragma unroll
-        for (int i = 0; i < LOADS_B; i++) load_b(s0, first, s1, second, i);
-    };
-    fill(k0, h00, h01);
-    fill(k0 + LIN_KT, h10, h11);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS_A + LOADS_B) : "memory");
-    __builtin_amdgcn_s_barrier();
+            for (int i = 0; i < SQ::INSTR; i++) sq.issue(i, at.q, at.rq, at.left, to, wave);
+        };
+        fill_p(k0, p00);
+        fill_q(k0, q00);
+        fill_p(k0 + LIN_KT, p10);
+        fill_q(k0 + LIN_KT, q10);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SP::INSTR + SQ::INSTR) : "memory");
+        __builtin_amdgcn_s_barrier();
 #pragma unroll
-    for (int i = 0; i < RD; i++) fragment(f0, h00, i);
-    if (LOADS_A) meet(Int<LOADS_A + LOADS_B>{});
-    uint32_t k = k0;  // below k1
-    do {              // a second step behind the end adds zeros
-        step(k, h00, h01, h10);
-        step(k + LIN_KT, h10, h11, h00);
-        // The products are written as asm, with their accumulators pinned to accumulation registers: left to choose, the compiler moved 200 of them in and out a step.  It does not
-        // see their latency then (4 passes, so 7 clocks until a result may be read): the last ones are waited for here, in front of all that may follow.
-        asm volatile("s_nop 15" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        k += 2u * LIN_KT;
-    } while (k < k1);
+        for (int i = 0; i < RD; i++) fragment(f0, Half{p00, q00, 0}, i);
+        // the wait behind the last products: see below
+        auto pair = [&](uint32_t k, char* a, char* b, char* c) __attribute__((always_inline)) {
+            step8(k, a, q00, b, q10, c);
+            step8(k + LIN_KT, b, q10, c, q00, a);
+            asm volatile("s_nop 15" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        uint32_t k = k0;
+        for (;;) {
+            pair(k, p00, p10, p20);
+            if ((k += 2u * LIN_KT) >= k1) break;
+            pair(k, p20, p00, p10);
+            if ((k += 2u * LIN_KT) >= k1) break;
+            pair(k, p10, p20, p00);
+            if ((k += 2u * LIN_KT) >= k1) break;
+        }
+    } else {
+        const Half h00 = {p00, q00, 0}, h01 = {PT ? p01 : p00, QT ? q01 : q00, 1}, h10 = {p10, q10, 0}, h11 = {PT ? p11 : p10, QT ? q11 : q10, 1};
+        auto fill = [&](uint32_t k, const Half& first, const Half& second) __attribute__((always_inline)) {
+            const Step s0 = step_at(k), s1 = step_at(k + LIN_KT / 2u);
+#pragma unroll
+            for (int i = 0; i < LOADS_A; i++) load_a(s0, first, i);
+#pragma unroll
+            for (int i = 0; i < LOADS_B; i++) load_b(s0, first, s1, second, i);
+        };
+        fill(k0, h00, h01);
+        fill(k0 + LIN_KT, h10, h11);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS_A + LOADS_B) : "memory");
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int i = 0; i < RD; i++) fragment(f0, h00, i);
+        if (LOADS_A) meet(Int<LOADS_A + LOADS_B>{});
+        uint32_t k = k0;  // below k1
+        do {              // a second step behind the end adds zeros
+            step(k, h00, h01, h10);
+            step(k + LIN_KT, h10, h11, h00);
+            // The products are written as asm, with their accumulators pinned to accumulation registers: left to choose, the compiler moved 200 of them in and out a step.  It does not
+            // see their latency then (4 passes, so 7 clocks until a result may be read): the last ones are waited for here, in front of all that may follow.
+            asm volatile("s_nop 15" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            k += 2u * LIN_KT;
+        } while (k < k1);
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads behind the end still write (zeros) to LDS
     __builtin_amdgcn_sched_barrier(0);
     if (slot != ~0u) {  // a part: sums as they lie in the registers, for linear_join_kernel
         f32x4* const to = (f32x4*)a.partial + ((size_t)slot * 4u + wave) * (FM * FN * 64u) + lane;
+        if constexpr (INT8) {
+            each<FM * FN>([&](auto G) __attribute__((always_inline)) { to[decltype(G)::value * 64] = acc_take<4 * decltype(G)::value>(); });
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < FM; i++)
 #pragma unroll
@@ -465,17 +562,21 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
     asm volatile("" : "+v"(own));  // formed here: else what follows from it is kept in registers through the whole walk
     const Out<FN, FORM, EXTRAS> out(a, m0 + wm * (FM * 16u), n0 + wn * (FN * 16u), own);
     typename Out<FN, FORM, EXTRAS>::Residual r = out.residual(a, 0);
+    const auto channels = [&]() __attribute__((always_inline)) {
+        if constexpr (INT8) return scales.channels(own);
+        else return 0;
+    }();
     each<FM>([&](auto I) __attribute__((always_inline)) {
         constexpr int i = decltype(I)::value;
         const typename Out<FN, FORM, EXTRAS>::Residual now = r;
         if (i + 1 < FM) r = out.residual(a, i + 1);
         f32x4 z[FN];
-#pragma unroll
-        for (int j = 0; j < FN; j++) z[j] = take(acc[i][j]);
         if constexpr (INT8) {
             const float x_scale = scales.row(i, own);
+            each<FN>([&](auto J) __attribute__((always_inline)) { z[decltype(J)::value] = scales.values(acc_take<4 * (i * FN + decltype(J)::value)>(), x_scale, channels, decltype(J)::value); });
+        } else {
 #pragma unroll
-            for (int j = 0; j < FN; j++) z[j] = scales.values(z[j], x_scale, j);
+            for (int j = 0; j < FN; j++) z[j] = take(acc[i][j]);
         }
         out.row(a, i, z, now, own);
         __builtin_amdgcn_sched_barrier(0);
@@ -505,8 +606,9 @@ __global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a, TileMap t
             for (int j = 0; j < FN; j++) sums[j] += __builtin_bit_cast(i32x4, from[j * 64]);
         }
         const float x_scale = scales.row(0, lane);
+        const typename Scales<1, FN, true>::Channels channels = scales.channels(lane);
 #pragma unroll
-        for (int j = 0; j < FN; j++) acc[j] = scales.values(__builtin_bit_cast(f32x4, sums[j]), x_scale, j);
+        for (int j = 0; j < FN; j++) acc[j] = scales.values(__builtin_bit_cast(f32x4, sums[j]), x_scale, channels, j);
         out.row(a, i, acc, res, lane);
         return;
     }

@@ -15,7 +15,7 @@ int main() {
         const unsigned K = codes / 2;
         printf("%u", !linear_few8(M, N, codes) ? 0u : M == 1u ? 1u : few_blocks8(M, N, codes) + (M > 16u ? 2u : 0u) + 2u);
         for (int act = 0; act < 2; act++) {
-            const LinearPlan p = plan_linear(M, N, K, act ? LINEAR_TILE8_ACT : LINEAR_TILE8);
+            const LinearPlan p = plan_linear8(M, N, K, act != 0);
             const TileMap map = make_tile_map(p);
             const unsigned blocks = p.whole + p.rest * p.parts, tiles = p.tiles_m * p.tiles_n;
             bool ok = blocks > 0 && blocks < LINEAR_GRID && p.whole + p.rest == tiles && (uint64_t)p.tiles_m * LINEAR_TILE[p.shape].m >= M && (uint64_t)p.tiles_n * LINEAR_TILE[p.shape].n >= N;

@@ -28,7 +28,7 @@ def _check(x, w, bias, residual, act, got):
 SIZES = [(1, 16, 8), (1, 5120, 40), (1, 1536, 4104), (2, 64, 128), (3, 80, 136), (5, 5120, 520), (16, 1008, 96), (17, 256, 72), (31, 528, 4104), (32, 5120, 264), (33, 144, 520), (64, 64, 64), (65, 208, 264),
          (100, 1536, 128), (127, 128, 8), (128, 128, 128), (129, 32, 384), (257, 272, 256), (390, 1008, 1000), (600, 2064, 232), (1025, 80, 520), (6566, 4112, 536), (528, 8016, 3616), (70001, 64, 72),
          (512, 256, 512), (1, 131056, 8), (40, 131056, 72), (923, 64, 4464), (6764, 4800, 80), (3650, 1920, 1248), (636, 5696, 4792), (7004, 64, 1392), (3726, 5696, 688),
-         (1124, 4592, 3632), (5616, 4992, 728), (48, 1408, 88), (9, 64, 264), (20, 528, 4104), (3, 4112, 4104)]
+         (1124, 4592, 3632), (5616, 4992, 728), (48, 1408, 88), (9, 64, 264), (20, 528, 4104), (3, 4112, 4104), (5535, 5696, 72), (1187, 7488, 3488), (10505, 288, 1200), (3046, 624, 4312), (48, 1568, 80)]
 
 
 @pytest.mark.parametrize("act", ["none", "gelu_tanh", "silu"])

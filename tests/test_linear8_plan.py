@@ -43,7 +43,7 @@ def test_every_part_of_every_tile_once(plans):
             continue
         for tm, tn, parts in cuts:
             tiles = -(-m // tm) * -(-n // tn)
-            slots = 256 * {(256, 256): 1, (128, 128): 2, (64, 64): 4, (128, 256): 1}[tm, tn]
+            slots = 256 * {(256, 256): 1, (128, 128): 2, (64, 64): 4}[tm, tn]
             assert space >= (tiles % slots * parts * tm * tn * 4 if parts > 1 else 0)
 
 
@@ -51,5 +51,4 @@ def test_the_gpu_tests_reach_every_kernel(plans):
     got = plans(test_gpu_linear_int8.SIZES)
     assert {few for few, *_ in got} == {0, 1, 3, 4, 5, 6}
     reached = [{(tm, tn, parts > 1) for few, *cuts in got if not few for tm, tn, parts in (cuts[act],)} for act in (0, 1)]
-    every = {(m, n, cut) for m, n in ((256, 256), (128, 128), (64, 64), (128, 256)) for cut in (False, True)}
-    assert reached[0] | reached[1] == every, every - (reached[0] | reached[1])
+    assert reached[0] == reached[1] == {(n, n, cut) for n in (256, 128, 64) for cut in (False, True)}

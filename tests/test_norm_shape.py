@@ -74,13 +74,25 @@ def test_accumulators_of_the_8_bit_products(tmp_path):
     flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "--cuda-device-only", "-S"]
     subprocess.run([HIPCC, *flags, os.path.join(CSRC, "linear_int8.hip"), "-o", out], check=True, stderr=subprocess.PIPE)
     kernels = re.findall(r"^(_ZN8skiparse13linear_kernel\w+):(.*?)\.Lfunc_end", open(out).read(), re.S | re.M)
-    assert len(kernels) == 8
-    registers = lambda x: {(m[0], i) for m in re.findall(r"\b([va])\[(\d+):(\d+)\]", x) for i in range(int(m[1]), int(m[2]) + 1)} | set((a, int(n)) for a, n in re.findall(r"\b([va])(\d+)\b", x))  # noqa: E731
+    assert len(kernels) == 6
+    number = r"(0x[0-9a-f]+|\d+)"
+
+    def registers(x):  # v[8:11], a[0x41], a7
+        found = {(kind, int(n, 0)) for kind, n in re.findall(r"\b([va])(\d+)\b", x)}
+        for kind, first, last in re.findall(r"\b([va])\[" + number + "(?::" + number + r")?\]", x):
+            found |= {(kind, i) for i in range(int(first, 0), int(last or first, 0) + 1)}
+        return found
+
     for name, body in kernels:
         lines = [x.split(";")[0].strip() for x in body.split("\n")]
         lines = [x for x in lines if x and (not x.startswith(".") or x.startswith(".LBB"))]
         label = {x.rstrip(":"): i for i, x in enumerate(lines) if x.startswith(".LBB")}
         products = [i for i, x in enumerate(lines) if x.startswith("v_mfma_i32_16x16x64_i8")]
+        tile = int(re.search(r"ILi(\d+)ELi", name).group(1)) * int(re.search(r"ELi(\d+)ELi3E", name).group(1))
+        # the accumulators are the program's: cleared once, read in both ways out, and the compiler has no use for them
+        moved = [x for x in lines if x.startswith("v_accvgpr")]
+        mine = [x for x in moved if all(i < tile // 256 for kind, i in registers(x) if kind == "a")]
+        assert sum(x.startswith("v_accvgpr_write") for x in mine) == tile // 256 and sum(x.startswith("v_accvgpr_read") for x in mine) == 2 * tile // 256 and not any("mov" in x for x in mine), name
         assert len(products) > 4 and not any(x.startswith("v_mfma") and i not in products for i, x in enumerate(lines))
         # from behind every product along all ways: other products, or the wait first
         seen, todo = set(), [i + 1 for i in products]
@@ -99,6 +111,7 @@ def test_accumulators_of_the_8_bit_products(tmp_path):
                 todo.append(label[m.group(1)])
             if not x.startswith("s_branch"):
                 todo.append(i + 1)
+        assert set().union(*(registers(lines[i].split(None, 1)[1].split(",")[0]) for i in products)) == {("a", i) for i in range(tile // 256)}
         for i in products:
             reads = set().union(*(registers(a) for a in lines[i].split(None, 1)[1].split(",")[1:]))
             for x in lines[max(0, i - 2):i]:
