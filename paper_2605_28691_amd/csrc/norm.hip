@@ -156,6 +156,8 @@ __device__ inline float into_range(float squares) { return squares <= 1.f ? 0x1p
 // 1 / sqrt(mean + eps), of values times `by` if that is not 1
 __device__ inline float inverse_size(float squares, float per_n, float eps, float by = 1.f) { return 1.f / sqrtf(squares * per_n + eps * by * by); }
 
+__device__ inline float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+
 __device__ inline uint32_t source_of(int order, const RowArgs& rows, uint32_t row) {
     return order == 1 ? source_row<TO_SPARSE>(rows, row, 0u) : order == 2 ? source_row<TO_ORIGINAL>(rows, row, 0u) : row;
 }
@@ -372,18 +374,25 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : NORM_BWD_THR
         row_sums<SPAN, CH, 2>(parts, sum, lanes, a.chunks, sums[turn & 1u]);
         turn++;
         float r = inverse_size(sum[0], a.per_n, a.eps), mean = sum[1] * a.per_n * r;
-        const bool bad = on && out_of_range(sum[0], a.per_n, a.eps);
+        // g h may be beyond float32's range where g u is not: g times 2^-80 then
+        const bool far = out_of_range(sum[0], a.per_n, a.eps), high = !(fabsf(sum[1]) <= 3.4028234663852886e38f), bad = on && (far || high);
         if (__builtin_expect(SPAN == SPAN_GROUP ? bad : __builtin_amdgcn_ballot_w64(bad) != 0, 0)) {
-            const float by = into_range(sum[0]);
+            float by = far ? into_range(sum[0]) : 1.f, down = high ? 0x1p-80f : 1.f;
+            if (SPAN == SPAN_GROUP) {  // the workgroup's: not in vector registers
+                by = uniform(by);
+                down = uniform(down);
+            }
 #pragma unroll
             for (int i = 0; i < CH; i++) {
                 parts[0][i] = parts[1][i] = 0.f;
                 if (LEAN) weight(i);
 #pragma unroll
+                for (int u = 0; u < (CH > 1 ? Piece<T>::UNITS : 0); u++) asm volatile("" : "+v"(hc[i].raw[u]), "+v"(yc[i].raw[u]));  // formed here once more, not kept for rows that need none of it
+#pragma unroll
                 for (int e = 0; e < 8; e++) {
                     const float h = hc[i].get(e) * by;
                     parts[0][i] = fmaf(h, h, parts[0][i]);
-                    parts[1][i] = fmaf(yc[i].get(e) * w[i].get(e), h, parts[1][i]);
+                    parts[1][i] = fmaf(yc[i].get(e) * w[i].get(e) * down, h, parts[1][i]);
                 }
             }
             if (SPAN == SPAN_GROUP) __syncthreads();  // the last such row's have been read
@@ -392,6 +401,7 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : NORM_BWD_THR
                 const float s = inverse_size(sum[0], a.per_n, a.eps, by);
                 r = by * s;
                 mean = sum[1] * a.per_n * s;
+                mean *= 1.f / down;
             }
         }
         if (LEAN) {

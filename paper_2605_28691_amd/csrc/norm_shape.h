@@ -43,8 +43,8 @@ struct NormBwdShape {
     uint32_t lanes, threads, parts;
 };
 // Parts: enough wavefronts for the chip, and no more, since a part's sums are written and read once more; few rows in few parts.  (us, 256 / 512 / 768 / 1024 parts: 32,760 x 1536, 3 wavefronts a row, 119 / 85 / 83 / 82;
-// 3840 x 5120, 10 wavefronts, 38 / 41 / 41 / 44; 390 x 1536 7.4 / 8.3 / 8.3 / 8.3; 80,640 x 1024, a wavefront a row and 4 in a workgroup, 128 / 136 / 138 / 143.)  Rows of more than 16,384 channels do not fit the
-// registers with all that the pass keeps: 4000 x 32,768 345 us in bf16, 495 in float32, floors 210 and 420.
+// 3840 x 5120, 10 wavefronts, 38 / 41 / 41 / 44; 390 x 1536 7.4 / 8.3 / 8.3 / 8.3; 80,640 x 1024, a wavefront a row and 4 in a workgroup, 128 / 136 / 138 / 143.)  Rows of more than 16,384 channels in float32 do
+// not fit the registers with all that the pass keeps: 4000 x 32,768 507 us, floor 420 (bf16 245, 210).
 inline NormBwdShape norm_bwd_shape(uint32_t rows, uint32_t cols) {
     const uint32_t pieces = (cols + 7u) / 8u, per_lane = (pieces + 63u) / 64u;
     NormBwdShape s;

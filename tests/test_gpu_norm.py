@@ -212,6 +212,26 @@ def test_rows_far_from_one(cols):
             nr.close(dw, ew, nr.F32 * ew.abs() + bw, "dw")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [40, 1000, 1536, 20480])
+def test_gradients_far_from_one(cols, dtype):
+    """Products of dy and h beyond float32's range, whose gradients are in it; rows between them are as they are alone."""
+    import paper_2605_28691_amd as sk
+
+    g = _gen(cols)
+    h, dy = (torch.randn(9, cols, generator=g, device="cuda") for _ in range(2))
+    sizes = [(0, 0), (62, 100), (50, 120), (90, 60), (-70, 20), (100, 110), (20, 122), (0, 0), (61, -100)]
+    h = (h * torch.tensor([2.0 ** a for a, _ in sizes], device="cuda")[:, None]).to(dtype)
+    dy = (dy * torch.tensor([2.0 ** b for _, b in sizes], device="cuda")[:, None]).to(dtype)
+    w = _weight(g, cols, dtype)
+    dx, dw = sk.skiparse_rmsnorm_bwd(dy, h, w)
+    ex, ew, bx, bw = nr.norm_grads(dy, h, w, None, EPS)
+    nr.close(dx, ex, (nr.ROUND[dtype] + 2 * nr.F32) * ex.abs() + bx + 2.0 ** (-149 if dtype is torch.float32 else -134), "dx")
+    nr.close(dw, ew, nr.ROUND[dtype] * ew.abs() + bw, "dw")
+    for i in (0, 3, 7):
+        assert torch.equal(dx[i:i + 1], sk.skiparse_rmsnorm_bwd(dy[i:i + 1].clone(), h[i:i + 1].clone(), w)[0]), i
+
+
 @pytest.mark.parametrize("cols", [24, 520, 5120])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_rows_that_are_not_finite(cols, dtype):
