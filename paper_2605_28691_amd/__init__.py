@@ -251,6 +251,19 @@ for _name in _TENSORS:
     globals()["_" + _name] = functools.partial(_general, _name)
 
 
+# Calls as a whole, natively: they answer NotImplemented to all but plain arguments, and before the module is there.
+_PLAIN = ("rmsnorm_fwd", "rmsnorm_bwd", "quantize_int8", "linear_fwd_int8")
+_PLAIN_SIZES = ("skiparse_rmsnorm_bwd_workspace_bytes", "skiparse_linear_fwd_int8_workspace_bytes")
+
+
+def _not_plain(*args):
+    return NotImplemented
+
+
+for _name in _PLAIN:
+    globals()["_plain_" + _name] = _not_plain
+
+
 def _torch_build() -> str:
     """Which torch this is: the module reads tensors by the layout in the headers that it was built with."""
     return f"{torch.__version__} {torch.version.git_version}"
@@ -270,6 +283,10 @@ def _bind(L: ctypes.CDLL) -> None:
         for name in _TENSORS:
             native.bind(name, ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
             globals()["_" + name] = getattr(native, name)
+        for name in _PLAIN_SIZES:
+            native.bind(name, ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
+        for name in _PLAIN:
+            globals()["_plain_" + name] = getattr(native, "plain_" + name)
     _marshal = native
 
 
@@ -782,12 +799,21 @@ def skiparse_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, re
     """h / sqrt(mean(h^2) + eps) * weight over the last dimension, h = x + residual: the result, or with a residual (result, h).  bf16 or float32, all of one type; h is rounded to it, the result made
     of what it is before that.  quantize=True: the result as Quantized, for skiparse_linear_fwd_int8.  order "to_sparse" or "to_original" moves the rows of the grid T x H x W on the way: x, residual and h
     are [B][T*H*W][channels] or [s*s*B][T*H*W/(s*s)][channels], the result the other; h stays where x is.  `out` and `total` (of h; may be residual or x) are buffers to use; out may be x where rows stay."""
+    p = PATTERNS[pattern]
+    if order == "same":
+        place = None
+    else:
+        grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
+        place = (*lead, *grid, s, p, ORDERS[order])
+    if out is None and total is None:
+        done = _plain_rmsnorm_fwd(x, weight, residual, eps, quantize, Quantized, place, _get_device, _raw_stream)
+        if done is not NotImplemented:
+            return done
     at = x.shape
     cols = at[-1]
-    if order == "same":
+    if place is None:
         grid, shape = (1, 1, 1, x.numel() // max(cols, 1)), at
     else:
-        grid, lead = _linear_rows(at[:-1], order, T, H, W, s)
         shape = (*lead, cols)
     _of_channels(weight, cols)
     _same_type(x, weight, residual)
@@ -803,7 +829,7 @@ def skiparse_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, re
     elif total is not None:
         raise ValueError("without a residual the sum is x")
     _here(x, weight, residual, total, codes, scales)
-    _skiparse_rmsnorm_fwd(x, residual, weight, total, codes, scales, *grid, cols, float(eps), s, PATTERNS[pattern], ORDERS[order], _DTYPES[x.dtype], _stream())
+    _skiparse_rmsnorm_fwd(x, residual, weight, total, codes, scales, *grid, cols, float(eps), s, p, ORDERS[order], _DTYPES[x.dtype], _stream())
     return out if residual is None else (out, total)
 
 
@@ -818,6 +844,11 @@ def skiparse_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor
     dx is the gradient of x and of the residual, with dx_add, what comes along the residual stream, added to it; dx_add may be dx."""
     if not (need_dx or need_dw):
         return None, None
+    p = PATTERNS[pattern]
+    if order == "same" and dx is None and dw is None and workspace is None:
+        done = _plain_rmsnorm_bwd(dy, h, weight, dx_add, eps, need_dx, need_dw, _get_device, _raw_stream)
+        if done is not NotImplemented:
+            return done
     cols = h.shape[-1]
     grid, back = _linear_rows(dy.shape[:-1], _BACK[order], T, H, W, s)
     if dy.shape[-1] != cols or tuple(h.shape) != (*back, cols) or (dx_add is not None and dx_add.shape != h.shape):
@@ -832,23 +863,32 @@ def skiparse_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor
         workspace, size = _space(workspace, h, "skiparse_rmsnorm_bwd_workspace_bytes", grid[0] * grid[1] * grid[2] * grid[3], cols)
     else:
         workspace = None
-    _skiparse_rmsnorm_bwd(dy, h, weight, dx_add, dx, dw, *grid, cols, float(eps), s, PATTERNS[pattern], ORDERS[order], _DTYPES[h.dtype], workspace, size, _stream())
+    _skiparse_rmsnorm_bwd(dy, h, weight, dx_add, dx, dw, *grid, cols, float(eps), s, p, ORDERS[order], _DTYPES[h.dtype], workspace, size, _stream())
     return dx, dw
 
 
 def skiparse_quantize_int8(x: torch.Tensor, order: str = "same", T: int = 0, H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", out: Quantized | None = None) -> Quantized:
     """[..., channels] in bf16 or float32 -> int8 codes and a float32 scale a row: activations in front of skiparse_linear_fwd_int8, or once its weights [out, in].  order moves rows on the way, as in
     skiparse_rmsnorm_fwd."""
+    p = PATTERNS[pattern]
+    if order == "same":
+        place = None
+    else:
+        grid, lead = _linear_rows(x.shape[:-1], order, T, H, W, s)
+        place = (*lead, *grid, s, p, ORDERS[order])
+    if out is None:
+        done = _plain_quantize_int8(x, Quantized, place, _get_device, _raw_stream)
+        if done is not NotImplemented:
+            return done
     shape = x.shape
     cols = shape[-1]
-    if order == "same":
+    if place is None:
         grid = (1, 1, 1, x.numel() // max(cols, 1))
     else:
-        grid, lead = _linear_rows(shape[:-1], order, T, H, W, s)
         shape = (*lead, cols)
     codes, scales = out = _quantized_of(shape, x) if out is None else _is_quantized(out, "out", shape)
     _here(x, codes, scales)
-    _skiparse_quantize_int8(x, codes, scales, *grid, cols, s, PATTERNS[pattern], ORDERS[order], _DTYPES[x.dtype], _stream())
+    _skiparse_quantize_int8(x, codes, scales, *grid, cols, s, p, ORDERS[order], _DTYPES[x.dtype], _stream())
     return out
 
 
@@ -860,6 +900,14 @@ def skiparse_linear_fwd_int8(x: Quantized, w: Quantized, bias: torch.Tensor | No
                              H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """act(x w^T + bias) + residual in bf16 from 8-bit integers: x [..., in] and w [out, in] as skiparse_quantize_int8 or skiparse_rmsnorm_fwd leave them, bias [out], residual and result
     [..., out] bf16.  order as in skiparse_linear_fwd; the scales' rows move with the codes'.  `out` (may be residual) and `workspace` are buffers to use."""
+    p, a, place = PATTERNS[pattern], ACTS[act], None
+    if out is None and workspace is None:
+        if order != "same" and type(x) is Quantized:
+            grid, lead = _linear_rows(x.codes.shape[:-1], order, T, H, W, s)
+            place = (*lead, *grid, s, p, ORDERS[order])
+        done = _plain_linear_fwd_int8(x, w, bias, residual, a, Quantized, place, _get_device, _raw_stream)
+        if done is not NotImplemented:
+            return done
     _is_quantized(x, "x")
     _is_quantized(w, "w")
     xc, xs = x
@@ -877,5 +925,5 @@ def skiparse_linear_fwd_int8(x: Quantized, w: Quantized, bias: torch.Tensor | No
         raise ValueError(f"residual must have the result's shape {shape}")
     _here(xc, xs, wc, ws, bias, residual, out, workspace)
     workspace, size = _space(workspace, xc, "skiparse_linear_fwd_int8_workspace_bytes", grid[0] * grid[1] * grid[2] * grid[3], K, N)
-    _skiparse_linear_fwd_int8(xc, xs, wc, ws, bias, residual, out, *grid, K, N, s, PATTERNS[pattern], ORDERS[order], ACTS[act], workspace, size, _stream())
+    _skiparse_linear_fwd_int8(xc, xs, wc, ws, bias, residual, out, *grid, K, N, s, p, ORDERS[order], a, workspace, size, _stream())
     return out

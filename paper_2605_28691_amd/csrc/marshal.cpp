@@ -12,8 +12,11 @@
 // The module is not linked to the library: the binding hands it the addresses in the copy that it has opened itself, so that a process that
 // rebuilds the library calls one copy only.
 #include <Python.h>
+#include <ATen/DimVector.h>
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <climits>
 #include <cstring>
 #include <tuple>
 #include <utility>
@@ -197,6 +200,232 @@ constexpr unsigned at(int i, I... more) { return 1u << i | at(more...); }
 ENTRIES(SLOT)
 ENTRIES(ENTRY)
 
+// ---- whole calls
+//
+// A norm of one row, its codes or its projection is a kernel of 2 to 7 us behind 8 of host work, of which the launch takes 3.5 and the results' tensors 2.5 from Python.  So these calls are here once more as a
+// whole: their checks, their results' tensors and the C function.  (us a call on the host, by way of Python / so: norm with residual 7.7 / 5.2, rows in codes 8.1 / 5.4, a token's projection 8.0 / 4.4.)  plain_x(...) answers NotImplemented to anything but plain arguments that fit each other, and the binding goes on as if it had not asked: what
+// is refused, and with which words, is decided there.  PLACE: None where rows stay, else (leading dimensions of the result, B, T, H, W, s, pattern, order).
+
+decltype(&::skiparse_linear_fwd_int8_workspace_bytes) g_linear8_bytes = nullptr;
+decltype(&::skiparse_rmsnorm_bwd_workspace_bytes) g_norm_bwd_bytes = nullptr;
+
+struct Place {
+    int64_t lead[2] = {0, 0};
+    int B = 1, T = 1, H = 1, W = 0, s = 1, pattern = 0, order = 0;
+    bool moved = false;
+    bool get(PyObject* o, int64_t rows) {
+        if (o == Py_None) {
+            W = (int)rows;
+            return rows >= 1 && W == rows;
+        }
+        int l[2];
+        moved = true;
+        if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 9) return false;
+        int* const to[9] = {&l[0], &l[1], &B, &T, &H, &W, &s, &pattern, &order};
+        for (int i = 0; i < 9; i++)
+            if (!Arg<int>::get(PyTuple_GET_ITEM(o, i), *to[i])) return false;
+        lead[0] = l[0];
+        lead[1] = l[1];
+        return true;
+    }
+    // of a result with `cols` channels, made of rows as those of `x`
+    at::DimVector shape(const at::Tensor& x, int64_t cols, bool scales = false) const {
+        at::DimVector d;
+        if (moved) d.append(lead, lead + 2);
+        else d.append(x.sizes().begin(), x.sizes().end() - 1);
+        if (!scales) d.push_back(cols);
+        return d;
+    }
+};
+
+struct Here {
+    int device;
+    void* stream;
+    // the current device, which is a number, and its stream's handle
+    bool get(PyObject* get_device, PyObject* raw_stream) {
+        if (get_device == Py_None || raw_stream == Py_None) return false;
+        PyObject* d = PyObject_CallNoArgs(get_device);
+        PyObject* h = d != nullptr ? PyObject_CallOneArg(raw_stream, d) : nullptr;
+        const bool ok = h != nullptr && PyLong_CheckExact(d) && PyLong_CheckExact(h);
+        if (ok) {
+            device = (int)PyLong_AsLong(d);
+            stream = (void*)(uintptr_t)PyLong_AsUnsignedLongLongMask(h);
+        }
+        Py_XDECREF(d);
+        Py_XDECREF(h);
+        PyErr_Clear();
+        return ok;
+    }
+};
+
+const at::Tensor* tensor_of(PyObject* o) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.is_contiguous() ? &t : nullptr;
+}
+// like `x` in type and device; null for None
+bool also(PyObject* o, const at::Tensor& x, const at::Tensor*& t, at::ScalarType type) {
+    t = nullptr;
+    if (o == Py_None) return true;
+    t = tensor_of(o);
+    return t != nullptr && t->scalar_type() == type && t->get_device() == x.get_device();
+}
+bool of_channels(const at::Tensor* t, int64_t cols) { return t == nullptr || (t->dim() == 1 && t->size(0) == cols); }
+void* pointer(const at::Tensor* t) { return t != nullptr ? t->data_ptr() : nullptr; }
+int elements(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 ? SKIPARSE_BF16 : t.scalar_type() == at::kFloat ? SKIPARSE_FP32 : -1; }
+// (codes, scales) as the binding's class of these
+PyObject* quantized(PyObject* type, at::Tensor&& codes, at::Tensor&& scales) {
+    PyObject* two = PyTuple_New(2);
+    if (two == nullptr) return nullptr;
+    PyTuple_SET_ITEM(two, 0, THPVariable_Wrap(std::move(codes)));
+    PyTuple_SET_ITEM(two, 1, THPVariable_Wrap(std::move(scales)));
+    PyObject* args = PyTuple_Pack(1, two);
+    PyObject* q = args != nullptr ? PyTuple_Type.tp_new((PyTypeObject*)type, args, nullptr) : nullptr;
+    Py_XDECREF(args);
+    Py_DECREF(two);
+    return q;
+}
+bool quantized_of(PyObject* o, PyObject* type, const at::Tensor*& codes, const at::Tensor*& scales) {
+    if ((PyObject*)Py_TYPE(o) != type || PyTuple_GET_SIZE(o) != 2) return false;
+    codes = tensor_of(PyTuple_GET_ITEM(o, 0));
+    scales = tensor_of(PyTuple_GET_ITEM(o, 1));
+    return codes != nullptr && scales != nullptr && codes->scalar_type() == at::kChar && scales->scalar_type() == at::kFloat && codes->dim() >= 1 &&
+           scales->sizes() == codes->sizes().slice(0, codes->dim() - 1) && codes->get_device() == scales->get_device();
+}
+bool is_class(PyObject* type) { return PyType_Check(type) && PyType_IsSubtype((PyTypeObject*)type, &PyTuple_Type); }
+bool yes_or_no(PyObject* o, bool& v) {
+    v = o == Py_True;
+    return v || o == Py_False;
+}
+PyObject* not_plain() {
+    Py_INCREF(Py_NotImplemented);
+    return Py_NotImplemented;
+}
+PyObject* raised(int code, const char* name) { return PyObject_CallFunction(g_failed, "is", code, name); }
+
+// x, weight, residual, eps, quantize, Quantized, PLACE, device and stream functions -> result, or (result, sum)
+PyObject* rmsnorm_fwd_of(PyObject* const* a) {
+    const at::Tensor *x = tensor_of(a[0]), *w, *r;
+    bool quantize;
+    if (x == nullptr || x->dim() < 1 || x->numel() < 1 || !PyFloat_CheckExact(a[3]) || !yes_or_no(a[4], quantize) || !is_class(a[5])) return not_plain();
+    const int type = elements(*x);
+    const int64_t cols = x->size(-1);
+    Place place;
+    Here here;
+    if (type < 0 || cols != (int)cols || !also(a[1], *x, w, x->scalar_type()) || !of_channels(w, cols) || !also(a[2], *x, r, x->scalar_type()) || (r != nullptr && r->sizes() != x->sizes()) ||
+        !place.get(a[6], x->numel() / cols) || !here.get(a[7], a[8]) || here.device != x->get_device())
+        return not_plain();
+    at::Tensor scales, sum, out = at::empty(place.shape(*x, cols), quantize ? x->options().dtype(at::kChar) : x->options());
+    if (quantize) scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
+    if (r != nullptr) sum = at::empty(x->sizes(), x->options());
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = g_skiparse_rmsnorm_fwd(x->data_ptr(), pointer(r), pointer(w), r != nullptr ? sum.data_ptr() : nullptr, out.data_ptr(), quantize ? (float*)scales.data_ptr() : nullptr, place.B, place.T, place.H,
+                                  place.W, (int)cols, (float)PyFloat_AS_DOUBLE(a[3]), place.s, place.pattern, place.order, type, here.stream);
+    Py_END_ALLOW_THREADS
+    if (code != SKIPARSE_OK) return raised(code, "skiparse_rmsnorm_fwd");
+    PyObject* result = quantize ? quantized(a[5], std::move(out), std::move(scales)) : THPVariable_Wrap(std::move(out));
+    if (result == nullptr || r == nullptr) return result;
+    PyObject* both = PyTuple_New(2);
+    if (both == nullptr) return nullptr;
+    PyTuple_SET_ITEM(both, 0, result);
+    PyTuple_SET_ITEM(both, 1, THPVariable_Wrap(std::move(sum)));
+    return both;
+}
+
+// x, Quantized, PLACE, device and stream functions
+PyObject* quantize_int8_of(PyObject* const* a) {
+    const at::Tensor* x = tensor_of(a[0]);
+    if (x == nullptr || x->dim() < 1 || x->numel() < 1 || !is_class(a[1])) return not_plain();
+    const int type = elements(*x);
+    const int64_t cols = x->size(-1);
+    Place place;
+    Here here;
+    if (type < 0 || cols != (int)cols || !place.get(a[2], x->numel() / cols) || !here.get(a[3], a[4]) || here.device != x->get_device()) return not_plain();
+    at::Tensor codes = at::empty(place.shape(*x, cols), x->options().dtype(at::kChar)), scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = g_skiparse_quantize_int8(x->data_ptr(), codes.data_ptr(), (float*)scales.data_ptr(), place.B, place.T, place.H, place.W, (int)cols, place.s, place.pattern, place.order, type, here.stream);
+    Py_END_ALLOW_THREADS
+    return code != SKIPARSE_OK ? raised(code, "skiparse_quantize_int8") : quantized(a[1], std::move(codes), std::move(scales));
+}
+
+// x, w, bias, residual, activation, Quantized, PLACE, device and stream functions
+PyObject* linear_fwd_int8_of(PyObject* const* a) {
+    const at::Tensor *x, *xs, *w, *ws, *bias, *residual;
+    int act;
+    if (!quantized_of(a[0], a[5], x, xs) || !quantized_of(a[1], a[5], w, ws) || x->numel() < 1 || w->dim() != 2 || w->get_device() != x->get_device() || !Arg<int>::get(a[4], act)) return not_plain();
+    const int64_t K = x->size(-1), N = w->size(0);
+    Place place;
+    Here here;
+    if (w->size(1) != K || K != (int)K || N != (int)N || N < 1 || !also(a[2], *x, bias, at::kBFloat16) || !of_channels(bias, N) || !also(a[3], *x, residual, at::kBFloat16) ||
+        !place.get(a[6], x->numel() / K) || x->numel() / K > INT_MAX || !here.get(a[7], a[8]) || here.device != x->get_device())
+        return not_plain();
+    const at::DimVector shape = place.shape(*x, N);
+    if (residual != nullptr && residual->sizes() != at::IntArrayRef(shape)) return not_plain();
+    const size_t need = g_linear8_bytes((int)(x->numel() / K), (int)K, (int)N);
+    at::Tensor space, out = at::empty(shape, x->options().dtype(at::kBFloat16));
+    if (need) space = at::empty({(int64_t)need}, x->options().dtype(at::kByte));
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = g_skiparse_linear_fwd_int8(x->data_ptr(), (const float*)xs->data_ptr(), w->data_ptr(), (const float*)ws->data_ptr(), pointer(bias), pointer(residual), out.data_ptr(), place.B, place.T, place.H, place.W,
+                                      (int)K, (int)N, place.s, place.pattern, place.order, act, need ? space.data_ptr() : nullptr, need, here.stream);
+    Py_END_ALLOW_THREADS
+    return code != SKIPARSE_OK ? raised(code, "skiparse_linear_fwd_int8") : THPVariable_Wrap(std::move(out));
+}
+
+// dy, h, weight, dx_add, eps, need_dx, need_dw, device and stream functions; rows stay -> (dx, dw)
+PyObject* rmsnorm_bwd_of(PyObject* const* a) {
+    const at::Tensor *dy = tensor_of(a[0]), *h, *w, *add;
+    bool need_dx, need_dw;
+    if (dy == nullptr || dy->dim() < 1 || dy->numel() < 1 || !PyFloat_CheckExact(a[4]) || !yes_or_no(a[5], need_dx) || !yes_or_no(a[6], need_dw)) return not_plain();
+    const int type = elements(*dy);
+    const int64_t cols = dy->size(-1);
+    Place place;
+    Here here;
+    if (type < 0 || cols != (int)cols || !also(a[1], *dy, h, dy->scalar_type()) || h == nullptr || h->sizes() != dy->sizes() || !also(a[2], *dy, w, dy->scalar_type()) || !of_channels(w, cols) ||
+        !also(a[3], *dy, add, dy->scalar_type()) || (add != nullptr && add->sizes() != dy->sizes()) || !place.get(Py_None, dy->numel() / cols) || !here.get(a[7], a[8]) || here.device != dy->get_device())
+        return not_plain();
+    at::Tensor dx, dw, space;
+    const size_t need = need_dw ? g_norm_bwd_bytes(place.W, (int)cols) : 0;
+    if (need_dx) dx = at::empty(h->sizes(), h->options());
+    if (need_dw) dw = at::empty({cols}, h->options());
+    if (need) space = at::empty({(int64_t)need}, h->options().dtype(at::kByte));
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = g_skiparse_rmsnorm_bwd(dy->data_ptr(), h->data_ptr(), pointer(w), pointer(add), need_dx ? dx.data_ptr() : nullptr, need_dw ? dw.data_ptr() : nullptr, 1, 1, 1, place.W, (int)cols,
+                                  (float)PyFloat_AS_DOUBLE(a[4]), 1, 0, 0, type, need ? space.data_ptr() : nullptr, need, here.stream);
+    Py_END_ALLOW_THREADS
+    if (code != SKIPARSE_OK) return raised(code, "skiparse_rmsnorm_bwd");
+    PyObject* both = PyTuple_New(2);
+    if (both == nullptr) return nullptr;
+    for (int i = 0; i < 2; i++) {
+        if (i ? need_dw : need_dx) {
+            PyTuple_SET_ITEM(both, i, THPVariable_Wrap(i ? std::move(dw) : std::move(dx)));
+        } else {
+            Py_INCREF(Py_None);
+            PyTuple_SET_ITEM(both, i, Py_None);
+        }
+    }
+    return both;
+}
+
+// An exception from within (no memory for a result): the binding comes upon it by itself.
+#define PLAIN(name, count, bound)                                                \
+    PyObject* plain_##name(PyObject*, PyObject* const* args, Py_ssize_t n) {     \
+        if (n != count || !(bound) || g_failed == nullptr) return not_plain();   \
+        try {                                                                    \
+            return name##_of(args);                                              \
+        } catch (...) {                                                          \
+            PyErr_Clear();                                                       \
+            return not_plain();                                                  \
+        }                                                                        \
+    }
+PLAIN(rmsnorm_fwd, 9, g_skiparse_rmsnorm_fwd)
+PLAIN(quantize_int8, 5, g_skiparse_quantize_int8)
+PLAIN(linear_fwd_int8, 9, g_skiparse_linear_fwd_int8 && g_linear8_bytes)
+PLAIN(rmsnorm_bwd, 9, g_skiparse_rmsnorm_bwd && g_norm_bwd_bytes)
+
 PyObject* set_up(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 2 || !PyCallable_Check(args[0]) || !PyCallable_Check(args[1])) {
         PyErr_SetString(PyExc_TypeError, "set_up(general, failed)");
@@ -220,10 +449,13 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
         return nullptr;
     }
     ENTRIES(BIND)
+    if (strcmp(what, "skiparse_linear_fwd_int8_workspace_bytes") == 0) g_linear8_bytes = (decltype(g_linear8_bytes))address;
+    if (strcmp(what, "skiparse_rmsnorm_bwd_workspace_bytes") == 0) g_norm_bwd_bytes = (decltype(g_norm_bwd_bytes))address;
     Py_RETURN_NONE;
 }
 
-PyMethodDef methods[] = {ENTRIES(LISTED){"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
+#define LISTED_PLAIN(name) {"plain_" #name, (PyCFunction)(void (*)(void))plain_##name, METH_FASTCALL, nullptr},
+PyMethodDef methods[] = {ENTRIES(LISTED) LISTED_PLAIN(rmsnorm_fwd) LISTED_PLAIN(quantize_int8) LISTED_PLAIN(linear_fwd_int8) LISTED_PLAIN(rmsnorm_bwd){"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
                          {"set_up", (PyCFunction)(void (*)(void))set_up, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Native marshalling of the binding's calls.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

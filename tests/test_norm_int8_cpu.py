@@ -118,3 +118,21 @@ def test_definition_of_codes():
     assert not codes[1].any() and scales[1] == 1 and not codes[2].any() and np.isnan(scales[2])
     assert codes[3].tolist()[:2] == [-127, 64] and float(scales[3]) == float(np.float32(2) / np.float32(127))  # 63.5 goes to the even code
     assert codes[4, 0] == 32 and float(scales[4]) == float(np.float32(2.0 ** -118) / np.float32(127))           # 31.75
+
+
+def test_whole_calls_answer_only_what_is_plain():
+    """On the CPU nothing is: the native module says so without a look at the device."""
+    native = sk._marshal
+    assert sk.lib() and native is not None and sk._plain_rmsnorm_fwd is native.plain_rmsnorm_fwd
+
+    def never(*args):
+        raise AssertionError("asked for the device")
+
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    q = sk.Quantized(x.to(torch.int8), torch.zeros(4))
+    for call, good in ((native.plain_rmsnorm_fwd, (x, None, None, 1e-6, False, sk.Quantized, None, never, never)), (native.plain_quantize_int8, (x, sk.Quantized, None, never, never)),
+                       (native.plain_linear_fwd_int8, (q, q, None, None, 0, sk.Quantized, None, never, never)), (native.plain_rmsnorm_bwd, (x, x, None, None, 1e-6, True, True, never, never))):
+        assert call(*good) is call(*good[:-1]) is call(*good, 1) is call() is NotImplemented
+        for i in range(len(good)):
+            for bad in (None, 5, 1.5, "x", (), (1,) * 9, [x], torch.zeros(2), sk.Quantized, object()):
+                assert call(*good[:i], bad, *good[i + 1:]) is NotImplemented
