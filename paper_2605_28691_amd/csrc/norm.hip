@@ -162,23 +162,20 @@ __device__ inline uint32_t source_of(int order, const RowArgs& rows, uint32_t ro
     return order == 1 ? source_row<TO_SPARSE>(rows, row, 0u) : order == 2 ? source_row<TO_ORIGINAL>(rows, row, 0u) : row;
 }
 
+// What a row's sums and largest value need of LDS.
+template <int SPAN, int CH>
+struct RowPlaces {
+    float sums[SPAN == SPAN_GROUP ? NORM_WAVES * CH : 1][1], again[SPAN == SPAN_GROUP ? NORM_WAVES * CH : 1][1];
+    uint32_t tops[SPAN == SPAN_GROUP ? NORM_WAVES : 1];
+};
+
+// A row, of whose tensors the lane's pieces are in x and other (residual).
 template <typename T, int KIND, int SPAN, int CH, bool NT>
-__global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : 256) void norm_rows_kernel(NormArgs a, uint32_t lanes) {
-    constexpr int PLACES = SPAN == SPAN_GROUP ? NORM_WAVES : 1, CHUNKS = SPAN == SPAN_GROUP ? NORM_WAVES * CH : 1;
-    __shared__ float sums[CHUNKS][1];
-    __shared__ float again[CHUNKS][1];
-    __shared__ uint32_t tops[PLACES];
-    const Place<T, SPAN, CH> at(lanes, a.cols);
-    const uint32_t row = a.first + blockIdx.x * at.rows(lanes) + at.row(lanes);
-    const bool on = row < a.n_rows;
-    if (SPAN == SPAN_WAVE && !on) return;
-    const uint32_t from = on ? source_of(a.order, a.rows, row) : 0u;
-    const size_t in = (size_t)from * a.cols, to = (size_t)row * a.cols;
-    float h[CH][8];
-    Piece<T> x[CH], other[CH];
-    at.template load<NT>(a.x, in, on, x);
+__device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a, const Place<T, SPAN, CH>& at, uint32_t lanes, uint32_t row, size_t in, bool on, const Piece<T> (&x)[CH], Piece<T> (&other)[CH],
+                                                               RowPlaces<SPAN, CH>& lds) {
     const bool adds = KIND != ROWS_QUANTIZED && a.residual != nullptr;
-    if (adds) at.template load<NT>(a.residual, in, on, other);
+    const size_t to = (size_t)row * a.cols;
+    float h[CH][8];
     float squares[1][CH];
 #pragma unroll
     for (int i = 0; i < CH; i++) {
@@ -199,7 +196,7 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : 256) void no
     float r = 1.f;
     if (KIND != ROWS_QUANTIZED) {
         float sum[1];
-        row_sums<SPAN, CH, 1>(squares, sum, lanes, a.chunks, sums);
+        row_sums<SPAN, CH, 1>(squares, sum, lanes, a.chunks, lds.sums);
         r = inverse_size(sum[0], a.per_n, a.eps);
         const bool bad = on && out_of_range(sum[0], a.per_n, a.eps);
         if (__builtin_expect(SPAN == SPAN_GROUP ? bad : __builtin_amdgcn_ballot_w64(bad) != 0, 0)) {  // all lanes of a wavefront go
@@ -210,7 +207,7 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : 256) void no
 #pragma unroll
                 for (int e = 0; e < 8; e++) squares[0][i] = fmaf(h[i][e] * by, h[i][e] * by, squares[0][i]);
             }
-            row_sums<SPAN, CH, 1>(squares, sum, lanes, a.chunks, again);
+            row_sums<SPAN, CH, 1>(squares, sum, lanes, a.chunks, lds.again);
             if (bad) r = by * inverse_size(sum[0], a.per_n, a.eps, by);
         }
     }
@@ -233,7 +230,7 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : 256) void no
         }
     }
     if (KIND == ROWS_NORM) return;
-    const Int8Row q(row_largest<SPAN>(top, lanes, tops), r);
+    const Int8Row q(row_largest<SPAN>(top, lanes, lds.tops), r);
 #pragma unroll
     for (int i = 0; i < CH; i++) {
         uint32_t codes[2], c;
@@ -251,15 +248,48 @@ __global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : 256) void no
     if (on && at.first == 0u) a.scales[row] = q.scale;
 }
 
+template <typename T, int KIND, int SPAN, int CH, bool NT>
+__global__ __launch_bounds__(SPAN == SPAN_GROUP ? 64 * NORM_WAVES : 256) void norm_rows_kernel(NormArgs a, uint32_t lanes) {
+    __shared__ RowPlaces<SPAN, CH> lds;
+    const Place<T, SPAN, CH> at(lanes, a.cols);
+    const uint32_t row = a.first + blockIdx.x * at.rows(lanes) + at.row(lanes);
+    const bool on = row < a.n_rows;
+    if (SPAN == SPAN_WAVE && !on) return;
+    const size_t in = on ? (size_t)source_of(a.order, a.rows, row) * a.cols : 0;
+    Piece<T> x[CH], other[CH];
+    at.template load<NT>(a.x, in, on, x);
+    if (KIND != ROWS_QUANTIZED && a.residual != nullptr) at.template load<NT>(a.residual, in, on, other);
+    norm_row<T, KIND, SPAN, CH, NT>(a, at, lanes, row, in, on, x, other, lds);
+}
+
+// The same for rows of a part of a wavefront without a residual, past the caches: the lanes have two rows, the second on its way while the first is worked on (norm_turns()).
+template <typename T, int KIND>
+__global__ __launch_bounds__(256) void norm_two_rows_kernel(NormArgs a, uint32_t lanes) {
+    __shared__ RowPlaces<SPAN_LANES, 1> lds;
+    const Place<T, SPAN_LANES, 1> at(lanes, a.cols);
+    const uint32_t row = a.first + blockIdx.x * (2u * at.rows(lanes)) + at.row(lanes), second = row + at.rows(lanes);
+    const bool on = row < a.n_rows, more = second < a.n_rows;
+    const size_t in = on ? (size_t)source_of(a.order, a.rows, row) * a.cols : 0, next = more ? (size_t)source_of(a.order, a.rows, second) * a.cols : 0;
+    Piece<T> x[1], y[1], other[1];
+    at.template load<true>(a.x, in, on, x);
+    at.template load<true>(a.x, next, more, y);
+    norm_row<T, KIND, SPAN_LANES, 1, true>(a, at, lanes, row, in, on, x, other, lds);
+    norm_row<T, KIND, SPAN_LANES, 1, true>(a, at, lanes, second, next, more, y, other, lds);
+}
+
 template <typename T, int KIND, bool NT>
 static hipError_t launch_rows_t(NormArgs a, hipStream_t stream) {
-    const NormShape s = norm_shape(a.n_rows, a.cols, sizeof(T) * (a.residual ? 2u : 1u));
-    const uint32_t per = s.span == SPAN_LANES ? s.threads / s.lanes : s.span == SPAN_WAVE ? s.threads / 64u : 1u;
+    const uint32_t read = sizeof(T) * (a.residual ? 2u : 1u);
+    const NormShape s = norm_shape(a.n_rows, a.cols, read);
+    const bool two = norm_turns(s.span, read, NT) == 2u;
+    const uint32_t per = (s.span == SPAN_LANES ? s.threads / s.lanes : s.span == SPAN_WAVE ? s.threads / 64u : 1u) * (two ? 2u : 1u);
     const uint64_t at_once = ((1ull << 31) / s.threads) * per;  // rows of a launch: a grid has less than 2^32 threads
     for (uint64_t first = 0; first < a.n_rows; first += at_once) {
         a.first = (uint32_t)first;
         const uint32_t n = (uint32_t)(a.n_rows - first < at_once ? a.n_rows - first : at_once), blocks = (n + per - 1u) / per;
-        if (s.span == SPAN_LANES) norm_rows_kernel<T, KIND, SPAN_LANES, 1, NT><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
+        if (two) {
+            if constexpr (NT && sizeof(T) == 2) norm_two_rows_kernel<T, KIND><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
+        } else if (s.span == SPAN_LANES) norm_rows_kernel<T, KIND, SPAN_LANES, 1, NT><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
 #define ROWS(SPAN, CH) \
     else if (s.span == SPAN && s.ch == CH) norm_rows_kernel<T, KIND, SPAN, CH, NT><<<blocks, s.threads, 0, stream>>>(a, 64u);
         ROWS(SPAN_WAVE, 1)

@@ -17,6 +17,11 @@ struct NormShape {
     uint32_t lanes, threads; // of a row (SPAN_LANES); of a workgroup
 };
 
+// Rows that lanes have at once, `read` bytes of a channel: two where a part of a wavefront has a row and a lane no more than 16 bytes of it on their way, in calls past the caches.  (us, one / two: 3,225,600 rows of
+// 128 channels in bf16 285 / 270, quantised 224 / 207; with residual, 800,000 x 256, 268 / 283; 2,000,000 x 64 in float32 170 / 175; rows of a wavefront, 131,040 x 1536 with residual 264 / 284; through the caches,
+// 393,120 x 128, 42.6 / 43.4.)
+constexpr uint32_t norm_turns(int span, uint32_t read, bool past_caches) { return past_caches && span == SPAN_LANES && read <= 2u ? 2u : 1u; }
+
 inline uint32_t norm_lanes(uint32_t pieces) {
     uint32_t lanes = 1u;
     while (lanes < pieces) lanes *= 2u;

@@ -153,6 +153,31 @@ def test_a_row_depends_on_nothing_but_itself(rows, cols, dtype):
     nr.close(dw, ew, nr.ROUND[dtype] * ew.abs() + bw, "dw")
 
 
+@pytest.mark.parametrize("rows, cols", [(1_400_003, 64), (3_800_001, 24), (360_001, 256), (11_000_001, 8)])
+def test_two_rows_of_a_lane(rows, cols):
+    """bf16 without a residual, 256 MB moved and more: the lanes of a short row have two, the last ones one or none."""
+    import paper_2605_28691_amd as sk
+
+    g = _gen(cols)
+    x, w = torch.randn(rows, cols, generator=g, device="cuda").bfloat16(), _weight(g, cols, torch.bfloat16)
+    out, q, z = sk.skiparse_rmsnorm_fwd(x, w), sk.skiparse_rmsnorm_fwd(x, w, quantize=True), sk.skiparse_quantize_int8(x)
+    into = x.clone()
+    assert torch.equal(sk.skiparse_rmsnorm_fwd(into, w, out=into), out)
+    for part in (slice(0, 300_000), slice(rows // 2, rows // 2 + 77_777), slice(rows - 100_001, rows), slice(rows - 1, rows)):
+        xs = x[part].clone()
+        assert torch.equal(sk.skiparse_rmsnorm_fwd(xs, w), out[part])
+        for p, whole in ((sk.skiparse_rmsnorm_fwd(xs, w, quantize=True), q), (sk.skiparse_quantize_int8(xs), z)):
+            assert torch.equal(p.codes, whole.codes[part]) and torch.equal(p.scales, whole.scales[part])
+    # rows that move: B = 2 grids of 4 x H x 2, H as long as it takes
+    H = rows // 16 // 4 * 4
+    n = 2 * 4 * H * 2
+    place = dict(T=4, H=H, W=2, s=2, pattern="token")
+    v = x[:n].view(2, n // 2, cols)
+    moved = sk.skiparse_rmsnorm_fwd(v, w, order="to_sparse", **place)
+    assert torch.equal(moved, ref.moved(out[:n].view(2, n // 2, cols), "to_sparse", (2, 4, H, 2), 2, "token"))
+    assert torch.equal(sk.skiparse_rmsnorm_fwd(moved, order="to_original", **place), sk.skiparse_rmsnorm_fwd(sk.skiparse_rmsnorm_fwd(v, w).contiguous()))
+
+
 GRIDS = [(1, (2, 4, 8), 2, "token"), (2, (1, 8, 4), 2, "group"), (3, (1, 9, 18), 3, "token"), (2, (2, 9, 9), 3, "group"), (1, (3, 16, 16), 4, "group"), (1, (21, 30, 52), 2, "token")]
 
 
