@@ -49,7 +49,8 @@ struct NormBwdShape {
 };
 // Parts: enough wavefronts for the chip, and no more, since a part's sums are written and read once more; few rows in few parts.  (us, 256 / 512 / 768 / 1024 parts: 32,760 x 1536, 3 wavefronts a row, 119 / 85 / 83 / 82;
 // 3840 x 5120, 10 wavefronts, 38 / 41 / 41 / 44; 390 x 1536 7.4 / 8.3 / 8.3 / 8.3; 80,640 x 1024, a wavefront a row and 4 in a workgroup, 128 / 136 / 138 / 143.)  Narrow rows' parts cost little: twice as many, and
-// of fewer rows (as the others / so: 3,225,600 x 128 496 / 485, 393,120 x 128 67.5 / 63.0, 64,260 x 128 19.2 / 17.2, 20,000 x 256 in float32 24.9 / 20.7; four times as many 505, 65.8, 21.4, 22.2).  Rows of more than 16,384 channels in float32 do
+// of fewer rows (as the others / so: 3,225,600 x 128 496 / 485, 393,120 x 128 67.5 / 63.0, 64,260 x 128 19.2 / 17.2, 20,000 x 256 in float32 24.9 / 20.7; four times as many 505, 65.8, 21.4, 22.2).
+// Rounds of a part, 8 / 4: a wavefront a row, 16,000 x 512 18.7 / 17.8, 16,000 x 1000 28.5 / 26.7.  Rows of more than 16,384 channels in float32 do
 // not fit the registers with all that the pass keeps: 4000 x 32,768 507 us, floor 420 (bf16 245, 210).
 inline NormBwdShape norm_bwd_shape(uint32_t rows, uint32_t cols) {
     const uint32_t pieces = (cols + 7u) / 8u, per_lane = (pieces + 63u) / 64u;
@@ -67,7 +68,7 @@ inline NormBwdShape norm_bwd_shape(uint32_t rows, uint32_t cols) {
     }
     const uint32_t rounds = (rows + at_once - 1u) / at_once, waves = s.threads / 64u;
     const bool narrow = s.span == SPAN_LANES;
-    const uint32_t each = rounds / (narrow ? 2u : 8u), most = (narrow ? 512u : 256u) * ((7u + waves) / waves), few = each > 256u ? each : 256u;
+    const uint32_t each = rounds / (narrow ? 2u : s.span == SPAN_WAVE ? 4u : 8u), most = (narrow ? 512u : 256u) * ((7u + waves) / waves), few = each > 256u ? each : 256u;
     s.parts = most < few ? most : few;
     if (s.parts > rounds) s.parts = rounds;
     return s;
