@@ -289,7 +289,9 @@ static hipError_t launch_rows_t(NormArgs a, hipStream_t stream) {
         const uint32_t n = (uint32_t)(a.n_rows - first < at_once ? a.n_rows - first : at_once), blocks = (n + per - 1u) / per;
         if (two) {
             if constexpr (NT && sizeof(T) == 2) norm_two_rows_kernel<T, KIND><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
-        } else if (s.span == SPAN_LANES) norm_rows_kernel<T, KIND, SPAN_LANES, 1, NT><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
+        } else if (s.span == SPAN_LANES) {
+            if constexpr (!(NT && sizeof(T) == 2 && KIND == ROWS_QUANTIZED)) norm_rows_kernel<T, KIND, SPAN_LANES, 1, NT><<<blocks, s.threads, 0, stream>>>(a, s.lanes);
+        }
 #define ROWS(SPAN, CH) \
     else if (s.span == SPAN && s.ch == CH) norm_rows_kernel<T, KIND, SPAN, CH, NT><<<blocks, s.threads, 0, stream>>>(a, 64u);
         ROWS(SPAN_WAVE, 1)
