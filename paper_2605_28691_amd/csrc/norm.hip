@@ -333,8 +333,8 @@ hipError_t launch_norm_rows(const NormArgs& all, hipStream_t stream) {
 
 // ---- gradients
 
-// dx and the weights' gradient in one pass over dy and h: 32,760 x 1536 with dx_add 75 us, and 4.4 for the parts' sums (403 MB: 5.1 TB/s), 80,640 x 5120 637 (5.2 TB/s), 6426 x 1000 float32 18 + 3.9 (77 MB: what
-// is in flight with 1024 wavefronts; with twice as many the parts cost what is won).
+// dx and the weights' gradient in one pass over dy and h: 32,760 x 1536 with dx_add 75 us, and 4.4 for the parts' sums (403 MB: 5.1 TB/s), 80,640 x 5120 637 (5.2 TB/s), 6426 x 1000 float32 15.9 + 4.0 (77 MB: what
+// is in flight with 1604 wavefronts; 17.6 + 3.9 with 1024).
 // A workgroup takes a contiguous part of the rows, and has the sums of its part for the weights' gradient in registers: each lane those of its channels.  The next row is on its way while one is
 // worked on.  LEAN, for rows so long that the registers do not hold all that: no next row, weights and dx_add are read where they are used.
 template <typename T, int SPAN, int CH, bool NT>
