@@ -271,7 +271,10 @@ bool also(PyObject* o, const at::Tensor& x, const at::Tensor*& t, at::ScalarType
     return t != nullptr && t->scalar_type() == type && t->get_device() == x.get_device();
 }
 bool of_channels(const at::Tensor* t, int64_t cols) { return t == nullptr || (t->dim() == 1 && t->size(0) == cols); }
+// Asked for in front of Py_BEGIN_ALLOW_THREADS, all of them: it throws for a tensor without memory of its own (one inside vmap or grad, which looks like any other), and an exception from between there and
+// Py_END_ALLOW_THREADS would leave the interpreter's lock released.
 void* pointer(const at::Tensor* t) { return t != nullptr ? t->data_ptr() : nullptr; }
+void* pointer(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 int elements(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 ? SKIPARSE_BF16 : t.scalar_type() == at::kFloat ? SKIPARSE_FP32 : -1; }
 // (codes, scales) as the binding's class of these
 PyObject* quantized(PyObject* type, at::Tensor&& codes, at::Tensor&& scales) {
@@ -318,10 +321,12 @@ PyObject* rmsnorm_fwd_of(PyObject* const* a) {
     at::Tensor scales, sum, out = at::empty(place.shape(*x, cols), quantize ? x->options().dtype(at::kChar) : x->options());
     if (quantize) scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
     if (r != nullptr) sum = at::empty(x->sizes(), x->options());
+    const void *const from = pointer(x), *const add = pointer(r), *const weight = pointer(w);
+    void *const sum_to = pointer(sum), *const to = pointer(out), *const scales_to = pointer(scales);
+    const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_rmsnorm_fwd(x->data_ptr(), pointer(r), pointer(w), r != nullptr ? sum.data_ptr() : nullptr, out.data_ptr(), quantize ? (float*)scales.data_ptr() : nullptr, place.B, place.T, place.H,
-                                  place.W, (int)cols, (float)PyFloat_AS_DOUBLE(a[3]), place.s, place.pattern, place.order, type, here.stream);
+    code = g_skiparse_rmsnorm_fwd(from, add, weight, sum_to, to, (float*)scales_to, place.B, place.T, place.H, place.W, (int)cols, eps, place.s, place.pattern, place.order, type, here.stream);
     Py_END_ALLOW_THREADS
     if (code != SKIPARSE_OK) return raised(code, "skiparse_rmsnorm_fwd");
     PyObject* result = quantize ? quantized(a[5], std::move(out), std::move(scales)) : THPVariable_Wrap(std::move(out));
@@ -343,9 +348,11 @@ PyObject* quantize_int8_of(PyObject* const* a) {
     Here here;
     if (type < 0 || cols != (int)cols || !place.get(a[2], x->numel() / cols) || !here.get(a[3], a[4]) || here.device != x->get_device()) return not_plain();
     at::Tensor codes = at::empty(place.shape(*x, cols), x->options().dtype(at::kChar)), scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
+    const void* const from = pointer(x);
+    void *const to = pointer(codes), *const scales_to = pointer(scales);
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_quantize_int8(x->data_ptr(), codes.data_ptr(), (float*)scales.data_ptr(), place.B, place.T, place.H, place.W, (int)cols, place.s, place.pattern, place.order, type, here.stream);
+    code = g_skiparse_quantize_int8(from, to, (float*)scales_to, place.B, place.T, place.H, place.W, (int)cols, place.s, place.pattern, place.order, type, here.stream);
     Py_END_ALLOW_THREADS
     return code != SKIPARSE_OK ? raised(code, "skiparse_quantize_int8") : quantized(a[1], std::move(codes), std::move(scales));
 }
@@ -366,10 +373,12 @@ PyObject* linear_fwd_int8_of(PyObject* const* a) {
     const size_t need = g_linear8_bytes((int)(x->numel() / K), (int)K, (int)N);
     at::Tensor space, out = at::empty(shape, x->options().dtype(at::kBFloat16));
     if (need) space = at::empty({(int64_t)need}, x->options().dtype(at::kByte));
+    const void *const xc = pointer(x), *const wc = pointer(w), *const plus = pointer(bias), *const add = pointer(residual);
+    const float *const x_scales = (const float*)pointer(xs), *const w_scales = (const float*)pointer(ws);
+    void *const to = pointer(out), *const workspace = pointer(space);
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_linear_fwd_int8(x->data_ptr(), (const float*)xs->data_ptr(), w->data_ptr(), (const float*)ws->data_ptr(), pointer(bias), pointer(residual), out.data_ptr(), place.B, place.T, place.H, place.W,
-                                      (int)K, (int)N, place.s, place.pattern, place.order, act, need ? space.data_ptr() : nullptr, need, here.stream);
+    code = g_skiparse_linear_fwd_int8(xc, x_scales, wc, w_scales, plus, add, to, place.B, place.T, place.H, place.W, (int)K, (int)N, place.s, place.pattern, place.order, act, workspace, need, here.stream);
     Py_END_ALLOW_THREADS
     return code != SKIPARSE_OK ? raised(code, "skiparse_linear_fwd_int8") : THPVariable_Wrap(std::move(out));
 }
@@ -391,10 +400,12 @@ PyObject* rmsnorm_bwd_of(PyObject* const* a) {
     if (need_dx) dx = at::empty(h->sizes(), h->options());
     if (need_dw) dw = at::empty({cols}, h->options());
     if (need) space = at::empty({(int64_t)need}, h->options().dtype(at::kByte));
+    const void *const from = pointer(dy), *const rows = pointer(h), *const weight = pointer(w), *const plus = pointer(add);
+    void *const dx_to = pointer(dx), *const dw_to = pointer(dw), *const workspace = pointer(space);
+    const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_rmsnorm_bwd(dy->data_ptr(), h->data_ptr(), pointer(w), pointer(add), need_dx ? dx.data_ptr() : nullptr, need_dw ? dw.data_ptr() : nullptr, 1, 1, 1, place.W, (int)cols,
-                                  (float)PyFloat_AS_DOUBLE(a[4]), 1, 0, 0, type, need ? space.data_ptr() : nullptr, need, here.stream);
+    code = g_skiparse_rmsnorm_bwd(from, rows, weight, plus, dx_to, dw_to, 1, 1, 1, place.W, (int)cols, eps, 1, 0, 0, type, workspace, need, here.stream);
     Py_END_ALLOW_THREADS
     if (code != SKIPARSE_OK) return raised(code, "skiparse_rmsnorm_bwd");
     PyObject* both = PyTuple_New(2);
@@ -410,7 +421,7 @@ PyObject* rmsnorm_bwd_of(PyObject* const* a) {
     return both;
 }
 
-// An exception from within (no memory for a result): the binding comes upon it by itself.
+// An exception from within (no memory for a result, a tensor without memory): the binding comes upon it by itself.
 #define PLAIN(name, count, bound)                                                \
     PyObject* plain_##name(PyObject*, PyObject* const* args, Py_ssize_t n) {     \
         if (n != count || !(bound) || g_failed == nullptr) return not_plain();   \
