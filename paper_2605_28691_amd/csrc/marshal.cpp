@@ -238,6 +238,14 @@ struct Place {
     }
 };
 
+// Without the interpreter's lock: for the C function, and for results' tensors, whose memory can take a wait for the GPU.  It is taken again whichever way that ends, an exception from within among them.
+struct Unlocked {
+    PyThreadState* const state = PyEval_SaveThread();
+    Unlocked() = default;
+    Unlocked(const Unlocked&) = delete;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 struct Here {
     int device;
     void* stream;
@@ -271,8 +279,7 @@ bool also(PyObject* o, const at::Tensor& x, const at::Tensor*& t, at::ScalarType
     return t != nullptr && t->scalar_type() == type && t->get_device() == x.get_device();
 }
 bool of_channels(const at::Tensor* t, int64_t cols) { return t == nullptr || (t->dim() == 1 && t->size(0) == cols); }
-// Asked for in front of Py_BEGIN_ALLOW_THREADS, all of them: it throws for a tensor without memory of its own (one inside vmap or grad, which looks like any other), and an exception from between there and
-// Py_END_ALLOW_THREADS would leave the interpreter's lock released.
+// Throws for a tensor without memory of its own (one inside vmap or grad, which looks like any other).
 void* pointer(const at::Tensor* t) { return t != nullptr ? t->data_ptr() : nullptr; }
 void* pointer(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 int elements(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 ? SKIPARSE_BF16 : t.scalar_type() == at::kFloat ? SKIPARSE_FP32 : -1; }
@@ -318,16 +325,17 @@ PyObject* rmsnorm_fwd_of(PyObject* const* a) {
     if (type < 0 || cols != (int)cols || !also(a[1], *x, w, x->scalar_type()) || !of_channels(w, cols) || !also(a[2], *x, r, x->scalar_type()) || (r != nullptr && r->sizes() != x->sizes()) ||
         !place.get(a[6], x->numel() / cols) || !here.get(a[7], a[8]) || here.device != x->get_device())
         return not_plain();
-    at::Tensor scales, sum, out = at::empty(place.shape(*x, cols), quantize ? x->options().dtype(at::kChar) : x->options());
-    if (quantize) scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
-    if (r != nullptr) sum = at::empty(x->sizes(), x->options());
-    const void *const from = pointer(x), *const add = pointer(r), *const weight = pointer(w);
-    void *const sum_to = pointer(sum), *const to = pointer(out), *const scales_to = pointer(scales);
     const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+    at::Tensor out, scales, sum;
     int code;
-    Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_rmsnorm_fwd(from, add, weight, sum_to, to, (float*)scales_to, place.B, place.T, place.H, place.W, (int)cols, eps, place.s, place.pattern, place.order, type, here.stream);
-    Py_END_ALLOW_THREADS
+    {
+        const Unlocked unlocked;
+        out = at::empty(place.shape(*x, cols), quantize ? x->options().dtype(at::kChar) : x->options());
+        if (quantize) scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
+        if (r != nullptr) sum = at::empty(x->sizes(), x->options());
+        code = g_skiparse_rmsnorm_fwd(pointer(x), pointer(r), pointer(w), pointer(sum), pointer(out), (float*)pointer(scales), place.B, place.T, place.H, place.W, (int)cols, eps, place.s, place.pattern,
+                                      place.order, type, here.stream);
+    }
     if (code != SKIPARSE_OK) return raised(code, "skiparse_rmsnorm_fwd");
     PyObject* result = quantize ? quantized(a[5], std::move(out), std::move(scales)) : THPVariable_Wrap(std::move(out));
     if (result == nullptr || r == nullptr) return result;
@@ -347,13 +355,14 @@ PyObject* quantize_int8_of(PyObject* const* a) {
     Place place;
     Here here;
     if (type < 0 || cols != (int)cols || !place.get(a[2], x->numel() / cols) || !here.get(a[3], a[4]) || here.device != x->get_device()) return not_plain();
-    at::Tensor codes = at::empty(place.shape(*x, cols), x->options().dtype(at::kChar)), scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
-    const void* const from = pointer(x);
-    void *const to = pointer(codes), *const scales_to = pointer(scales);
+    at::Tensor codes, scales;
     int code;
-    Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_quantize_int8(from, to, (float*)scales_to, place.B, place.T, place.H, place.W, (int)cols, place.s, place.pattern, place.order, type, here.stream);
-    Py_END_ALLOW_THREADS
+    {
+        const Unlocked unlocked;
+        codes = at::empty(place.shape(*x, cols), x->options().dtype(at::kChar));
+        scales = at::empty(place.shape(*x, cols, true), x->options().dtype(at::kFloat));
+        code = g_skiparse_quantize_int8(pointer(x), pointer(codes), (float*)pointer(scales), place.B, place.T, place.H, place.W, (int)cols, place.s, place.pattern, place.order, type, here.stream);
+    }
     return code != SKIPARSE_OK ? raised(code, "skiparse_quantize_int8") : quantized(a[1], std::move(codes), std::move(scales));
 }
 
@@ -371,15 +380,15 @@ PyObject* linear_fwd_int8_of(PyObject* const* a) {
     const at::DimVector shape = place.shape(*x, N);
     if (residual != nullptr && residual->sizes() != at::IntArrayRef(shape)) return not_plain();
     const size_t need = g_linear8_bytes((int)(x->numel() / K), (int)K, (int)N);
-    at::Tensor space, out = at::empty(shape, x->options().dtype(at::kBFloat16));
-    if (need) space = at::empty({(int64_t)need}, x->options().dtype(at::kByte));
-    const void *const xc = pointer(x), *const wc = pointer(w), *const plus = pointer(bias), *const add = pointer(residual);
-    const float *const x_scales = (const float*)pointer(xs), *const w_scales = (const float*)pointer(ws);
-    void *const to = pointer(out), *const workspace = pointer(space);
+    at::Tensor space, out;
     int code;
-    Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_linear_fwd_int8(xc, x_scales, wc, w_scales, plus, add, to, place.B, place.T, place.H, place.W, (int)K, (int)N, place.s, place.pattern, place.order, act, workspace, need, here.stream);
-    Py_END_ALLOW_THREADS
+    {
+        const Unlocked unlocked;
+        out = at::empty(shape, x->options().dtype(at::kBFloat16));
+        if (need) space = at::empty({(int64_t)need}, x->options().dtype(at::kByte));
+        code = g_skiparse_linear_fwd_int8(pointer(x), (const float*)pointer(xs), pointer(w), (const float*)pointer(ws), pointer(bias), pointer(residual), pointer(out), place.B, place.T, place.H, place.W, (int)K,
+                                          (int)N, place.s, place.pattern, place.order, act, pointer(space), need, here.stream);
+    }
     return code != SKIPARSE_OK ? raised(code, "skiparse_linear_fwd_int8") : THPVariable_Wrap(std::move(out));
 }
 
@@ -395,18 +404,17 @@ PyObject* rmsnorm_bwd_of(PyObject* const* a) {
     if (type < 0 || cols != (int)cols || !also(a[1], *dy, h, dy->scalar_type()) || h == nullptr || h->sizes() != dy->sizes() || !also(a[2], *dy, w, dy->scalar_type()) || !of_channels(w, cols) ||
         !also(a[3], *dy, add, dy->scalar_type()) || (add != nullptr && add->sizes() != dy->sizes()) || !place.get(Py_None, dy->numel() / cols) || !here.get(a[7], a[8]) || here.device != dy->get_device())
         return not_plain();
-    at::Tensor dx, dw, space;
     const size_t need = need_dw ? g_norm_bwd_bytes(place.W, (int)cols) : 0;
-    if (need_dx) dx = at::empty(h->sizes(), h->options());
-    if (need_dw) dw = at::empty({cols}, h->options());
-    if (need) space = at::empty({(int64_t)need}, h->options().dtype(at::kByte));
-    const void *const from = pointer(dy), *const rows = pointer(h), *const weight = pointer(w), *const plus = pointer(add);
-    void *const dx_to = pointer(dx), *const dw_to = pointer(dw), *const workspace = pointer(space);
     const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
+    at::Tensor dx, dw, space;
     int code;
-    Py_BEGIN_ALLOW_THREADS
-    code = g_skiparse_rmsnorm_bwd(from, rows, weight, plus, dx_to, dw_to, 1, 1, 1, place.W, (int)cols, eps, 1, 0, 0, type, workspace, need, here.stream);
-    Py_END_ALLOW_THREADS
+    {
+        const Unlocked unlocked;
+        if (need_dx) dx = at::empty(h->sizes(), h->options());
+        if (need_dw) dw = at::empty({cols}, h->options());
+        if (need) space = at::empty({(int64_t)need}, h->options().dtype(at::kByte));
+        code = g_skiparse_rmsnorm_bwd(pointer(dy), pointer(h), pointer(w), pointer(add), pointer(dx), pointer(dw), 1, 1, 1, place.W, (int)cols, eps, 1, 0, 0, type, pointer(space), need, here.stream);
+    }
     if (code != SKIPARSE_OK) return raised(code, "skiparse_rmsnorm_bwd");
     PyObject* both = PyTuple_New(2);
     if (both == nullptr) return nullptr;

@@ -1,4 +1,5 @@
-"""The binding's native module built once more for tensors of the CPU (device -1), with functions of the test's in the place of the library's, so that its whole calls run without a GPU."""
+"""The binding's native module built once more for tensors of the CPU (device -1), with functions of the test's in the place of the library's, so that its whole calls run without a GPU; and with a look at
+every tensor that it makes: whether the interpreter's lock is held meanwhile (an allocation can wait for the GPU, and other threads with it)."""
 import ctypes
 import importlib.machinery
 import importlib.util
@@ -9,9 +10,15 @@ import paper_2605_28691_amd as sk
 
 LAUNCHES = ("skiparse_rmsnorm_fwd", "skiparse_rmsnorm_bwd", "skiparse_quantize_int8", "skiparse_linear_fwd_int8")
 SPACE = 48  # bytes that the workspaces need, as the module is told
+EMPTY = """
+static at::Tensor unlocked_empty(at::IntArrayRef shape, at::TensorOptions options) {
+    if (PyGILState_Check()) throw 0;  // the call is not answered then
+    return at::empty(shape, options);
+}
+"""
 
 
-def build(folder: str, change=lambda source: source) -> str:
+def build(folder: str) -> str:
     """Compiles the module into `folder`; returns its path."""
     from paper_2605_28691_amd import build as b
 
@@ -20,9 +27,10 @@ def build(folder: str, change=lambda source: source) -> str:
     shutil.copytree(os.path.join(os.path.dirname(b.HERE), "include"), os.path.join(folder, "include"))
     with open(os.path.join(b.CSRC, "marshal.cpp")) as f:
         source = f.read()
-    assert source.count("is_cuda()") == 2
+    assert source.count("is_cuda()") == 2 and source.count("at::empty(") == 10
+    source = source.replace("is_cuda()", "is_cpu()").replace("at::empty(", "unlocked_empty(").replace("\nnamespace {\n", EMPTY + "\nnamespace {\n", 1)
     with open(os.path.join(csrc, "marshal.cpp"), "w") as f:
-        f.write(change(source.replace("is_cuda()", "is_cpu()")))
+        f.write(source)
     kept = b.CSRC, b.MARSHAL
     b.CSRC, b.MARSHAL = csrc, os.path.join(folder, "_marshal.so")
     try:
