@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void linear_int8_row_kernel(LinearArgs a) {
     if (lane >= CH) return;
     const uint32_t n = n0 + lane;
     const LinearEpilogue& e = a.e;
-    float z = act_value(e.act, int8_value(sum, a.x_scales[0], a.w_scales[n], e.bias != nullptr ? (float)((const __bf16*)e.bias)[n] : 0.f));
+    float z = act_value(e.act, int8_value_far(sum, a.x_scales[0], a.w_scales[n], e.bias != nullptr ? (float)((const __bf16*)e.bias)[n] : 0.f));
     if (e.residual != nullptr) z = int8_plus(z, (float)((const __bf16*)e.residual)[n]);
     ((__bf16*)e.out)[n] = (__bf16)z;
 }

@@ -93,6 +93,15 @@ __device__ __attribute__((always_inline)) inline float int8_value(int sum, float
 #pragma clang fp contract(off)
     return fmaf((float)sum * x_scale, w_scale, bias);
 }
+// A sum is below 2^31, so from scales of 2^97 on its product with a row's could leave float32's range where that with the channel's scale as well does not.  Rows of 2^64 and more have theirs times 2^-32, the
+// channels' times 2^32 then: powers of two, so no rounding changes.  A channel's that leaves the range by that is kept at its end, since a sum of 0 is 0 times it; all others are infinite either way.
+__device__ __attribute__((always_inline)) inline bool int8_far(float x_scale) { return fabsf(x_scale) >= 0x1p64f; }
+__device__ __attribute__((always_inline)) inline float int8_value_far(int sum, float x_scale, float w_scale, float bias) {
+    const bool far = int8_far(x_scale);
+    float up = w_scale * 0x1p32f;
+    if (__builtin_isinf(up) && !__builtin_isinf(w_scale)) up = copysignf(3.4028234663852886e38f, w_scale);
+    return int8_value(sum, far ? x_scale * 0x1p-32f : x_scale, far ? up : w_scale, bias);
+}
 __device__ __attribute__((always_inline)) inline float int8_plus(float z, float residual) {
 #pragma clang fp contract(off)
     return z + residual;
@@ -141,12 +150,22 @@ struct Scales<FM, FN, true> {
             }
         return c;
     }
-    __device__ __attribute__((always_inline)) inline static f32x4 values(const f32x4& sums, float x_scale, const Channels& c, int j) {
-        const i32x4 s = __builtin_bit_cast(i32x4, sums);
-        f32x4 z;
+    // sums of the lane's row -> z, in their place
+    __device__ __attribute__((always_inline)) inline static void values(f32x4 (&z)[FN], float x_scale, const Channels& c) {
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(int8_far(x_scale)) != 0, 0)) {
+            values<true>(z, x_scale, c);
+            return;
+        }
+        values<false>(z, x_scale, c);
+    }
+    template <bool FAR>
+    __device__ __attribute__((always_inline)) inline static void values(f32x4 (&z)[FN], float x_scale, const Channels& c) {
 #pragma unroll
-        for (int e = 0; e < 4; e++) z[e] = int8_value(s[e], x_scale, c.w[j][e], c.bias[j][e]);
-        return z;
+        for (int j = 0; j < FN; j++) {
+            const i32x4 s = __builtin_bit_cast(i32x4, z[j]);
+#pragma unroll
+            for (int e = 0; e < 4; e++) z[j][e] = FAR ? int8_value_far(s[e], x_scale, c.w[j][e], c.bias[j][e]) : int8_value(s[e], x_scale, c.w[j][e], c.bias[j][e]);
+        }
     }
 };
 
@@ -572,8 +591,8 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
         if (i + 1 < FM) r = out.residual(a, i + 1);
         f32x4 z[FN];
         if constexpr (INT8) {
-            const float x_scale = scales.row(i, own);
-            each<FN>([&](auto J) __attribute__((always_inline)) { z[decltype(J)::value] = scales.values(acc_take<4 * (i * FN + decltype(J)::value)>(), x_scale, channels, decltype(J)::value); });
+            each<FN>([&](auto J) __attribute__((always_inline)) { z[decltype(J)::value] = acc_take<4 * (i * FN + decltype(J)::value)>(); });
+            scales.values(z, scales.row(i, own), channels);
         } else {
 #pragma unroll
             for (int j = 0; j < FN; j++) z[j] = take(acc[i][j]);
@@ -608,7 +627,8 @@ __global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a, TileMap t
         const float x_scale = scales.row(0, lane);
         const typename Scales<1, FN, true>::Channels channels = scales.channels(lane);
 #pragma unroll
-        for (int j = 0; j < FN; j++) acc[j] = scales.values(__builtin_bit_cast(f32x4, sums[j]), x_scale, channels, j);
+        for (int j = 0; j < FN; j++) acc[j] = __builtin_bit_cast(f32x4, sums[j]);
+        scales.values(acc, x_scale, channels);
         out.row(a, i, acc, res, lane);
         return;
     }
@@ -754,7 +774,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearArgs a
             f32x4 bias = {0.f, 0.f, 0.f, 0.f};
             if (e.bias != nullptr) add(bias, e.bias, c);
 #pragma unroll
-            for (int i = 0; i < 4; i++) z[i] = int8_value(s[i], x_scale, w_scale[i], bias[i]);
+            for (int i = 0; i < 4; i++) z[i] = int8_value_far(s[i], x_scale, w_scale[i], bias[i]);
             return z;
         }
 #pragma unroll
