@@ -782,6 +782,11 @@ def _is_quantized(q, what: str, shape=None) -> Quantized:
     return q
 
 
+def _from_16(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy where it does not begin at a multiple of 16 bytes, as the scales of a slice of rows."""
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 def _same_type(like, *tensors) -> None:
     dtype = like.dtype
     for t in tensors:
@@ -899,7 +904,8 @@ def skiparse_linear_fwd_int8_workspace_bytes(rows: int, in_features: int, out_fe
 def skiparse_linear_fwd_int8(x: Quantized, w: Quantized, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None, act: str = "none", order: str = "same", T: int = 0,
                              H: int = 0, W: int = 0, s: int = 1, pattern: str = "token", out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """act(x w^T + bias) + residual in bf16 from 8-bit integers: x [..., in] and w [out, in] as skiparse_quantize_int8 or skiparse_rmsnorm_fwd leave them, bias [out], residual and result
-    [..., out] bf16.  order as in skiparse_linear_fwd; the scales' rows move with the codes'.  `out` (may be residual) and `workspace` are buffers to use."""
+    [..., out] bf16.  order as in skiparse_linear_fwd; the scales' rows move with the codes'.  A slice of either's rows will do, Quantized(q.codes[3:], q.scales[3:]); scales that begin off a multiple of 16
+    bytes are copied first.  `out` (may be residual) and `workspace` are buffers to use."""
     p, a, place = PATTERNS[pattern], ACTS[act], None
     if out is None and workspace is None:
         if order != "same" and type(x) is Quantized:
@@ -924,6 +930,7 @@ def skiparse_linear_fwd_int8(x: Quantized, w: Quantized, bias: torch.Tensor | No
     if residual is not None and residual.shape != shape:
         raise ValueError(f"residual must have the result's shape {shape}")
     _here(xc, xs, wc, ws, bias, residual, out, workspace)
+    xs, ws = _from_16(xs), _from_16(ws)
     workspace, size = _space(workspace, xc, "skiparse_linear_fwd_int8_workspace_bytes", grid[0] * grid[1] * grid[2] * grid[3], K, N)
     _skiparse_linear_fwd_int8(xc, xs, wc, ws, bias, residual, out, *grid, K, N, s, p, ORDERS[order], a, workspace, size, _stream())
     return out

@@ -37,6 +37,7 @@ int elem_size(int dtype) {
 }
 
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool misaligned_float(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }  // written one at a time: as those of any rows of a larger tensor lie
 
 // [a, a + a_bytes) and [b, b + b_bytes) share at least one byte
 bool overlap2(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
@@ -842,8 +843,9 @@ int skiparse_rmsnorm_fwd(const void* x, const void* residual, const void* weight
     size_t rows;
     const int rc = rows_common(B, T, H, W, cols, s, pattern, order, dtype, &moved, &rows);
     if (rc != SKIPARSE_OK) return rc;
-    for (const void* p : {x, residual, weight, (const void*)sum, (const void*)out, (const void*)out_scales})
+    for (const void* p : {x, residual, weight, (const void*)sum, (const void*)out})
         if (p && misaligned(p)) return SKIPARSE_EINVAL;
+    if (misaligned_float(out_scales)) return SKIPARSE_EINVAL;
     const size_t bytes = rows * cols * elem_size(dtype);
     const Span sx = {x, bytes}, sr = {residual, bytes}, sw = {weight, (size_t)cols * elem_size(dtype)}, ss = {sum, bytes};
     const Span so = {out, out_scales ? rows * cols : bytes}, sc = {out_scales, rows * sizeof(float)};
@@ -867,7 +869,7 @@ int skiparse_quantize_int8(const void* x, void* codes, float* scales, int B, int
     size_t rows;
     const int rc = rows_common(B, T, H, W, cols, s, pattern, order, dtype, &moved, &rows);
     if (rc != SKIPARSE_OK) return rc;
-    if (misaligned(x) || misaligned(codes) || misaligned(scales)) return SKIPARSE_EINVAL;
+    if (misaligned(x) || misaligned(codes) || misaligned_float(scales)) return SKIPARSE_EINVAL;
     const Span sx = {x, rows * cols * elem_size(dtype)}, so = {codes, rows * cols}, sc = {scales, rows * sizeof(float)};
     if (touches(so, {sx, sc}) || touches(sc, {sx})) return SKIPARSE_EINVAL;
     NormArgs a = {};

@@ -366,7 +366,7 @@ PyObject* quantize_int8_of(PyObject* const* a) {
     return code != SKIPARSE_OK ? raised(code, "skiparse_quantize_int8") : quantized(a[1], std::move(codes), std::move(scales));
 }
 
-// x, w, bias, residual, activation, Quantized, PLACE, device and stream functions
+// x, w, bias, residual, activation, Quantized, PLACE, device and stream functions.  Scales that begin off 16 bytes are the binding's to copy.
 PyObject* linear_fwd_int8_of(PyObject* const* a) {
     const at::Tensor *x, *xs, *w, *ws, *bias, *residual;
     int act;
@@ -379,6 +379,7 @@ PyObject* linear_fwd_int8_of(PyObject* const* a) {
         return not_plain();
     const at::DimVector shape = place.shape(*x, N);
     if (residual != nullptr && residual->sizes() != at::IntArrayRef(shape)) return not_plain();
+    if ((((uintptr_t)pointer(xs) | (uintptr_t)pointer(ws)) & 15u) != 0) return not_plain();
     const size_t need = g_linear8_bytes((int)(x->numel() / K), (int)K, (int)N);
     at::Tensor space, out;
     int code;

@@ -153,3 +153,14 @@ def test_refused_by_the_library(host):
     for call, good, _ in _calls(host):
         with pytest.raises(sk.SkiparseError):
             call(*good)
+
+
+def test_scales_of_a_slice_are_the_bindings(host):
+    """Scales that begin off 16 bytes are copied there; the module leaves them alone."""
+    n, at = host.native, (hm.device, hm.stream)
+    q, w8 = sk.Quantized(torch.zeros(9, 64, dtype=torch.int8), torch.ones(9)), sk.Quantized(torch.zeros(16, 64, dtype=torch.int8), torch.ones(16))
+    assert q.scales.data_ptr() % 16 == w8.scales.data_ptr() % 16 == 0
+    for i, j, answered in ((0, 0, True), (4, 4, True), (1, 0, False), (0, 2, False), (3, 5, False), (5, 8, False)):
+        got = n.plain_linear_fwd_int8(sk.Quantized(q.codes[i:], q.scales[i:]), sk.Quantized(w8.codes[j:j + 8], w8.scales[j:j + 8]), None, None, 0, sk.Quantized, None, *at)
+        assert (got is not NotImplemented) == answered == bool(host.calls)
+        host.calls.clear()
