@@ -7,7 +7,10 @@ import importlib
 import os
 import subprocess
 import sysconfig
+import tempfile
 import warnings
+
+from . import accumulators
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -73,8 +76,25 @@ def _build_one(lib: str, sources, verbose: bool, save_temps: bool) -> str:
         out = lib + ".tmp"
     cmd += ["-o", out] + [os.path.join(CSRC, s) for s in sources]
     _run(cmd, verbose)
+    if accumulators.SOURCE in sources:
+        try:
+            accumulators.check(assembly(accumulators.SOURCE))
+        except RuntimeError:
+            os.remove(out)  # sums may be wrong: no library then
+            raise
     os.replace(out, lib)
     return lib
+
+
+def assembly(source: str) -> str:
+    """What the compiler makes of the kernels of `source`, with the flags of the library."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    flags = [f for f in FLAGS if f != "-shared"] + os.environ.get("SKIPARSE_EXTRA_FLAGS", "").split()
+    with tempfile.TemporaryDirectory() as tmp:
+        out = os.path.join(tmp, "kernels.s")
+        _run([hipcc] + flags + ["--cuda-device-only", "-S", os.path.join(CSRC, source), "-o", out], False)
+        with open(out) as f:
+            return f.read()
 
 
 def _run(cmd, verbose: bool) -> None:

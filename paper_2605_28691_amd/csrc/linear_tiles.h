@@ -336,15 +336,17 @@ __device__ __attribute__((always_inline)) inline f32x4 take(const f32x4& acc) {
     return f32x4{w, x, y, z};
 }
 
-// Accumulators by their registers' names, four for block R / 4: of the products in 8-bit integers, whose walk over three buffers has several ways out, where the compiler would move them about.  It knows no
-// more of them than that begin() overwrites them; with fewer than 256 other values at once it has no use for accumulation registers of its own (tests/test_norm_shape.py looks at what it makes).
+// Accumulators by their registers' names, four for block R / 4: of the products in 8-bit integers, whose walk over three buffers has several ways out, where the compiler would move them about.  It does not know
+// that they hold anything.  acc_own() overwrites all of them as far as it can tell, so nothing of its own is in one there; it stands round the walk, in it every 16 products, and on the way out in front of every
+// 16 rows.  And the build looks through what was made of these kernels (accumulators.py), and fails if any other instruction of theirs names an accumulation register.  (All of them as clobbers of every
+// statement cost a wait state each: 32,760 x 1536 -> 8960 with GELU 551 -> 561 us.)
 #define ACC10(t) "a" #t "0", "a" #t "1", "a" #t "2", "a" #t "3", "a" #t "4", "a" #t "5", "a" #t "6", "a" #t "7", "a" #t "8", "a" #t "9"
 #define ACC16 ACC10(), "a10", "a11", "a12", "a13", "a14", "a15"
 #define ACC64 ACC10(), ACC10(1), ACC10(2), ACC10(3), ACC10(4), ACC10(5), "a60", "a61", "a62", "a63"
 #define ACC256 ACC10(), ACC10(1), ACC10(2), ACC10(3), ACC10(4), ACC10(5), ACC10(6), ACC10(7), ACC10(8), ACC10(9), ACC10(10), ACC10(11), ACC10(12), ACC10(13), ACC10(14), ACC10(15), ACC10(16), ACC10(17), \
     ACC10(18), ACC10(19), ACC10(20), ACC10(21), ACC10(22), ACC10(23), ACC10(24), "a250", "a251", "a252", "a253", "a254", "a255"
 template <int REGISTERS>
-__device__ __attribute__((always_inline)) inline void acc_begin() {
+__device__ __attribute__((always_inline)) inline void acc_own() {
     static_assert(REGISTERS == 16 || REGISTERS == 64 || REGISTERS == 256, "a tile's");
     if constexpr (REGISTERS == 16) asm volatile("" ::: ACC16);
     else if constexpr (REGISTERS == 64) asm volatile("" ::: ACC64);
@@ -425,9 +427,11 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
     };
     const Scales<FM, FN, INT8> scales(a, m0 + wm * (FM * 16u), n0 + wn * (FN * 16u), lane);  // on their way before the walk begins
     f32x4 acc[INT8 ? 1 : FM][INT8 ? 1 : FN];  // sums begin with the bias; those of a part, and whole numbers, with 0
+    constexpr int ACCS = FM * FN * 4;
     if constexpr (INT8) {
-        acc_begin<FM * FN * 4>();
+        acc_own<ACCS>();
         each<FM * FN>([&](auto G) __attribute__((always_inline)) { acc_clear<4 * decltype(G)::value>(); });
+        acc_own<ACCS>();
     } else
 #pragma unroll
     for (int j = 0; j < FN; j++) {
@@ -465,8 +469,10 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
         constexpr int LOADS = decltype(LOADC)::value;
         each<MF>([&](auto G) __attribute__((always_inline)) {
             constexpr int g = decltype(G)::value;
-            if constexpr (INT8) acc_product<4 * g>(f.q[g % FN], f.p[g / FN]);
-            else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[g / FN][g % FN]) : "v"(f.q[g % FN]), "v"(f.p[g / FN]));
+            if constexpr (INT8) {
+                if constexpr (g % 16 == 0) acc_own<ACCS>();
+                acc_product<4 * g>(f.q[g % FN], f.p[g / FN]);
+            } else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[g / FN][g % FN]) : "v"(f.q[g % FN]), "v"(f.p[g / FN]));
             // number i of n stands behind product i * MF / n
             constexpr int first = (g * RD + MF - 1) / MF, last = ((g + 1) * RD + MF - 1) / MF;
             each<last - first>([&](auto I) __attribute__((always_inline)) { fragment(next, from, first + decltype(I)::value); });
@@ -568,6 +574,7 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
     if (slot != ~0u) {  // a part: sums as they lie in the registers, for linear_join_kernel
         f32x4* const to = (f32x4*)a.partial + ((size_t)slot * 4u + wave) * (FM * FN * 64u) + lane;
         if constexpr (INT8) {
+            acc_own<ACCS>();
             each<FM * FN>([&](auto G) __attribute__((always_inline)) { to[decltype(G)::value * 64] = acc_take<4 * decltype(G)::value>(); });
             return;
         }
@@ -591,6 +598,7 @@ __global__ __launch_bounds__(256, 65536 / (BM * BN) < 4 ? 1 : 65536 / (BM * BN) 
         if (i + 1 < FM) r = out.residual(a, i + 1);
         f32x4 z[FN];
         if constexpr (INT8) {
+            acc_own<ACCS>();
             each<FN>([&](auto J) __attribute__((always_inline)) { z[decltype(J)::value] = acc_take<4 * (i * FN + decltype(J)::value)>(); });
             scales.values(z, scales.row(i, own), channels);
         } else {
