@@ -783,8 +783,8 @@ def _is_quantized(q, what: str, shape=None) -> Quantized:
 
 
 def _from_16(t: torch.Tensor) -> torch.Tensor:
-    """t, or a copy where it does not begin at a multiple of 16 bytes, as the scales of a slice of rows."""
-    return t if t.data_ptr() % 16 == 0 else t.clone()
+    """t, or a copy where it does not begin at a multiple of 16 bytes, as the scales of a slice of rows.  (What lies in strides is refused as it stands.)"""
+    return t if t.data_ptr() % 16 == 0 or not t.is_contiguous() else t.clone()
 
 
 def _same_type(like, *tensors) -> None:

@@ -29,6 +29,11 @@ def test_products_of_a_slice(K, N):
         for rows in (1, 20, 300):
             assert torch.equal(sk.skiparse_linear_fwd_int8(_rows(sk, q, 0, rows), _rows(sk, w, at, n)), whole[:rows, at:at + n]), (at, n, rows)
     assert torch.equal(sk.skiparse_linear_fwd_int8(_rows(sk, q, 3, 40), _rows(sk, w, 5, 64)), whole[3:43, 5:69])
+    # in strides they are refused, wherever they begin
+    for at in (0, 1):
+        strided = torch.ones(80, device="cuda")[at::2]
+        with pytest.raises(ValueError):
+            sk.skiparse_linear_fwd_int8(sk.Quantized(q.codes[:40], strided), w)
 
 
 def test_a_slice_in_a_graph():
