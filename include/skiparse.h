@@ -299,7 +299,8 @@ int skiparse_linear_bwd(const void* dy, const void* x, const void* x_scales, con
  *   stays where it is.  rows = B*T*H*W (plain rows: a grid 1 x 1 x rows).  All tensors are of one type.
  *   sum: NULL, or where h, rounded, is kept; only with a residual.  It may be x or residual.  y is made of the sum as it is before that rounding.
  *   out: y rounded to the type of x, with out_scales NULL; or, with out_scales [rows], the int8 codes and scales of y.  Where rows keep their places out may be x (if it is no codes, and sum is not x).
- *   Nothing else may overlap.  out_scales (and the quantiser's scales) lie at any multiple of 4 bytes.  cols a multiple of 8 up to 32,768; eps from 2^-126 to 2^100.  Sums in float32, of values times a power of two where their squares (or products with dy) would leave its range; one rounding.
+ *   Nothing else may overlap.  out_scales (and the quantiser's scales) lie at any multiple of 4 bytes.  cols a multiple of 8 up to 32,768; eps from 2^-126 to 2^100.  Sums in float32, of values times
+ *   a power of two where their squares would leave its range, or products with dy exceed it (those of dy weight and h below 2^-126 have as many digits as a float32 of that size); one rounding.
  * Rows in 8-bit integers: m = largest |v| of the row (at least 2^-118), code = rne(v * (127 / m)), scale = m / 127, all decisions in float32: codes are -127 .. 127, a value is code * scale.  A row of
  *   zeros has scale 1; one that holds a value that is not finite has codes 0 and scale NaN, so that what a product makes of it is NaN too.  The norm's codes are those of v = h weight, which is y up to
  *   the row's factor r (h weight beyond float32's range is not finite).

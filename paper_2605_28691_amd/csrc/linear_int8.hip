@@ -2,8 +2,8 @@
 // The products are those of linear_tiles.h with v_mfma_i32_16x16x64_i8: its operands are 16 bytes a lane, as those of the bf16 product are, and k is summed over, so the walk over k, what it
 // loads and how it lies in LDS are the same bytes, two codes in the place of one number.  What is left of the sums on the way out are scales: those of a wavefront's rows and channels are asked for before
 // its walk begins.  Parts of a sum are whole numbers too: however a product is cut, a row's bits are the same.
-// Large products are bound by the matrix cores at the board's power limit: 16,384^3 2915 TOP/s (a library's product without an epilogue 2434), 80,640 x 5120 -> 20,480 2.74 without an epilogue and
-// 2.62 with GELU (6.2 and 6.4 ms).  Small ones by what stands outside the walk: 32,760 x 1536 -> 1536, three rounds of 256 tiles, 84 us.  A tile of it has 1.5 until its loads leave, 2.5 until they land, 5 for its
+// Large products are bound by the matrix cores at the board's power limit: 16,384^3 2925 TOP/s (a library's product without an epilogue 2384), 80,640 x 5120 -> 20,480 2.68 POP/s without an epilogue and
+// 2.45 to 2.62 with GELU (6.3 and 6.44 to 6.9 ms: cards differ).  Small ones by what stands outside the walk: 32,760 x 1536 -> 1536, three rounds of 256 tiles, 77 to 84 us.  A tile of it has 1.5 until its loads leave, 2.5 until they land, 5 for its
 // results, 12 with a residual, which all CUs move at once, and the rest for twelve steps (20 to 23 with two buffers, 14 on codes of zero; without any results the product took 71 of then 87).  Loads sent off
 // earlier in a step and waited for later, in a second barrier, were 3 % slower, results past the caches as well, and first tiles that begin at four different times no faster.
 #include "linear_tiles.h"

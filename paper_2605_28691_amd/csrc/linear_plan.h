@@ -110,8 +110,8 @@ inline uint32_t few_blocks(uint32_t M, uint32_t N, uint32_t K) { return N >= 409
 // The same in 8-bit integers, whose weights take half the time to read; K in codes.  (us, these / tiles: 5120 -> 5120, 2 rows 8.8 / 15.8, 16 rows 9.9 / 15.9, 32 rows 11.9 / 16.2; 8960 -> 1536, 16 rows 8.8 / 14.5,
 // 32 rows 11.5 / 14.8; 5120 -> 30,720, 16 rows 39.9 / 39.5, 32 rows 46.3 / 40.8; 64 -> 11,200, 2 rows 5.9 / 3.6.  One row: 5120 -> 5120 7.2 / 15.8, 64 -> 11,200 3.6 / 3.5.)
 inline bool linear_few8(uint32_t M, uint32_t N, uint32_t K) { return M == 1u || (K >= 512u && (M <= 16u || (M <= 32u && N < 16384u))); }
-// (us, one / two blocks of 16 channels: 5120 -> 5120, 2 rows 9.9 / 8.8, 16 rows 11.1 / 9.9, 17 rows 13.8 / 10.6; 1536 -> 8960, 16 rows 8.6 / 9.3, 17 rows 11.6 / 10.4; 8960 -> 1536, 16 rows 8.8 / 11.9.)
-inline uint32_t few_blocks8(uint32_t M, uint32_t N, uint32_t K) { return N >= 4096u && (K >= 4096u || M > 16u) ? 2u : 1u; }
+// The rule above, as it happens.  (us, one / two blocks of 16 channels: 5120 -> 5120, 2 rows 9.9 / 8.8, 16 rows 11.1 / 9.9, 17 rows 13.8 / 10.6; 1536 -> 8960, 16 rows 8.6 / 9.3, 17 rows 11.6 / 10.4; 8960 -> 1536, 16 rows 8.8 / 11.9.)
+inline uint32_t few_blocks8(uint32_t M, uint32_t N, uint32_t K) { return few_blocks(M, N, K); }
 
 // K in pairs of codes
 inline LinearPlan plan_linear8(uint32_t M, uint32_t N, uint32_t K, bool act) { return plan_linear(M, N, K, act ? LINEAR_TILE8_ACT : LINEAR_TILE8, LINEAR_SHAPES8); }

@@ -3,8 +3,8 @@
 //     h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h r w          int8: codes and scale of h w (int8_rows.h), the scale times r: r is the same for a row and changes no code
 //     g = dy w,  u = h r,  dx = r (g - u mean(g u)) + dx_add,  dw = sum over the rows of dy u
 // Bound by HBM bandwidth: every tensor is moved once, a row stays in registers between its sum and its result (norm_shape.h: which lanes have it).  Of the norm's codes the largest value and the sum of squares
-// come from one pass over these registers: codes do not need r.  80,640 x 5120 in bf16: with residual and sum, into the sparse layout, 560 us (3.3 GB, 5.9 TB/s; a copy of 2 GiB reaches 4.96), in 8-bit
-// integers 199 us (1.24 GB, 6.2); 32,760 x 1536 with residual in codes 57 us (5.3).
+// come from one pass over these registers: codes do not need r.  80,640 x 5120 in bf16: with residual and sum, into the sparse layout, 565 us (3.3 GB, 5.85 TB/s; a copy of 2 GiB reaches 4.9, permute.hip 6.5), in 8-bit
+// integers 200 us (1.24 GB, 6.2); 32,760 x 1536 with residual in codes 58 us (5.2).
 #include "int8_rows.h"
 #include "kernels.h"
 #include "norm_shape.h"
