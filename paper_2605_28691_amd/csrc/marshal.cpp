@@ -16,6 +16,8 @@
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cxxabi.h>
+
 #include <climits>
 #include <cstring>
 #include <tuple>
@@ -239,11 +241,12 @@ struct Place {
 };
 
 // Without the interpreter's lock: for the C function, and for results' tensors, whose memory can take a wait for the GPU.  It is taken again whichever way that ends, an exception from within among them.
+// In a process that ends, a daemon thread that asks for it is taken off its stack instead: let through here and by PLAIN, since both would end the process in an abort otherwise.
 struct Unlocked {
     PyThreadState* const state = PyEval_SaveThread();
     Unlocked() = default;
     Unlocked(const Unlocked&) = delete;
-    ~Unlocked() { PyEval_RestoreThread(state); }
+    ~Unlocked() noexcept(false) { PyEval_RestoreThread(state); }
 };
 
 struct Here {
@@ -436,6 +439,8 @@ PyObject* rmsnorm_bwd_of(PyObject* const* a) {
         if (n != count || !(bound) || g_failed == nullptr) return not_plain();   \
         try {                                                                    \
             return name##_of(args);                                              \
+        } catch (const abi::__forced_unwind&) { /* of a thread that is ended */  \
+            throw;                                                               \
         } catch (...) {                                                          \
             PyErr_Clear();                                                       \
             return not_plain();                                                  \

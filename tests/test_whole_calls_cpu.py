@@ -164,3 +164,37 @@ def test_scales_of_a_slice_are_the_bindings(host):
         got = n.plain_linear_fwd_int8(sk.Quantized(q.codes[i:], q.scales[i:]), sk.Quantized(w8.codes[j:j + 8], w8.scales[j:j + 8]), None, None, 0, sk.Quantized, None, *at)
         assert (got is not NotImplemented) == answered == bool(host.calls)
         host.calls.clear()
+
+
+# A daemon thread that does nothing but a whole call, of a function that returns 0 at once.
+AT_THE_END = """
+import ctypes
+import sys
+import threading
+import time
+import torch
+import _host_marshal as hm
+import paper_2605_28691_amd as sk
+
+n = hm.Host(sys.argv[1]).native
+n.bind("skiparse_quantize_int8", ctypes.cast(ctypes.CDLL(None).sched_yield, ctypes.c_void_p).value)
+x, calls = torch.randn(4, 64), []
+
+
+def loop():
+    while True:
+        calls.append(n.plain_quantize_int8(x, sk.Quantized, None, hm.device, hm.stream) is not NotImplemented)
+        del calls[:-1]
+
+
+threading.Thread(target=loop, daemon=True).start()
+time.sleep(0.2)
+assert calls and all(calls)
+"""
+
+
+def test_a_daemon_thread_at_the_end_of_the_process(path):
+    """It is ended where it asks for the interpreter's lock, and the process with the code of its own."""
+    for _ in range(3):
+        done = subprocess.run([sys.executable, "-c", AT_THE_END, path], cwd=HERE, env={**os.environ, "PYTHONPATH": os.path.dirname(HERE)}, stderr=subprocess.PIPE, text=True, timeout=100)
+        assert done.returncode == 0, (done.returncode, done.stderr)
